@@ -375,6 +375,95 @@ int dag_attn_prefill_paged(const dag_paged_prefill_desc_t* desc, const void* q, 
                            int32_t hkv, int32_t head_dim, float softmax_scale, void* ws,
                            size_t ws_bytes, void* stream);
 
+/* A paged KV cache held in 8 bits: codes in e4m3 (OCP, as torch.float8_e4m3fn) and one fp32 scale for each (page, KV head)
+ * of K and of V; a code c stands for scale * c.  Half the bytes of the bf16 pools, and decode is bound by bytes.
+ * Storage formats (page size 16), P = n_pages:
+ *   K pool [P][hkv][head_dim/16][16][16]  element (page, h, slot, d) at [page][h][d/16][slot][d%16]
+ *   V pool [P][hkv][head_dim][16]         element (page, h, slot, d) at [page][h][d][slot]
+ *   scales [P][hkv], finite and positive for every page that holds tokens
+ * The struct lives on the HOST, its pointers are DEVICE memory (pools 16-byte aligned). */
+typedef struct {
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;
+  float* v_scale;
+  int32_t n_pages, hkv, head_dim; /* head_dim 64 or 128 */
+} dag_kv_q8_t;
+
+/* Section 3.2 (a fired transition's new KV blocks join the cache references of its token), into an 8-bit cache: token t
+ * goes to slots[t] (= 16 * page + slot in the page, as dag_kv_tables writes them; a slot outside the pool, -1 say, leaves the
+ * token out), its key rotated at pos[t] as dag_kv_append_rope does, its value as is.
+ * k_new / v_new [n_tokens][hkv][head_dim] DAG_BF16 or DAG_F32 DEVICE, slots and pos DEVICE int32.
+ * The new tokens of a page stand next to each other in ascending slots without a gap, and a page has one such run in a call
+ * (a page with two is left with undefined contents, no other memory is touched).
+ * A run that starts in slot 0 begins the page: what was there is dropped, the scale is that of the new tokens, the slots
+ * behind them hold zeros.  Any other run adds to the page, whose slots in front hold tokens.
+ * Scale of (page, head): the smallest power of two, 2^-100 at least, with which all new elements of the head are within
+ * +-448, or the page's scale so far if that is larger; codes are rounded to nearest even.  When the scale grows, the codes that are there are
+ * divided by the same factor and rounded again (exact unless they fall under 2^-6 by it).  An Inf or NaN is stored as NaN and
+ * does not count for the scale.  No atomics: the same call gives the same bits.
+ * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_HIP. */
+int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new,
+                          const void* v_new, float theta, dag_dtype_t dtype, void* stream);
+
+/* dag_attn_decode over an 8-bit cache: same description, same attention of every live branch's query over (shared context, own
+ * tokens).  q / out [n_live][hq][head_dim] bf16 DEVICE, q already rotated; hq a multiple of kv->hkv, hq / hkv <= 32.
+ * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), and a branch
+ * that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
+ * never followed; the host bounds are trusted.  softmax_scale may be of either sign.  Sums, maxima and partial results are
+ * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches); the call
+ * allocates nothing and does not synchronise; calls that overlap need a workspace each. */
+size_t dag_decode_q8_workspace_bytes(const dag_decode_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);
+int dag_attn_decode_q8(const dag_decode_desc_t* desc, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
+                       float softmax_scale, void* ws, size_t ws_bytes, void* stream);
+
+/* dag_attn_decode_segments over an 8-bit cache: same description (seg_reader_len included: the incremental prefill of a few new
+ * tokens), otherwise as dag_attn_decode_q8 (three launches). */
+size_t dag_decode_segments_q8_workspace_bytes(const dag_decode_seg_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);
+int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* desc, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
+                                float softmax_scale, void* ws, size_t ws_bytes, void* stream);
+
+/* Pages of rows that grow, kept on the GPU.  A row is what owns pages: a live branch, a node.  All pointers DEVICE int32.
+ * Row r with n tokens holds the first ceil(n / 16) entries of its line of `table`; the first `*free_count` entries of `free_pages` are
+ * the pages that nobody holds, taken from the end.  With dag_kv_release and dag_kv_tables a step needs no round trip to the host:
+ * what they write is what dag_kv_append_rope_q8 (slots, pos) and the decode descriptions (page_off / pages / row_len as
+ * branch_page_off / branch_pages / branch_len or seg_page_off / seg_pages / seg_len) take, inside a captured graph too. */
+typedef struct {
+  int32_t n_rows, page_size; /* page_size must be 16                                             */
+  int32_t max_row_pages;     /* width of the table                                               */
+  int32_t n_pages;           /* length of free_pages: pages of the pool, at most 2^27 - 1         */
+  int32_t* table;            /* [n_rows][max_row_pages] page ids in token order                  */
+  int32_t* free_pages;       /* [n_pages]                                                        */
+} dag_kv_rows_t;
+
+/* Bytes of DEVICE workspace (4-byte aligned) of the two calls below; they may share one if they are on one stream. */
+size_t dag_kv_tables_workspace_bytes(int32_t n_rows);
+
+/* Rows with ended[r] != 0 give their pages back: free_pages[*free_count ..] gets them in the order of rows and tokens,
+ * row_len_out is 0 for them and row_len for the others, free_count_out the new number of free pages.  row_len_out may be row_len and
+ * free_count_out may be free_count. */
+int dag_kv_release(const dag_kv_rows_t* rows, const int32_t* ended, const int32_t* row_len, int32_t* row_len_out,
+                   const int32_t* free_count, int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Row r gets new_len[r] >= 0 more tokens and the pages for them: the table's line is continued, row_len_out = row_len + new_len, and
+ * page k of the call (in the order of rows and tokens) is free_pages[*free_count - 1 - k]; free_count_out is what is left.
+ *   new_off [n_rows+1]   sums of new_len: the new tokens of row r are new_off[r] .. new_off[r+1] - 1
+ *   slots   [max_new]    16 * page + slot of every new token
+ *   pos     [max_new]    pos0[r] (0 without pos0) + its place in the row: adaptive positions (section 4.2) where pos0 is the
+ *                        position of the row's first token; both nullable
+ *   page_off [n_rows+1], pages [max_pages]  the pages of every row, its new ones included, row after row; nullable
+ *   refused [1]          number of rows that got less than they asked for, which is nothing; nullable
+ * A row is refused if its tokens would not fit the table's line, or if its pages and those that the rows in front of it need (refused
+ * ones included that would fit their line) are more than are free: its slots are -1 and its length stays.  Rows that need no page are never
+ * refused for want of pages.  max_new and max_pages are HOST values, the lengths of the arrays; entries past them are dropped.
+ * The sums of new_len and of the listed pages have to fit an int32.  Negative lengths count as 0.  row_len_out may be row_len and
+ * free_count_out may be free_count.  Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE,
+ * DAG_ERR_HIP. */
+int dag_kv_tables(const dag_kv_rows_t* rows, const int32_t* new_len, const int32_t* row_len, int32_t* row_len_out,
+                  const int32_t* free_count, int32_t* free_count_out, int32_t* new_off, int32_t* slots, int64_t max_new,
+                  const int32_t* pos0, int32_t* pos, int32_t* page_off, int32_t* pages, int64_t max_pages, int32_t* refused,
+                  void* ws, size_t ws_bytes, void* stream);
+
 /* Host-side scheduler of the execution phase (section 3.2: the plan as a Petri net whose places
  * are the DAG nodes, one transition per node with its parents as input places; section 3.3, Eq. 1:
  * the enabled-transition frontier fires as a whole and the marking advances when all of it is

@@ -91,6 +91,16 @@ class dag_sched_step_t(C.Structure):
                 [(name, C.POINTER(C.c_int32)) for name in _SCHED_ARRAYS])
 
 
+class dag_kv_q8_t(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("hkv", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class dag_kv_rows_t(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("page_size", C.c_int32), ("max_row_pages", C.c_int32), ("n_pages", C.c_int32),
+                ("table", C.c_void_p), ("free_pages", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -131,6 +141,16 @@ def lib():
         L.dag_prefill_paged_workspace_bytes.restype = C.c_size_t
         L.dag_attn_prefill_paged.argtypes = [C.POINTER(dag_paged_prefill_desc_t), vp, vp, vp, i32, vp, vp, i32, i32,
                                              i32, f32, vp, C.c_size_t, vp]
+        L.dag_kv_append_rope_q8.argtypes = [C.POINTER(dag_kv_q8_t), vp, vp, i64, vp, vp, f32, C.c_int, vp]
+        for name, desc in (("decode_q8", dag_decode_desc_t), ("decode_segments_q8", dag_decode_seg_desc_t)):
+            need, call = getattr(L, "dag_%s_workspace_bytes" % name), getattr(L, "dag_attn_" + name)
+            need.argtypes, need.restype = [C.POINTER(desc), i32, i32, i32], C.c_size_t
+            call.argtypes = [C.POINTER(desc), C.POINTER(dag_kv_q8_t), vp, vp, i32, f32, vp, C.c_size_t, vp]
+        L.dag_kv_tables_workspace_bytes.argtypes = [i32]
+        L.dag_kv_tables_workspace_bytes.restype = C.c_size_t
+        L.dag_kv_release.argtypes = [C.POINTER(dag_kv_rows_t), vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.dag_kv_tables.argtypes = [C.POINTER(dag_kv_rows_t), vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp,
+                                    C.c_size_t, vp]
         L.dag_copy_calibration.argtypes = [vp, vp, C.c_size_t, vp]
         L.dag_sched_create.argtypes = [i32, vp, vp, vp, vp, i32, i32, C.POINTER(vp)]
         L.dag_sched_destroy.argtypes = [vp]
@@ -143,7 +163,8 @@ def lib():
                      "dag_attn_prefill", "dag_attn_prefill_prepared", "dag_prefill_prepare_v",
                      "dag_kv_append_rope", "dag_attn_decode", "dag_attn_decode_static", "dag_attn_decode_segments",
                      "dag_sched_create", "dag_attn_prefill_paged", "dag_copy_calibration",
-                     "dag_attn_prefill_bwd",
+                     "dag_attn_prefill_bwd", "dag_kv_append_rope_q8", "dag_attn_decode_q8", "dag_attn_decode_segments_q8",
+                     "dag_kv_release", "dag_kv_tables",
                      "dag_sched_step"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -284,6 +305,17 @@ def dag_prefill_prepare_v(meta, v, hq, workspace=None):
                                        workspace.numel(), _stream()))
 
 
+_DECODE_ARRAYS = ("group_branch_off", "shared_page_off", "shared_pages", "shared_len", "branch_page_off",
+                  "branch_pages", "branch_len", "branch_pos")
+
+
+def _device_arrays(arrays):
+    for name, x in arrays.items():
+        if x is not None and (x.dtype != torch.int32 or not x.is_contiguous()):
+            raise TypeError("%s has to be a contiguous int32 tensor" % name)
+    return arrays
+
+
 class DecodeDesc:
     """Device copies of the decode description arrays + the ctypes struct."""
 
@@ -305,6 +337,20 @@ class DecodeDesc:
                                    *[self.t[n].data_ptr() for n in
                                      ("group_branch_off", "shared_page_off", "shared_pages", "shared_len",
                                       "branch_page_off", "branch_pages", "branch_len", "branch_pos")])
+
+
+    @classmethod
+    def on_device(cls, n_groups, n_live, max_shared_pages, max_branch_pages, max_group_size, group_branch_off=None,
+                  shared_page_off=None, shared_pages=None, shared_len=None, branch_page_off=None, branch_pages=None,
+                  branch_len=None, branch_pos=None):
+        """A description whose arrays are on the device already (int32 tensors, kept alive here), with the host bounds."""
+        self = cls.__new__(cls)
+        arrays = (group_branch_off, shared_page_off, shared_pages, shared_len, branch_page_off, branch_pages, branch_len,
+                  branch_pos)
+        self.t = _device_arrays(dict(zip(_DECODE_ARRAYS, arrays)))
+        self.c = dag_decode_desc_t(n_groups, n_live, PAGE, max_shared_pages, max_branch_pages, max_group_size,
+                                   *[0 if x is None else x.data_ptr() for x in arrays])
+        return self
 
 
 def dag_kv_append_rope(ddesc, k_new, v_new, k_pool, v_pool, theta):
@@ -363,6 +409,19 @@ class SegDecodeDesc:
             self.c.seg_reader_len = self.t["seg_reader_len"].data_ptr()
 
 
+    @classmethod
+    def on_device(cls, n_live, n_segments, max_seg_pages, max_readers, total_readers, seg_page_off, seg_pages, seg_len,
+                  seg_reader_off, seg_readers, branch_entry_off, branch_entries, seg_reader_len=None):
+        """A description whose arrays are on the device already (int32 tensors, kept alive here), with the host bounds."""
+        self = cls.__new__(cls)
+        arrays = (seg_page_off, seg_pages, seg_len, seg_reader_off, seg_readers, branch_entry_off, branch_entries,
+                  seg_reader_len)
+        self.t = _device_arrays(dict(zip(_SEG_ARRAYS + ("seg_reader_len",), arrays)))
+        self.c = dag_decode_seg_desc_t(n_live, n_segments, PAGE, max_seg_pages, max_readers, total_readers,
+                                       *[0 if x is None else x.data_ptr() for x in arrays])
+        return self
+
+
 def dag_decode_segments_workspace_bytes(sdesc, hq, hkv, head_dim):
     return int(lib().dag_decode_segments_workspace_bytes(C.byref(sdesc.c), hq, hkv, head_dim))
 
@@ -412,6 +471,133 @@ def dag_attn_prefill_paged(pdesc, q, k_pool, v_pool, out, workspace, lse=None, s
     _check(lib().dag_attn_prefill_paged(C.byref(pdesc.c), _ptr(q), _ptr(k_pool), _ptr(v_pool), k_pool.shape[0],
                                         _ptr(out), _ptr(lse) if lse is not None else None, hq, hkv, d,
                                         float(softmax_scale), _ptr(workspace), workspace.numel(), _stream()))
+
+
+class KvCacheQ8:
+    """The tensors of an 8-bit cache (kept alive here) + the ctypes struct.  k_pool [P][hkv][d/16][16][16] and v_pool
+    [P][hkv][d][16] float8_e4m3fn, k_scale / v_scale [P][hkv] float32."""
+
+    def __init__(self, k_pool, v_pool, k_scale, v_scale):
+        p, hkv, d = v_pool.shape[:3]
+        if tuple(k_pool.shape) != (p, hkv, d // 16, PAGE, 16) or tuple(v_pool.shape) != (p, hkv, d, PAGE):
+            raise ValueError("pools are [pages][heads][dim / 16][16][16] and [pages][heads][dim][16]")
+        if tuple(k_scale.shape) != (p, hkv) or tuple(v_scale.shape) != (p, hkv):
+            raise ValueError("scales are [pages][heads]")
+        for x, dt in ((k_pool, torch.float8_e4m3fn), (v_pool, torch.float8_e4m3fn), (k_scale, torch.float32),
+                      (v_scale, torch.float32)):
+            if x.dtype != dt or not x.is_contiguous():
+                raise TypeError("pools are contiguous float8_e4m3fn, scales contiguous float32")
+        self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
+        self.hkv, self.head_dim = hkv, d
+        self.c = dag_kv_q8_t(k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, hkv, d)
+
+    @classmethod
+    def empty(cls, n_pages, hkv, head_dim, device):
+        """A cache without tokens (zeros, scales one)."""
+        pool = lambda *shape: torch.zeros((n_pages, hkv) + shape, dtype=torch.uint8, device=device).view(  # noqa: E731
+            torch.float8_e4m3fn)
+        one = lambda: torch.ones((n_pages, hkv), dtype=torch.float32, device=device)  # noqa: E731
+        return cls(pool(head_dim // 16, PAGE, 16), pool(head_dim, PAGE), one(), one())
+
+
+def _on_current_device(*tensors):
+    here = torch.cuda.current_device()
+    for x in tensors:
+        if x is not None and x.numel() and x.get_device() != here:
+            raise ValueError("tensors have to be on the current device, cuda:%d: got %s" % (here, x.device))
+
+
+def _rows_of(x, heads, dim, what):
+    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim or not x.is_contiguous():
+        raise ValueError("%s has to be a contiguous [rows][%d][%d]" % (what, heads, dim))
+
+
+def dag_kv_append_rope_q8(cache, slots, pos, k_new, v_new, theta):
+    n = slots.numel()
+    _rows_of(k_new, cache.hkv, cache.head_dim, "k_new")
+    _rows_of(v_new, cache.hkv, cache.head_dim, "v_new")
+    if not (k_new.shape[0] == v_new.shape[0] == pos.numel() == n) or k_new.dtype != v_new.dtype:
+        raise ValueError("slots, pos, k_new and v_new are of one length, k_new and v_new of one type")
+    _device_arrays({"slots": slots, "pos": pos})
+    _on_current_device(slots, pos, k_new, v_new, cache.k_pool)
+    _check(lib().dag_kv_append_rope_q8(C.byref(cache.c), slots.data_ptr(), pos.data_ptr(), n, k_new.data_ptr(),
+                                       v_new.data_ptr(), theta, _dtype_code(k_new), _stream()))
+
+
+def dag_decode_q8_workspace_bytes(ddesc, cache, hq):
+    return lib().dag_decode_q8_workspace_bytes(C.byref(ddesc.c), hq, cache.hkv, cache.head_dim)
+
+
+def dag_decode_segments_q8_workspace_bytes(sdesc, cache, hq):
+    return lib().dag_decode_segments_q8_workspace_bytes(C.byref(sdesc.c), hq, cache.hkv, cache.head_dim)
+
+
+def _decode_q8(call, desc, q, cache, out, workspace, softmax_scale):
+    n, hq, d = q.shape
+    if n != desc.c.n_live or d != cache.head_dim or out.shape != q.shape:
+        raise ValueError("q and out are [n_live][heads][head_dim]")
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous():
+        raise TypeError("q and out are contiguous bfloat16")
+    _on_current_device(q, out, cache.k_pool, workspace)
+    _check(call(C.byref(desc.c), C.byref(cache.c), q.data_ptr(), out.data_ptr(), hq,
+                d ** -0.5 if softmax_scale is None else softmax_scale, workspace.data_ptr(), workspace.numel(), _stream()))
+
+
+def dag_attn_decode_q8(ddesc, q, cache, out, workspace, softmax_scale=None):
+    _decode_q8(lib().dag_attn_decode_q8, ddesc, q, cache, out, workspace, softmax_scale)
+
+
+def dag_attn_decode_segments_q8(sdesc, q, cache, out, workspace, softmax_scale=None):
+    _decode_q8(lib().dag_attn_decode_segments_q8, sdesc, q, cache, out, workspace, softmax_scale)
+
+
+class KvRows:
+    """The page table of rows that grow: table [rows][width] and the stack of free pages [pages], int32 (kept alive here), the
+    ctypes struct and the calls' workspace (calls that overlap need rows objects of their own)."""
+
+    def __init__(self, table, free_pages):
+        self.table, self.free_pages = table, free_pages
+        _device_arrays({"table": table, "free_pages": free_pages})
+        n_rows, width = table.shape
+        self.c = dag_kv_rows_t(n_rows, PAGE, width, free_pages.numel(), table.data_ptr(), free_pages.data_ptr())
+        self.workspace = torch.empty(int(lib().dag_kv_tables_workspace_bytes(n_rows)), dtype=torch.uint8, device=table.device)
+
+
+def _at(x):
+    return 0 if x is None else x.data_ptr()
+
+
+def _lengths(rows, **arrays):
+    n = {"slots": None, "pos": None, "pages": None, "free_count": 1, "free_count_out": 1, "refused": 1,
+         "new_off": rows.c.n_rows + 1, "page_off": rows.c.n_rows + 1}
+    for name, x in arrays.items():
+        want = n.get(name, rows.c.n_rows)
+        if x is not None and want is not None and x.numel() != want:
+            raise ValueError("%s has %d elements, not %d" % (name, x.numel(), want))
+    _device_arrays(arrays)
+    _on_current_device(rows.table, *arrays.values())
+
+
+def dag_kv_release(rows, ended, row_len, row_len_out, free_count, free_count_out):
+    _lengths(rows, ended=ended, row_len=row_len, row_len_out=row_len_out, free_count=free_count, free_count_out=free_count_out)
+    _check(lib().dag_kv_release(C.byref(rows.c), ended.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(),
+                                free_count.data_ptr(), free_count_out.data_ptr(), rows.workspace.data_ptr(),
+                                rows.workspace.numel(), _stream()))
+
+
+def dag_kv_tables(rows, new_len, row_len, row_len_out, free_count, free_count_out, new_off, slots, pos0=None, pos=None,
+                  page_off=None, pages=None, refused=None):
+    """`pos` is as long as `slots`; entries past the ends of `slots` and `pages` are dropped."""
+    if pos is not None and pos.numel() != slots.numel():
+        raise ValueError("pos and slots are of one length")
+    _lengths(rows, new_len=new_len, row_len=row_len, row_len_out=row_len_out, free_count=free_count,
+             free_count_out=free_count_out, new_off=new_off, slots=slots, pos0=pos0, pos=pos, page_off=page_off, pages=pages,
+             refused=refused)
+    _check(lib().dag_kv_tables(C.byref(rows.c), new_len.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(),
+                               free_count.data_ptr(), free_count_out.data_ptr(), new_off.data_ptr(), slots.data_ptr(),
+                               slots.numel(), _at(pos0), _at(pos), _at(page_off), _at(pages),
+                               0 if pages is None else pages.numel(), _at(refused), rows.workspace.data_ptr(),
+                               rows.workspace.numel(), _stream()))
 
 
 class Scheduler:

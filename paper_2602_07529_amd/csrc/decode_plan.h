@@ -253,3 +253,36 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
   p->bytes = off + 256;
   return DAG_OK;
 }
+
+// Decode over an 8-bit cache: slices of one length for the shared pages and one for the own ones, as long as the step still has a wave for
+// every fourth of a SIMD's places.
+struct Q8Plan {
+  int rb_max, chunk_a, splits_a, chunk_b, splits_b, items_a, items_b;
+  size_t off_ml, bytes;
+};
+inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Plan* p) {
+  if (!d) return DAG_ERR_NULL;
+  if (d->n_groups < 0 || d->n_live < 0 || d->max_shared_pages < 0 || d->max_branch_pages < 0 || d->max_group_size < 0) return DAG_ERR_BAD_LEN;
+  if (d->page_size != PAGE) return DAG_ERR_UNSUPPORTED;
+  if (hq < 1 || hkv < 1 || hq % hkv != 0 || hq / hkv > 32) return DAG_ERR_UNSUPPORTED;
+  if (D != 64 && D != 128) return DAG_ERR_UNSUPPORTED;
+  const int shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages;
+  p->rb_max = (int)dag_ceil_div((int64_t)d->max_group_size * (hq / hkv), 32);
+  const int64_t base_a = (int64_t)d->n_groups * hkv * p->rb_max, base_b = (int64_t)d->n_live * hkv;
+  auto halved = [](int c, int least, int64_t base, int pages, int64_t want) {
+    while (c > least && base * dag_ceil_div(pages, c) < want) c /= 2;
+    return c;
+  };
+  p->chunk_a = halved(128, 8, base_a, shared, 512);
+  p->chunk_b = halved(64, 4, base_b, own, 1024);
+  p->splits_a = base_a > 0 ? (int)dag_ceil_div(shared, p->chunk_a) : 0;
+  p->splits_b = (int)dag_ceil_div(own, p->chunk_b);
+  const int64_t ia = base_a * p->splits_a, ib = base_b * p->splits_b;
+  const int64_t rows = (int64_t)d->n_live * ((int64_t)p->splits_a + p->splits_b) * hq;
+  if (ia + ib > INT32_MAX || rows > INT32_MAX || (int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;
+  p->items_a = (int)ia;
+  p->items_b = (int)ib;
+  p->off_ml = dag_align_up((size_t)rows * D * 4, 256);
+  p->bytes = p->off_ml + dag_align_up((size_t)rows * 2 * 4, 256) + 256;
+  return DAG_OK;
+}
