@@ -254,8 +254,9 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
   return DAG_OK;
 }
 
-// Decode over an 8-bit cache: slices of one length for the shared pages and one for the own ones, as long as the step still has a wave for
-// every fourth of a SIMD's places.
+// Decode over an 8-bit cache: slices of about one length, so that there are Q8_WAVES of them and all run at once (what was measured
+// stands at stream_slice), no shorter than Q8_LEAST_PAGES.
+constexpr int Q8_WAVES = 1536, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
 struct Q8Plan {
   int rb_max, chunk_a, splits_a, chunk_b, splits_b, items_a, items_b;
   size_t off_ml, bytes;
@@ -269,14 +270,15 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
   const int shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages;
   p->rb_max = (int)dag_ceil_div((int64_t)d->max_group_size * (hq / hkv), 32);
   const int64_t base_a = (int64_t)d->n_groups * hkv * p->rb_max, base_b = (int64_t)d->n_live * hkv;
-  auto halved = [](int c, int least, int64_t base, int pages, int64_t want) {
-    while (c > least && base * dag_ceil_div(pages, c) < want) c /= 2;
-    return c;
+  const int64_t even_share = dag_ceil_div(base_a * shared + base_b * own, Q8_WAVES);
+  const int most = even_share < Q8_LEAST_PAGES ? Q8_LEAST_PAGES : even_share > Q8_MOST_PAGES ? Q8_MOST_PAGES : (int)even_share;
+  auto cut = [&](int pages, int* splits, int* chunk) {  // slices of one length, of whole pairs of pages
+    *splits = (int)dag_ceil_div(pages, most);
+    *chunk = *splits > 0 ? (int)dag_ceil_div(dag_ceil_div(pages, *splits), 2) * 2 : 2;
+    *splits = (int)dag_ceil_div(pages, *chunk);
   };
-  p->chunk_a = halved(128, 8, base_a, shared, 512);
-  p->chunk_b = halved(64, 4, base_b, own, 1024);
-  p->splits_a = base_a > 0 ? (int)dag_ceil_div(shared, p->chunk_a) : 0;
-  p->splits_b = (int)dag_ceil_div(own, p->chunk_b);
+  cut(base_a > 0 ? shared : 0, &p->splits_a, &p->chunk_a);
+  cut(own, &p->splits_b, &p->chunk_b);
   const int64_t ia = base_a * p->splits_a, ib = base_b * p->splits_b;
   const int64_t rows = (int64_t)d->n_live * ((int64_t)p->splits_a + p->splits_b) * hq;
   if (ia + ib > INT32_MAX || rows > INT32_MAX || (int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;

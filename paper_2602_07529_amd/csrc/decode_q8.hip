@@ -4,8 +4,8 @@
 // dag_attn_decode_segments_q8 : contexts as lists of KV segments (that of dag_attn_decode_segments).
 //
 // out = sum_j softmax_j(scale q . k_j) v_j.  With the key scale s of page(j) the exponent of key j is t_j = (scale log2(e) s) q . c_j,
-// one product more a score, and with the value scale z its probability enters the second product as z 2^(t_j - m); the
-// sum of the probabilities has none.  The codes become bf16 in registers, which holds every e4m3 value, so nothing but
+// one product more a score, and with the value scale z its probability enters the second product as 2^(t_j - m + log2 z); the
+// sum of the probabilities is without z.  The codes become bf16 in registers, which holds every e4m3 value, so nothing but
 // the probabilities is rounded, as with a bf16 cache.  A step has to read 2 hkv D bytes a token, half of what that one needs.
 //
 // Pool formats (16 tokens a page) are operand images, as those of the bf16 cache:
@@ -73,7 +73,12 @@ struct Block {         // 32 keys (two pages)
   u32x4 v[D / 32];     // v[db]: the slots of page H of dimension 32 db + L
 };
 
-template <int D>
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const uint8_t* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4*)p);
+  else return *(const u32x4*)p;
+}
+template <int D, bool ONCE>
 __device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pages, int rel, int last_rel, int hk, int L, int H) {
   const int pg0 = __builtin_amdgcn_readlane(pages, rel & 63), pg1 = __builtin_amdgcn_readlane(pages, min(rel + 1, last_rel) & 63);
   const int slot = (L & 3) + 4 * (L >> 3);
@@ -81,9 +86,9 @@ __device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pa
   const uint8_t* const kp = c.k_pool + ((L >> 2) & 1 ? base1 : base0) + H * 256 + slot * 16;
   const uint8_t* const vp = c.v_pool + (H ? base1 : base0) + L * 16;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.k[s] = *(const u32x4*)(kp + s * 512);
+  for (int s = 0; s < D / 32; ++s) b.k[s] = load16<ONCE>(kp + s * 512);
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.v[s] = *(const u32x4*)(vp + s * 512);
+  for (int s = 0; s < D / 32; ++s) b.v[s] = load16<ONCE>(vp + s * 512);
 }
 
 // A block some of whose tokens are hidden from some rows only (the new tokens of a node): a value that is no number may not reach the rows
@@ -122,10 +127,13 @@ __device__ __forceinline__ void hide_not_numbers(Block<D>& b, f32x16* O, int key
 // The exponent's reference m is raised only where a score is more than this above it (log2): the rescale of the sums stays rare.
 constexpr float Q8_TH = 3.f;
 
-// One block: scores, probabilities, their product with the values.  key0: first key of the block; keys from `lim` on are hidden from this
-// lane's row; len: the smallest lim of the wave; slots from vlen on hold no token.
+// One block: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e), lv: log2 of
+// its value scale.  A lane's 16 scores are of one page, so their largest is found among the plain products, one multiply-add gives
+// the exponent with the value scale in it, and the sum of a lane loses that factor again once.
+// key0: first key of the block; keys from `lim` on are hidden from this lane's row; len: the smallest lim of the wave; slots from vlen on
+// hold no token.
 template <int D, typename QF>
-__device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, float& m, float& l, float ks, float vs, int key0, int len,
+__device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, float& m, float& l, float ks, float lv, int key0, int len,
                                               int lim, int vlen, int H) {
   f32x16 S;
 #pragma unroll
@@ -135,8 +143,6 @@ __device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, 
     S = mfma32(codes_to_bf16(b.k[s][0], b.k[s][1]), qop(2 * s), S);
     S = mfma32(codes_to_bf16(b.k[s][2], b.k[s][3]), qop(2 * s + 1), S);
   }
-#pragma unroll
-  for (int r = 0; r < 16; ++r) S[r] *= ks;
   if (key0 + 32 > len) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[r] = key0 + 16 * H + r < lim ? S[r] : -INFINITY;
@@ -144,6 +150,7 @@ __device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, 
   float bm = S[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
+  bm *= ks;
   bm = fmaxf(bm, __shfl_xor(bm, 32));
   if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) {
     const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
@@ -156,14 +163,15 @@ __device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, 
   }
   f32x8 p0, p1;
   float sum = 0.f;
+  const float ref = lv - m;
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
-    const float x = __builtin_amdgcn_exp2f(S[r] - m), y = __builtin_amdgcn_exp2f(S[8 + r] - m);
-    sum += x + y;
-    p0[r] = x * vs;  // (rounded to bf16 below, as the probabilities over a bf16 cache are)
-    p1[r] = y * vs;
+    p0[r] = __builtin_amdgcn_exp2f(fmaf(S[r], ks, ref));
+    p1[r] = __builtin_amdgcn_exp2f(fmaf(S[8 + r], ks, ref));
+    sum += p0[r] + p1[r];
   }
-  l += sum;
+  l = fmaf(sum, __builtin_amdgcn_exp2f(-lv), l);
+  // (rounded to bf16, as the probabilities over a bf16 cache are)
   const bf16x8 pb0 = __builtin_convertvector(p0, bf16x8), pb1 = __builtin_convertvector(p1, bf16x8);
   if (key0 + 32 > vlen) {  // slots without a token may hold codes that are no number
 #pragma unroll
@@ -182,8 +190,11 @@ __device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, 
   }
 }
 
-// Pages [p0, p1) of one list against the wave's 32 rows, two pages at a time, the next two on their way meanwhile.
-template <int D, typename QF>
+// Pages [p0, p1) of one list against the wave's 32 rows, two pages at a time, the next two on their way meanwhile (four of them are no
+// faster).  What bounds it is how the pages come from memory: pages that nobody else reads pass the caches by (ONCE; 16 groups of 8 over
+// 8192 | 1024 tokens 114 -> 101 us), and 1,300 to 1,800 waves ask for them, those of the KV heads of a page next to each other (-> 94 us =
+// 5.7 TB/s; 2,048 waves 99, 3,072 102 to 123; the loads alone of 2,048 waves take 98.6).
+template <int D, bool ONCE, typename QF>
 __device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk,
                                              float sc, int lane, QF&& qop, f32x16* O, float& m, float& l) {
   const int L = lane & 31, H = lane >> 5, np = p1 - p0;
@@ -194,49 +205,57 @@ __device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pa
   m = -1e30f;
   l = 0.f;
   int pg = 0;
-  float ksv = 0.f, vsv = 0.f;
+  float ksv = 0.f, lvv = 0.f;
   auto window = [&](int rel) __attribute__((always_inline)) {  // of 64 pages, a lane each: id (clamped to the pool) and scales
     pg = min(max(pages[p0 + min(rel + lane, np - 1)], 0), c.n_pages - 1);
-    ksv = c.k_scale[(size_t)pg * c.hkv + hk] * sc;
-    vsv = c.v_scale[(size_t)pg * c.hkv + hk];
+    ksv = c.k_scale[(size_t)pg * c.hkv + hk] * fabsf(sc);
+    lvv = __builtin_amdgcn_logf(c.v_scale[(size_t)pg * c.hkv + hk]);
   };
   auto of_page = [&](float x, int rel) __attribute__((always_inline)) {  // of page rel + H
     const float a = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), rel & 63));
     const float b = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), min(rel + 1, np - 1) & 63));
     return H ? b : a;
   };
-  Block<D> b0, b1;
-  float k0, v0, k1, v1;
-  auto load = [&](Block<D>& b, float& ks, float& vs, int rel) __attribute__((always_inline)) {
+  struct Ahead {
+    Block<D> b;
+    float ks, lv;
+  };
+  Ahead x0, x1;
+  auto load = [&](Ahead& x, int rel) __attribute__((always_inline)) {
+    if (rel >= np) return;
     if ((rel & 63) == 0) {
       window(rel);
-      asm volatile("" ::"v"(ksv), "v"(vsv));  // arrived: a wait for them later would also wait for the blocks in flight
+      asm volatile("" ::"v"(ksv), "v"(lvv));  // arrived: a wait for them later would also wait for the blocks in flight
     }
-    ks = of_page(ksv, rel);
-    vs = of_page(vsv, rel);
-    load_block<D>(b, c, pg, rel, np - 1, hk, L, H);
+    x.ks = of_page(ksv, rel);
+    x.lv = of_page(lvv, rel);
+    load_block<D, ONCE>(x.b, c, pg, rel, np - 1, hk, L, H);
   };
-  load(b0, k0, v0, 0);
+  auto compute = [&](Ahead& x, int rel) __attribute__((always_inline)) {
+    compute_block<D>(x.b, qop, O, m, l, x.ks, x.lv, (p0 + rel) * PAGE, len, lim, vlen, H);
+  };
+  load(x0, 0);
   for (int rel = 0;;) {
-    if (rel + 2 < np) load(b1, k1, v1, rel + 2);
-    compute_block<D>(b0, qop, O, m, l, k0, v0, (p0 + rel) * PAGE, len, lim, vlen, H);
-    rel += 2;
-    if (rel >= np) break;
-    if (rel + 2 < np) load(b0, k0, v0, rel + 2);
-    compute_block<D>(b1, qop, O, m, l, k1, v1, (p0 + rel) * PAGE, len, lim, vlen, H);
-    rel += 2;
-    if (rel >= np) break;
+    load(x1, rel + 2);
+    compute(x0, rel);
+    if ((rel += 2) >= np) break;
+    load(x0, rel + 2);
+    compute(x1, rel);
+    if ((rel += 2) >= np) break;
   }
 }
 
-// Query operands of the wave's rows in LDS: step 2 s + u has dims 16 (2 s + H) + 8 u .. of row L.
+// Query operands of the wave's rows in LDS: step 2 s + u has dims 16 (2 s + H) + 8 u .. of row L, with the sign of the softmax scale.
 template <int D>
-__device__ __forceinline__ void stage_q(bf16x8* qs, const uint16_t* row, int lane) {
+__device__ __forceinline__ void stage_q(bf16x8* qs, const uint16_t* row, float sc, int lane) {
   const uint16_t* const p = row + 16 * (lane >> 5);
+  const uint32_t sign = sc < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    qs[(2 * s) * 64 + lane] = *(const bf16x8*)(p + 32 * s);
-    qs[(2 * s + 1) * 64 + lane] = *(const bf16x8*)(p + 32 * s + 8);
+  for (int s = 0; s < D / 16; ++s) {
+    u32x4 x = *(const u32x4*)(p + 32 * (s >> 1) + 8 * (s & 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] ^= sign;
+    qs[s * 64 + lane] = __builtin_bit_cast(bf16x8, x);
   }
 }
 
@@ -253,12 +272,14 @@ __device__ __forceinline__ void store_part(float* part_o, float* part_ml, size_t
 
 // A wave to a work item: a slice of a group's shared pages against 32 of its (branch, query head) rows of a KV head, or a slice of a
 // branch's own pages against its rows.
-template <int D>
+template <int D, bool ONCE>
 __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
   __shared__ bf16x8 qs[(D / 16) * 64];
   const int lane = threadIdx.x, L = lane & 31, H = lane >> 5;
   const bool shared = (int)blockIdx.x < a.items_a;
   int x = shared ? blockIdx.x : blockIdx.x - a.items_a;
+  const int hk = x % a.hkv;
+  x /= a.hkv;
   const int splits = shared ? a.splits_a : a.splits_b, split = x % splits;
   x /= splits;
   int row0 = 0;
@@ -266,8 +287,6 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
     row0 = x % a.rb_max * 32;
     x /= a.rb_max;
   }
-  const int hk = x % a.hkv;
-  x /= a.hkv;
   const int branch0 = shared ? a.group_branch_off[x] : x;
   const int nrows = shared ? (a.group_branch_off[x + 1] - branch0) * a.G : a.G;
   const int32_t* const pages = shared ? a.shared_pages + a.shared_page_off[x] : a.branch_pages + a.branch_page_off[x];
@@ -283,17 +302,17 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
     if (row_ok && H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
     return;
   }
-  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, lane);
+  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
   auto qop = [&](int s) { return qs[s * 64 + lane]; };
   f32x16 O[D / 32];
   float m, l;
-  stream_slice<D>(a.kv, pages, p0, p1, len, len, len, hk, a.sc, lane, qop, O, m, l);
+  stream_slice<D, ONCE>(a.kv, pages, p0, p1, len, len, len, hk, a.sc, lane, qop, O, m, l);
   l += __shfl_xor(l, 32);
   if (row_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
 }
 
 // The same for the items that k_seg_plan listed.
-template <int D>
+template <int D, bool ONCE>
 __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
   __shared__ bf16x8 qs[(D / 16) * 64];
   const SegArgs& a = args.s;
@@ -329,11 +348,11 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
     }
   }
   const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
-  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, lane);
+  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
   auto qop = [&](int s) { return qs[s * 64 + lane]; };
   f32x16 O[D / 32];
   float m, l;
-  stream_slice<D>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, lane, qop, O, m, l);
+  stream_slice<D, ONCE>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, lane, qop, O, m, l);
   l += __shfl_xor(l, 32);
   if (store_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
 }
@@ -477,7 +496,9 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   a.sc = softmax_scale * 1.4426950408889634f;
   hipStream_t stream = (hipStream_t)stream_;
   if (p.items_a + p.items_b > 0) {
-    hipLaunchKernelGGL(D == 128 ? k_q8_decode<128> : k_q8_decode<64>, dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
+    auto* const kernel = p.rb_max <= 1 ? (D == 128 ? k_q8_decode<128, true> : k_q8_decode<64, true>)
+                                       : (D == 128 ? k_q8_decode<128, false> : k_q8_decode<64, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge<128> : k_q8_merge<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, a);
@@ -547,7 +568,9 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
     const int64_t waves = dag_ceil_div(d->n_segments, 64);
     hipLaunchKernelGGL(k_seg_plan, dim3(1), dim3((unsigned)(waves * 64 < PLAN_THREADS ? waves * 64 : PLAN_THREADS)), 0, stream, a);
     DAG_LAUNCH_CHECK();
-    hipLaunchKernelGGL(D == 128 ? k_q8_decode_seg<128> : k_q8_decode_seg<64>, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
+    auto* const kernel = p.rb_max <= 1 ? (D == 128 ? k_q8_decode_seg<128, true> : k_q8_decode_seg<64, true>)
+                                       : (D == 128 ? k_q8_decode_seg<128, false> : k_q8_decode_seg<64, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge_seg<128> : k_q8_merge_seg<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, args);
