@@ -67,28 +67,25 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(bf16x8, x);
 }
 
+__device__ __forceinline__ float other_half(float x) { return __uint_as_float(dag_other_group<32>(__float_as_uint(x))); }  // of lane ^ 32
+
 template <int D>
 struct Block {         // 32 keys (two pages)
   u32x4 k[D / 32];     // k[s]: dims 16 (2 s + H) .. of the key of MFMA row L
   u32x4 v[D / 32];     // v[db]: the slots of page H of dimension 32 db + L
 };
 
-template <bool ONCE>
-__device__ __forceinline__ u32x4 load16(const uint8_t* p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4*)p);
-  else return *(const u32x4*)p;
-}
-template <int D, bool ONCE>
+template <int D>
 __device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pages, int rel, int last_rel, int hk, int L, int H) {
-  const int pg0 = __builtin_amdgcn_readlane(pages, rel & 63), pg1 = __builtin_amdgcn_readlane(pages, min(rel + 1, last_rel) & 63);
+  const int pg0 = __builtin_amdgcn_readlane(pages, min(rel, last_rel) & 63), pg1 = __builtin_amdgcn_readlane(pages, min(rel + 1, last_rel) & 63);
   const int slot = (L & 3) + 4 * (L >> 3);
   const size_t base0 = ((size_t)pg0 * c.hkv + hk) * (D * PAGE), base1 = ((size_t)pg1 * c.hkv + hk) * (D * PAGE);
   const uint8_t* const kp = c.k_pool + ((L >> 2) & 1 ? base1 : base0) + H * 256 + slot * 16;
   const uint8_t* const vp = c.v_pool + (H ? base1 : base0) + L * 16;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.k[s] = load16<ONCE>(kp + s * 512);
+  for (int s = 0; s < D / 32; ++s) b.k[s] = __builtin_nontemporal_load((const u32x4*)(kp + s * 512));
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.v[s] = load16<ONCE>(vp + s * 512);
+  for (int s = 0; s < D / 32; ++s) b.v[s] = __builtin_nontemporal_load((const u32x4*)(vp + s * 512));
 }
 
 // A block some of whose tokens are hidden from some rows only (the new tokens of a node): a value that is no number may not reach the rows
@@ -127,31 +124,42 @@ __device__ __forceinline__ void hide_not_numbers(Block<D>& b, f32x16* O, int key
 // The exponent's reference m is raised only where a score is more than this above it (log2): the rescale of the sums stays rare.
 constexpr float Q8_TH = 3.f;
 
-// One block: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e), lv: log2 of
-// its value scale.  A lane's 16 scores are of one page, so their largest is found among the plain products, one multiply-add gives
-// the exponent with the value scale in it, and the sum of a lane loses that factor again once.
-// key0: first key of the block; keys from `lim` on are hidden from this lane's row; len: the smallest lim of the wave; slots from vlen on
-// hold no token.
-template <int D, typename QF>
-__device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, float& m, float& l, float ks, float lv, int key0, int len,
-                                              int lim, int vlen, int H) {
-  f32x16 S;
+// U blocks together: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
+// lv: log2 of its value scale.  A lane's 16 scores of a block are of one page, so their largest is found among the plain products, one
+// multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.
+// key0: first key of the first block; keys from `lim` on are hidden from this lane's row; len: the smallest lim of the wave; slots from vlen on
+// hold no token.  What bounds a wave by itself is the chain from the scores to the second product: two blocks share it.
+template <int D, int U, bool LIMITS, typename QF, typename VF>
+__device__ __forceinline__ void compute_blocks(Block<D> (&b)[U], QF&& q, VF&& values, f32x16* O, float& m, float& l, const float (&ks)[U],
+                                               const float (&lv)[U], int key0, int len, int lim, int vlen, int H) {
+  f32x16 S[U];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) S[r] = 0.f;
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[u][r] = 0.f;
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
-    S = mfma32(codes_to_bf16(b.k[s][0], b.k[s][1]), qop(2 * s), S);
-    S = mfma32(codes_to_bf16(b.k[s][2], b.k[s][3]), qop(2 * s + 1), S);
-  }
-  if (key0 + 32 > len) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) S[r] = key0 + 16 * H + r < lim ? S[r] : -INFINITY;
-  }
-  float bm = S[0];
+    for (int u = 0; u < U; ++u) S[u] = mfma32(codes_to_bf16(b[u].k[s][0], b[u].k[s][1]), q(2 * s), S[u]);
 #pragma unroll
-  for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
-  bm *= ks;
-  bm = fmaxf(bm, __shfl_xor(bm, 32));
+    for (int u = 0; u < U; ++u) S[u] = mfma32(codes_to_bf16(b[u].k[s][2], b[u].k[s][3]), q(2 * s + 1), S[u]);
+  }
+  values(b);
+  if (key0 + 32 * U > len) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[u][r] = key0 + 32 * u + 16 * H + r < lim ? S[u][r] : -INFINITY;
+  }
+  float bm = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float x = S[u][0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) x = fmaxf(x, S[u][r]);
+    bm = fmaxf(bm, x * ks[u]);
+  }
+  bm = fmaxf(bm, other_half(bm));
   if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) {
     const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
     l *= alpha;
@@ -161,42 +169,52 @@ __device__ __forceinline__ void compute_block(Block<D>& b, QF&& qop, f32x16* O, 
       for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
     m = m_new;
   }
-  f32x8 p0, p1;
-  float sum = 0.f;
-  const float ref = lv - m;
+  bf16x8 p[U][2];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    p0[r] = __builtin_amdgcn_exp2f(fmaf(S[r], ks, ref));
-    p1[r] = __builtin_amdgcn_exp2f(fmaf(S[8 + r], ks, ref));
-    sum += p0[r] + p1[r];
-  }
-  l = fmaf(sum, __builtin_amdgcn_exp2f(-lv), l);
-  // (rounded to bf16, as the probabilities over a bf16 cache are)
-  const bf16x8 pb0 = __builtin_convertvector(p0, bf16x8), pb1 = __builtin_convertvector(p1, bf16x8);
-  if (key0 + 32 > vlen) {  // slots without a token may hold codes that are no number
+  for (int u = 0; u < U; ++u) {
+    const float ref = lv[u] - m;
+    f32x8 x[2];
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int n = vlen - (key0 + 16 * H + 4 * w);  // slots of this word that hold one
-      const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) b.v[db][w] &= mask;
+    for (int r = 0; r < 16; ++r) {
+      x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[u][r], ks[u], ref));
+      sum[r >> 3] += x[r >> 3][r & 7];
     }
+    l = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-lv[u]), l);
+    // (rounded to bf16, as the probabilities over a bf16 cache are)
+    p[u][0] = __builtin_convertvector(x[0], bf16x8);
+    p[u][1] = __builtin_convertvector(x[1], bf16x8);
   }
-  if (key0 + 32 > len && len < vlen) hide_not_numbers<D>(b, O, key0, lim, H);
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) {
-    O[db] = mfma32(codes_to_bf16(b.v[db][0], b.v[db][1]), pb0, O[db]);
-    O[db] = mfma32(codes_to_bf16(b.v[db][2], b.v[db][3]), pb1, O[db]);
+  for (int u = 0; u < U; ++u) {
+    const int first = key0 + 32 * u;
+    if (first + 32 > vlen) {  // slots without a token may hold codes that are no number
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int n = vlen - (first + 16 * H + 4 * w);  // slots of this word that hold one
+        const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) b[u].v[db][w] &= mask;
+      }
+    }
+    if constexpr (LIMITS)
+      if (first + 32 > len && len < vlen) hide_not_numbers<D>(b[u], O, first, lim, H);
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(b[u].v[db][2 * i], b[u].v[db][2 * i + 1]), p[u][i], O[db]);
 }
 
 // Pages [p0, p1) of one list against the wave's 32 rows, two pages at a time, the next two on their way meanwhile (four of them are no
 // faster).  What bounds it is how the pages come from memory: pages that nobody else reads pass the caches by (ONCE; 16 groups of 8 over
 // 8192 | 1024 tokens 114 -> 101 us), and 1,300 to 1,800 waves ask for them, those of the KV heads of a page next to each other (-> 94 us =
 // 5.7 TB/s; 2,048 waves 99, 3,072 102 to 123; the loads alone of 2,048 waves take 98.6).
-template <int D, bool ONCE, typename QF>
+template <int D, bool LIMITS>
 __device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk,
-                                             float sc, int lane, QF&& qop, f32x16* O, float& m, float& l) {
+                                             float sc, int lane, const bf16x8 (&q)[D / 16], f32x16* O, float& m, float& l) {
   const int L = lane & 31, H = lane >> 5, np = p1 - p0;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -212,42 +230,43 @@ __device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pa
     lvv = __builtin_amdgcn_logf(c.v_scale[(size_t)pg * c.hkv + hk]);
   };
   auto of_page = [&](float x, int rel) __attribute__((always_inline)) {  // of page rel + H
-    const float a = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), rel & 63));
+    const float a = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), min(rel, np - 1) & 63));
     const float b = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), min(rel + 1, np - 1) & 63));
     return H ? b : a;
   };
   struct Ahead {
-    Block<D> b;
-    float ks, lv;
+    Block<D> b[1];
+    float ks[1], lv[1];
   };
   Ahead x0, x1;
   auto load = [&](Ahead& x, int rel) __attribute__((always_inline)) {
-    if (rel >= np) return;
-    if ((rel & 63) == 0) {
+    if ((rel & 63) == 0 && rel < np) {
       window(rel);
       asm volatile("" ::"v"(ksv), "v"(lvv));  // arrived: a wait for them later would also wait for the blocks in flight
     }
-    x.ks = of_page(ksv, rel);
-    x.lv = of_page(lvv, rel);
-    load_block<D, ONCE>(x.b, c, pg, rel, np - 1, hk, L, H);
+    x.ks[0] = of_page(ksv, rel);
+    x.lv[0] = of_page(lvv, rel);
+    load_block<D>(x.b[0], c, pg, rel, np - 1, hk, L, H);
+    __builtin_amdgcn_sched_barrier(0);
   };
   auto compute = [&](Ahead& x, int rel) __attribute__((always_inline)) {
-    compute_block<D>(x.b, qop, O, m, l, x.ks, x.lv, (p0 + rel) * PAGE, len, lim, vlen, H);
+    compute_blocks<D, 1, LIMITS>(x.b, [&](int s) { return q[s]; }, [](auto&) {}, O, m, l, x.ks, x.lv, (p0 + rel) * PAGE, len, lim, vlen, H);
+    __builtin_amdgcn_sched_barrier(0);
   };
+  // No load behind a condition: the wait for a block would then be one for the block behind it as well.  What is loaded behind the slice is
+  // its last page again, which nobody uses.
   load(x0, 0);
-  for (int rel = 0;;) {
+  for (int rel = 0; rel < np; rel += 4) {
     load(x1, rel + 2);
     compute(x0, rel);
-    if ((rel += 2) >= np) break;
-    load(x0, rel + 2);
-    compute(x1, rel);
-    if ((rel += 2) >= np) break;
+    load(x0, rel + 4);
+    if (rel + 2 < np) compute(x1, rel + 2);
   }
 }
 
-// Query operands of the wave's rows in LDS: step 2 s + u has dims 16 (2 s + H) + 8 u .. of row L, with the sign of the softmax scale.
+// Query operands of the lane's row: step 2 s + u has dims 16 (2 s + H) + 8 u .., with the sign of the softmax scale.
 template <int D>
-__device__ __forceinline__ void stage_q(bf16x8* qs, const uint16_t* row, float sc, int lane) {
+__device__ __forceinline__ void load_q(bf16x8 (&q)[D / 16], const uint16_t* row, float sc, int lane) {
   const uint16_t* const p = row + 16 * (lane >> 5);
   const uint32_t sign = sc < 0.f ? 0x80008000u : 0u;
 #pragma unroll
@@ -255,7 +274,7 @@ __device__ __forceinline__ void stage_q(bf16x8* qs, const uint16_t* row, float s
     u32x4 x = *(const u32x4*)(p + 32 * (s >> 1) + 8 * (s & 1));
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] ^= sign;
-    qs[s * 64 + lane] = __builtin_bit_cast(bf16x8, x);
+    q[s] = __builtin_bit_cast(bf16x8, x);
   }
 }
 
@@ -272,9 +291,8 @@ __device__ __forceinline__ void store_part(float* part_o, float* part_ml, size_t
 
 // A wave to a work item: a slice of a group's shared pages against 32 of its (branch, query head) rows of a KV head, or a slice of a
 // branch's own pages against its rows.
-template <int D, bool ONCE>
+template <int D>
 __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
-  __shared__ bf16x8 qs[(D / 16) * 64];
   const int lane = threadIdx.x, L = lane & 31, H = lane >> 5;
   const bool shared = (int)blockIdx.x < a.items_a;
   int x = shared ? blockIdx.x : blockIdx.x - a.items_a;
@@ -302,19 +320,18 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
     if (row_ok && H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
     return;
   }
-  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-  auto qop = [&](int s) { return qs[s * 64 + lane]; };
+  bf16x8 q[D / 16];
+  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
   f32x16 O[D / 32];
   float m, l;
-  stream_slice<D, ONCE>(a.kv, pages, p0, p1, len, len, len, hk, a.sc, lane, qop, O, m, l);
-  l += __shfl_xor(l, 32);
+  stream_slice<D, false>(a.kv, pages, p0, p1, len, len, len, hk, a.sc, lane, q, O, m, l);
+  l += other_half(l);
   if (row_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
 }
 
 // The same for the items that k_seg_plan listed.
-template <int D, bool ONCE>
+template <int D, bool LIMITS>
 __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
-  __shared__ bf16x8 qs[(D / 16) * 64];
   const SegArgs& a = args.s;
   const int lane = threadIdx.x, L = lane & 31, H = lane >> 5;
   const int hk = blockIdx.x % a.hkv, idx = blockIdx.x / a.hkv;
@@ -332,7 +349,7 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
   const bool store_ok = row_ok && there && place < a.splits * a.total_readers;  // (reader lists longer than announced: no partial)
   const size_t at = (size_t)place * a.hq + head;
   int lim = it.len, lim_min = it.len;
-  if (a.seg_reader_len) {
+  if constexpr (LIMITS) {
     lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
     int lim_max = lim;
     lim_min = lim;
@@ -348,13 +365,289 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
     }
   }
   const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
-  stage_q<D>(qs, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-  auto qop = [&](int s) { return qs[s * 64 + lane]; };
+  bf16x8 q[D / 16];
+  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
   f32x16 O[D / 32];
   float m, l;
-  stream_slice<D, ONCE>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, lane, qop, O, m, l);
-  l += __shfl_xor(l, 32);
+  stream_slice<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, lane, q, O, m, l);
+  l += other_half(l);
   if (store_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
+}
+
+// Lists with more than 32 rows of a KV head: a workgroup of eight waves takes up to eight blocks of 32 rows together, so that a page comes
+// from memory once for all of them.  Tiles of four pages go straight into a ring in LDS, codes as they are (a page is the operand image), and
+// every wave makes its own operands of them.  Up to four blocks: the waves w, w + blocks, .. share a block, its units of 32 keys in turn;
+// five to seven: waves 0 to 3 have one each and the others share what is left, so that the SIMDs have the same to do.  Waves of one block
+// put their sums together in LDS at the end.
+constexpr int WG_WAVES = 8, WG_TILE = 4, WG_RING = 6;
+static_assert(WG_ROWS == 32 * WG_WAVES && WG_MOST_PAGES >= 9 << 4, "");
+constexpr int K_PAD = 128;  // bytes behind a page's keys: the 16 slots of two pages that are read together lie on all banks
+template <int D>
+constexpr int wg_lds_bytes() {  // the ring, or the sums of the waves in its place
+  constexpr int tiles = WG_RING * WG_TILE * (2 * D * PAGE + K_PAD), sums = WG_WAVES * (D / 2 + 2) * 64 * 4;
+  return tiles > sums ? tiles : sums;
+}
+
+struct WgShare {  // of a wave: its block, which of the waves of the block it is, how many there are, what lies between them
+  int block, sub, parts, step, first;
+};
+__device__ __forceinline__ WgShare wg_share(int w, int blocks) {
+  if (blocks > 4) {
+    const int left = blocks - 4;
+    if (w < 4) return WgShare{w, 0, 1, 1, w};
+    const int b = (w - 4) % left;
+    return WgShare{4 + b, (w - 4) / left, (WG_WAVES - 4 - b + left - 1) / left, left, 4 + b};
+  }
+  const int b = w % blocks;
+  return WgShare{b, w / blocks, (WG_WAVES - b + blocks - 1) / blocks, blocks, b};
+}
+
+// 16 bytes each from N places of LDS, `step` bytes apart.  (Reads and their wait in one block: to the compiler a register that a read has
+// been told to fill holds its value already.)
+template <int STEP>
+__device__ __forceinline__ void lds_read(u32x4 (&x)[2], uint32_t at) {
+  asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]), "=&v"(x[1]) : "v"(at), "n"(STEP));
+}
+template <int STEP>
+__device__ __forceinline__ void lds_read(u32x4 (&x)[4], uint32_t at) {
+  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:%5\n\tds_read_b128 %2, %4 offset:%6\n\tds_read_b128 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+               : "v"(at), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP));
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
+
+template <int D, bool LIMITS>
+__device__ __forceinline__ void wg_stream(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk, float sc,
+                                          unsigned char* smem, int w, int lane, int sub, int parts, const bf16x8 (&q)[D / 16], f32x16* O, float& m,
+                                          float& l) {
+  constexpr int PB = D * PAGE, KB = PB + K_PAD, PLACE = WG_TILE * (KB + PB);
+  const int L = lane & 31, H = lane >> 5, np = p1 - p0, nt = (np + WG_TILE - 1) / WG_TILE, nu = (np + 1) / 2;
+  static_assert(WG_MOST_PAGES <= 192, "");
+  auto page_of = [&](int i) { return min(max(pages[p0 + min(i + lane, np - 1)], 0), c.n_pages - 1); };
+  const int pg0 = page_of(0), pg1 = page_of(64), pg2 = page_of(128);
+  auto ks_of = [&](int pg) { return c.k_scale[(size_t)pg * c.hkv + hk] * fabsf(sc); };
+  auto lv_of = [&](int pg) { return __builtin_amdgcn_logf(c.v_scale[(size_t)pg * c.hkv + hk]); };
+  const float ks0 = ks_of(pg0), ks1 = ks_of(pg1), ks2 = ks_of(pg2), lv0 = lv_of(pg0), lv1 = lv_of(pg1), lv2 = lv_of(pg2);
+  asm volatile("" ::"v"(ks0), "v"(ks1), "v"(ks2), "v"(lv0), "v"(lv1), "v"(lv2));  // (arrived: from here on only tiles are under way)
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) asm volatile("" ::"v"(q[s]));
+  auto pick = [&](auto x, auto y, auto z, int i) __attribute__((always_inline)) {
+    const auto v = i < 64 ? x : i < 128 ? y : z;
+    return __builtin_bit_cast(decltype(x), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i & 63));
+  };
+  auto of_pages = [&](float x, float y, float z, int rel) __attribute__((always_inline)) {  // of page rel + H
+    const float a = pick(x, y, z, rel), b = pick(x, y, z, min(rel + 1, np - 1));
+    return H ? b : a;
+  };
+  // A wave brings 1 KiB of the keys and of the values of a page of the tile, at dimension 64 of either.
+  constexpr int LOADS = D / 64;
+  const int mine = D == 128 ? w >> 1 : w & 3, at = D == 128 ? (w & 1) * 1024 : 0;
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    if (t >= nt) return;
+    const size_t src = ((size_t)pick(pg0, pg1, pg2, min(WG_TILE * t + mine, np - 1)) * c.hkv + hk) * PB + at + lane * 16;
+    unsigned char* const place = smem + t % WG_RING * PLACE;
+    typedef __attribute__((address_space(1))) const void* from_t;
+    typedef __attribute__((address_space(3))) void* to_t;
+    if (D == 128 || w < 4) __builtin_amdgcn_global_load_lds((from_t)(c.k_pool + src), (to_t)(place + mine * KB + at), 16, 0, 0);
+    if (D == 128 || w >= 4) __builtin_amdgcn_global_load_lds((from_t)(c.v_pool + src), (to_t)(place + WG_TILE * KB + mine * PB + at), 16, 0, 0);
+  };
+  // Tile t is there for everybody, and everybody has left tile t - 1.
+  auto arrive = [&](int t) __attribute__((always_inline)) {
+    static_assert(WG_RING == 6, "");
+    const int behind = nt - 1 - t;  // tiles under way behind it, four at most
+    if (behind >= 4) wait_vmcnt<4 * LOADS>();
+    else if (behind == 3) wait_vmcnt<3 * LOADS>();
+    else if (behind == 2) wait_vmcnt<2 * LOADS>();
+    else if (behind == 1) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  for (int t = 0; t < WG_RING - 1; ++t) issue(t);
+  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)smem;
+  const uint32_t koff = ring + ((L >> 2) & 1) * KB + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = ring + WG_TILE * KB + H * PB + L * 16;
+  // Units behind the slice are its last page again, hidden like what lies behind the list.
+  len = min(len, p1 * PAGE);
+  lim = min(lim, p1 * PAGE);
+  auto units = [&](auto u_c, int t, int h) __attribute__((always_inline)) {  // from half h of tile t on
+    constexpr int U = decltype(u_c)::value;
+    const uint32_t place = t % WG_RING * PLACE;
+    Block<D> b[U];
+    float ks[U], lv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      lds_read<512>(b[u].k, koff + place + 2 * (h + u) * KB);
+      const int rel = min(2 * (2 * t + h + u), np - 1);
+      ks[u] = of_pages(ks0, ks1, ks2, rel);
+      lv[u] = of_pages(lv0, lv1, lv2, rel);
+    }
+    auto values = [&](auto& x) __attribute__((always_inline)) {  // (read behind the scores, where the keys' registers are free)
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) lds_read<512>(x[u].v, voff + place + 2 * (h + u) * PB);
+    };
+    compute_blocks<D, U, LIMITS>(b, [&](int s) { return q[s]; }, values, O, m, l, ks, lv, (p0 + 2 * (2 * t + h)) * PAGE, len, lim, vlen, H);
+  };
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+  m = -1e30f;
+  l = 0.f;
+  if (parts == 1) {
+#pragma unroll 1
+    for (int t = 0; t < nt; ++t) {
+      arrive(t);
+      issue(t + WG_RING - 1);
+      units(std::integral_constant<int, 2>{}, t, 0);
+    }
+  } else {
+    int next = sub;  // unit
+#pragma unroll 1
+    for (int t = 0; t < nt; ++t) {
+      arrive(t);
+      issue(t + WG_RING - 1);
+#pragma unroll 1
+      for (; next < min(2 * t + 2, nu); next += parts) units(std::integral_constant<int, 1>{}, t, next - 2 * t);  // (one or two)
+    }
+  }
+  __syncthreads();
+}
+
+// The rest of an item: sums of the waves of a block put together, a range of dimensions each, and stored.  (The tiles' places are free.)
+template <int D>
+__device__ __forceinline__ void wg_store(float* smem, const WgShare& s, int w, int lane, f32x16* O, float m, float l, bool row_ok, float* part_o,
+                                         float* part_ml, size_t at) {
+  constexpr int DB = D / 32, EACH = (16 * DB + 2) * 64;
+  const int H = lane >> 5;
+  l += other_half(l);
+  if (s.parts > 1) {
+    float* const mine = smem + w * EACH + lane;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mine[(16 * db + r) * 64] = O[db][r];
+    mine[16 * DB * 64] = m;
+    mine[(16 * DB + 1) * 64] = l;
+  }
+  __syncthreads();
+  if (s.parts > 1) {
+    float top = -1e30f;
+    for (int p = 0; p < s.parts; ++p) top = fmaxf(top, smem[(s.first + p * s.step) * EACH + 16 * DB * 64 + lane]);
+    float total = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      if (db % s.parts == s.sub)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+    for (int p = 0; p < s.parts; ++p) {
+      const float* const theirs = smem + (s.first + p * s.step) * EACH + lane;
+      const float wgt = __builtin_amdgcn_exp2f(theirs[16 * DB * 64] - top);
+      total = fmaf(theirs[(16 * DB + 1) * 64], wgt, total);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        if (db % s.parts == s.sub)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[db][r] = fmaf(theirs[(16 * db + r) * 64], wgt, O[db][r]);
+    }
+    m = top;
+    l = total;
+  }
+  if (!row_ok) return;
+  float* const po = part_o + at * D;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    if (db % s.parts == s.sub)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *(f32x4*)(po + 32 * db + 8 * r4 + 4 * H) = f32x4{O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
+  if (H == 0 && s.sub == 0) *(float2*)(part_ml + at * 2) = make_float2(m, l);
+}
+
+// Workgroups with shared items, then with own ones, a wave each.
+template <int D>
+__global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_wg(Q8DecodeArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 31;
+  f32x16 O[D / 32];
+  float m, l;
+  if ((int)blockIdx.x < a.items_a) {
+    int x = blockIdx.x;
+    const int hk = x % a.hkv;
+    x /= a.hkv;
+    const int split = x % a.splits_a;
+    x /= a.splits_a;
+    const int row0 = x % a.rb_max * WG_ROWS, g = x / a.rb_max;
+    const int branch0 = a.group_branch_off[g], nrows = (a.group_branch_off[g + 1] - branch0) * a.G, len = a.shared_len[g];
+    if (row0 >= nrows) return;
+    const int p0 = split * a.chunk_a, p1 = min(p0 + a.chunk_a, (len + PAGE - 1) / PAGE);
+    const WgShare s = wg_share(w, min((nrows - row0 + 31) / 32, WG_WAVES));
+    const int row = row0 + 32 * s.block + L;
+    const bool row_ok = row < nrows;
+    const int rr = row_ok ? row : row0, branch = min(max(branch0 + rr / a.G, 0), a.n_live - 1), head = hk * a.G + rr % a.G;
+    const size_t at = (size_t)(branch * a.splits_a + split) * a.hq + head;
+    if (p0 >= p1) {
+      if (row_ok && s.sub == 0 && lane < 32) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
+      return;
+    }
+    bf16x8 q[D / 16];
+    load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
+    wg_stream<D, false>(a.kv, a.shared_pages + a.shared_page_off[g], p0, p1, len, len, len, hk, a.sc, smem, w, lane, s.sub, s.parts, q, O, m, l);
+    wg_store<D>((float*)smem, s, w, lane, O, m, l, row_ok, a.part_o, a.part_ml, at);
+    return;
+  }
+  int x = (blockIdx.x - a.items_a) * WG_WAVES + w;
+  const int hk = x % a.hkv;
+  x /= a.hkv;
+  const int split = x % a.splits_b, branch = x / a.splits_b;
+  if (branch >= a.n_live) return;
+  const int len = a.branch_len[branch], p0 = split * a.chunk_b, p1 = min(p0 + a.chunk_b, (len + PAGE - 1) / PAGE);
+  const size_t at = (size_t)(a.first_own + branch * a.splits_b + split) * a.hq + hk * a.G + min(L, a.G - 1);
+  if (p0 >= p1) {
+    if (lane < a.G) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
+    return;
+  }
+  bf16x8 q[D / 16];
+  load_q<D>(q, a.q + ((size_t)branch * a.hq + hk * a.G + min(L, a.G - 1)) * D, a.sc, lane);
+  stream_slice<D, false>(a.kv, a.branch_pages + a.branch_page_off[branch], p0, p1, len, len, len, hk, a.sc, lane, q, O, m, l);
+  l += other_half(l);
+  if (L < a.G) store_part<D>(a.part_o, a.part_ml, at, O, m, l, lane >> 5);
+}
+
+template <int D, bool LIMITS>
+__global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_seg_wg(Q8SegArgs args) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const SegArgs& a = args.s;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 31;
+  const int hk = blockIdx.x % a.hkv, idx = blockIdx.x / a.hkv;
+  if (idx >= a.totals[0]) return;
+  const SegItem it = a.items[idx];
+  const int slice = (it.nsplit >> 23) & 0x1fe, nsplit = it.nsplit & 0xffffff;
+  const int npages = min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits), p1 = min(it.p0 + slice, npages);  // (a slice has 9 << 4 pages at most)
+  if (it.row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
+  const WgShare s = wg_share(w, min((it.nrows - it.row0 + 31) / 32, WG_WAVES));
+  const int row = it.row0 + 32 * s.block + L;
+  const bool row_ok = row < it.nrows;
+  const int rr = row_ok ? row : it.row0;
+  const int entry = it.e0 + rr / a.G, head = hk * a.G + rr % a.G, place = it.place + rr / a.G * nsplit;
+  const bool there = entry >= 0 && entry < a.total_readers;
+  const bool store_ok = row_ok && there && place < a.splits * a.total_readers;
+  const size_t at = (size_t)place * a.hq + head;
+  int lim = it.len, lim_min = it.len;
+  if constexpr (LIMITS) {
+    lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
+    lim_min = lim;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) lim_min = min(lim_min, __shfl_xor(lim_min, o));
+  }
+  const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
+  bf16x8 q[D / 16];
+  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
+  f32x16 O[D / 32];
+  float m, l;
+  wg_stream<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, smem, w, lane, s.sub, s.parts, q, O, m, l);
+  wg_store<D>((float*)smem, s, w, lane, O, m, l, store_ok, a.part_o, a.part_ml, at);
 }
 
 // A wave to a (branch, query head): its partials are put together by their references, 64 at a time a lane each has reference and
@@ -496,9 +789,14 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   a.sc = softmax_scale * 1.4426950408889634f;
   hipStream_t stream = (hipStream_t)stream_;
   if (p.items_a + p.items_b > 0) {
-    auto* const kernel = p.rb_max <= 1 ? (D == 128 ? k_q8_decode<128, true> : k_q8_decode<64, true>)
-                                       : (D == 128 ? k_q8_decode<128, false> : k_q8_decode<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
+    if (p.wg) {
+      auto* const kernel = D == 128 ? k_q8_decode_wg<128> : k_q8_decode_wg<64>;
+      const int lds = D == 128 ? wg_lds_bytes<128>() : wg_lds_bytes<64>();
+      DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items_a + dag_ceil_div(p.items_b, WG_WAVES))), dim3(64 * WG_WAVES), lds, stream, a);
+    } else {
+      hipLaunchKernelGGL((D == 128 ? k_q8_decode<128> : k_q8_decode<64>), dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
+    }
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge<128> : k_q8_merge<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, a);
@@ -508,7 +806,8 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
 
 extern "C" size_t dag_decode_segments_q8_workspace_bytes(const dag_decode_seg_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim) {
   SegPlan p;
-  return make_seg_plan(desc, hq, hkv, head_dim, DecodeKnobs{0, 0, 0}, &p) == DAG_OK ? p.bytes : 0;
+  bool wg;
+  return make_q8_seg_plan(desc, hq, hkv, head_dim, &p, &wg) == DAG_OK ? p.bytes : 0;
 }
 
 extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
@@ -518,7 +817,8 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   if (rc != DAG_OK) return rc;
   SegPlan p;
   const int D = kv->head_dim, hkv = kv->hkv;
-  rc = make_seg_plan(d, hq, hkv, D, DecodeKnobs{0, 0, 0}, &p);
+  bool wg;
+  rc = make_q8_seg_plan(d, hq, hkv, D, &p, &wg);
   if (rc != DAG_OK) return rc;
   if (d->n_live == 0) return DAG_OK;
   if (!q || !out || !d->branch_entry_off || !d->branch_entries) return DAG_ERR_NULL;
@@ -555,6 +855,7 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   a.hkv = hkv;
   a.G = hq / hkv;
   a.rb_max = p.rb_max;
+  a.row_shift = wg ? 8 : 5;
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.total_readers = d->total_readers;
@@ -568,9 +869,17 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
     const int64_t waves = dag_ceil_div(d->n_segments, 64);
     hipLaunchKernelGGL(k_seg_plan, dim3(1), dim3((unsigned)(waves * 64 < PLAN_THREADS ? waves * 64 : PLAN_THREADS)), 0, stream, a);
     DAG_LAUNCH_CHECK();
-    auto* const kernel = p.rb_max <= 1 ? (D == 128 ? k_q8_decode_seg<128, true> : k_q8_decode_seg<64, true>)
-                                       : (D == 128 ? k_q8_decode_seg<128, false> : k_q8_decode_seg<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
+    if (wg) {
+      auto* const kernel = a.seg_reader_len ? (D == 128 ? k_q8_decode_seg_wg<128, true> : k_q8_decode_seg_wg<64, true>)
+                                            : (D == 128 ? k_q8_decode_seg_wg<128, false> : k_q8_decode_seg_wg<64, false>);
+      const int lds = D == 128 ? wg_lds_bytes<128>() : wg_lds_bytes<64>();
+      DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64 * WG_WAVES), lds, stream, args);
+    } else {
+      auto* const kernel = a.seg_reader_len ? (D == 128 ? k_q8_decode_seg<128, true> : k_q8_decode_seg<64, true>)
+                                            : (D == 128 ? k_q8_decode_seg<128, false> : k_q8_decode_seg<64, false>);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
+    }
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge_seg<128> : k_q8_merge_seg<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, args);
