@@ -258,7 +258,7 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
 // stands at stream_slice), no shorter than Q8_LEAST_PAGES.
 constexpr int Q8_WAVES = 1536, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
 // More than 32 rows of a KV head in some group: workgroups for up to WG_ROWS of them, whose page ids sit in three registers.
-constexpr int WG_ROWS = 256, WG_MOST_PAGES = 144, WG_LEAST_PAGES = 16, WG_GROUPS = 384;
+constexpr int WG_ROWS = 256, WG_MOST_PAGES = 144, WG_LEAST_PAGES = 16, WG_GROUPS = 256;
 struct Q8Plan {
   bool wg;
   int rb_max, chunk_a, splits_a, chunk_b, splits_b, items_a, items_b;

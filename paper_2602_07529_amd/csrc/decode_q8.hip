@@ -124,6 +124,30 @@ __device__ __forceinline__ void hide_not_numbers(Block<D>& b, f32x16* O, int key
 // The exponent's reference m is raised only where a score is more than this above it (log2): the rescale of the sums stays rare.
 constexpr float Q8_TH = 3.f;
 
+// The reference to at least bm, the sums with it.
+template <int D>
+__device__ __forceinline__ void raise(f32x16* O, float& m, float& l, float bm) {
+  const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
+  l *= alpha;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
+  m = m_new;
+}
+
+// Slots from vlen on hold no token: their codes may be no numbers, which a probability of zero does not keep from the sums.
+template <int D>
+__device__ __forceinline__ void clear_behind(Block<D>& b, int key0, int vlen, int H) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int n = vlen - (key0 + 16 * H + 4 * w);  // slots of this word that hold one
+    const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) b.v[db][w] &= mask;
+  }
+}
+
 // U blocks together: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
 // lv: log2 of its value scale.  A lane's 16 scores of a block are of one page, so their largest is found among the plain products, one
 // multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.
@@ -146,6 +170,7 @@ __device__ __forceinline__ void compute_blocks(Block<D> (&b)[U], QF&& q, VF&& va
   }
   values(b);
   if (key0 + 32 * U > len) {
+    asm volatile("");  // (a branch: the compiler would compare and select in every block)
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -160,15 +185,7 @@ __device__ __forceinline__ void compute_blocks(Block<D> (&b)[U], QF&& q, VF&& va
     bm = fmaxf(bm, x * ks[u]);
   }
   bm = fmaxf(bm, other_half(bm));
-  if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) {
-    const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
-    l *= alpha;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
-    m = m_new;
-  }
+  if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) raise<D>(O, m, l, bm);
   bf16x8 p[U][2];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -188,15 +205,7 @@ __device__ __forceinline__ void compute_blocks(Block<D> (&b)[U], QF&& q, VF&& va
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int first = key0 + 32 * u;
-    if (first + 32 > vlen) {  // slots without a token may hold codes that are no number
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int n = vlen - (first + 16 * H + 4 * w);  // slots of this word that hold one
-        const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) b[u].v[db][w] &= mask;
-      }
-    }
+    if (first + 32 > vlen) clear_behind<D>(b[u], first, vlen, H);
     if constexpr (LIMITS)
       if (first + 32 > len && len < vlen) hide_not_numbers<D>(b[u], O, first, lim, H);
   }
@@ -375,74 +384,79 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
 }
 
 // Lists with more than 32 rows of a KV head: a workgroup of eight waves takes up to eight blocks of 32 rows together, so that a page comes
-// from memory once for all of them.  Tiles of four pages go straight into a ring in LDS, codes as they are (a page is the operand image), and
-// every wave makes its own operands of them.  Up to four blocks: the waves w, w + blocks, .. share a block, its units of 32 keys in turn;
-// five to seven: waves 0 to 3 have one each and the others share what is left, so that the SIMDs have the same to do.  Waves of one block
-// put their sums together in LDS at the end.
-constexpr int WG_WAVES = 8, WG_TILE = 4, WG_RING = 6;
+// from memory once for all of them.  Tiles of four pages (two units of 32 keys) go straight into a ring in LDS, codes as they are (a page is
+// the operand image), and every wave makes its own operands of them.  Up to four blocks: the waves w, w + blocks, .. share a block, its
+// units in turn; five to seven: waves 0 to 3 have one each and the others share what is left, so that the SIMDs have the same
+// to do.  Waves of one block put their sums together in LDS at the end.
+// A wave is a pipeline: in one run of instructions the scores of its next unit and the exponentials of this one, in the next run
+// this one's product with the values and the next one's maximum.  One after the other, the matrix and the vector pipe take turns in both waves of a
+// SIMD, which the tiles keep in step: 1,700 cycles a unit, of which they need 520 and 960 (two groups of 32 over 32768 | 640,
+// 5 heads on one: 93 us, so FIGURE).
+constexpr int WG_WAVES = 8, WG_TILE = 4, WG_RING = 8;
 static_assert(WG_ROWS == 32 * WG_WAVES && WG_MOST_PAGES >= 9 << 4, "");
+constexpr int WG_SCALES = 192;  // pages of a slice: three windows of 64
 constexpr int K_PAD = 128;  // bytes behind a page's keys: the 16 slots of two pages that are read together lie on all banks
 template <int D>
 constexpr int wg_lds_bytes() {  // the ring, or the sums of the waves in its place
-  constexpr int tiles = WG_RING * WG_TILE * (2 * D * PAGE + K_PAD), sums = WG_WAVES * (D / 2 + 2) * 64 * 4;
+  constexpr int tiles = WG_RING * WG_TILE * (2 * D * PAGE + K_PAD) + WG_SCALES * 8, sums = WG_WAVES * (D / 2 + 2) * 64 * 4;
   return tiles > sums ? tiles : sums;
 }
 
-struct WgShare {  // of a wave: its block, which of the waves of the block it is, how many there are, what lies between them
-  int block, sub, parts, step, first;
+struct WgShare {  // of a wave: its block, which of the waves of the block it is, how many there are, the first one, what lies between them
+  int block, sub, parts, first, step;
+  int most;  // largest number of waves of a block
 };
 __device__ __forceinline__ WgShare wg_share(int w, int blocks) {
   if (blocks > 4) {
-    const int left = blocks - 4;
-    if (w < 4) return WgShare{w, 0, 1, 1, w};
-    const int b = (w - 4) % left;
-    return WgShare{4 + b, (w - 4) / left, (WG_WAVES - 4 - b + left - 1) / left, left, 4 + b};
+    const int left = blocks - 4, b = (w - 4) % left;
+    const int most = (WG_WAVES - 4 + left - 1) / left;
+    return w < 4 ? WgShare{w, 0, 1, w, 1, most} : WgShare{4 + b, (w - 4) / left, (WG_WAVES - 4 - b + left - 1) / left, 4 + b, left, most};
   }
-  const int b = w % blocks;
-  return WgShare{b, w / blocks, (WG_WAVES - b + blocks - 1) / blocks, blocks, b};
+  return WgShare{w % blocks, w / blocks, (WG_WAVES - w % blocks + blocks - 1) / blocks, w % blocks, blocks, (WG_WAVES + blocks - 1) / blocks};
 }
 
-// 16 bytes each from N places of LDS, `step` bytes apart.  (Reads and their wait in one block: to the compiler a register that a read has
-// been told to fill holds its value already.)
-template <int STEP>
-__device__ __forceinline__ void lds_read(u32x4 (&x)[2], uint32_t at) {
-  asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]), "=&v"(x[1]) : "v"(at), "n"(STEP));
+// What a unit needs of LDS in one round trip: the next unit's scales and keys, this one's values.  (Reads and their wait in one block: to the
+// compiler a register that a read has been told to fill holds its value already.)
+__device__ __forceinline__ void lds_unit(u32x2& scales, u32x4 (&k)[4], u32x4 (&v)[4], uint32_t s_at, uint32_t k_at, uint32_t v_at) {
+  asm volatile(
+      "ds_read_b64 %0, %9\n\t"
+      "ds_read_b128 %1, %10\n\tds_read_b128 %2, %10 offset:512\n\tds_read_b128 %3, %10 offset:1024\n\tds_read_b128 %4, %10 offset:1536\n\t"
+      "ds_read_b128 %5, %11\n\tds_read_b128 %6, %11 offset:512\n\tds_read_b128 %7, %11 offset:1024\n\tds_read_b128 %8, %11 offset:1536\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(scales), "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+      : "v"(s_at), "v"(k_at), "v"(v_at));
 }
-template <int STEP>
-__device__ __forceinline__ void lds_read(u32x4 (&x)[4], uint32_t at) {
-  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:%5\n\tds_read_b128 %2, %4 offset:%6\n\tds_read_b128 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
-               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-               : "v"(at), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP));
+__device__ __forceinline__ void lds_unit(u32x2& scales, u32x4 (&k)[2], u32x4 (&v)[2], uint32_t s_at, uint32_t k_at, uint32_t v_at) {
+  asm volatile(
+      "ds_read_b64 %0, %5\n\tds_read_b128 %1, %6\n\tds_read_b128 %2, %6 offset:512\n\t"
+      "ds_read_b128 %3, %7\n\tds_read_b128 %4, %7 offset:512\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(scales), "=&v"(k[0]), "=&v"(k[1]), "=&v"(v[0]), "=&v"(v[1])
+      : "v"(s_at), "v"(k_at), "v"(v_at));
 }
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
 
 template <int D, bool LIMITS>
 __device__ __forceinline__ void wg_stream(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk, float sc,
-                                          unsigned char* smem, int w, int lane, int sub, int parts, const bf16x8 (&q)[D / 16], f32x16* O, float& m,
+                                          unsigned char* smem, int w, int lane, int sub, int parts, int most_parts, const bf16x8 (&q)[D / 16], f32x16* O, float& m,
                                           float& l) {
   constexpr int PB = D * PAGE, KB = PB + K_PAD, PLACE = WG_TILE * (KB + PB);
   const int L = lane & 31, H = lane >> 5, np = p1 - p0, nt = (np + WG_TILE - 1) / WG_TILE, nu = (np + 1) / 2;
-  static_assert(WG_MOST_PAGES <= 192, "");
+  static_assert(WG_MOST_PAGES <= WG_SCALES, "");
   auto page_of = [&](int i) { return min(max(pages[p0 + min(i + lane, np - 1)], 0), c.n_pages - 1); };
   const int pg0 = page_of(0), pg1 = page_of(64), pg2 = page_of(128);
-  auto ks_of = [&](int pg) { return c.k_scale[(size_t)pg * c.hkv + hk] * fabsf(sc); };
-  auto lv_of = [&](int pg) { return __builtin_amdgcn_logf(c.v_scale[(size_t)pg * c.hkv + hk]); };
-  const float ks0 = ks_of(pg0), ks1 = ks_of(pg1), ks2 = ks_of(pg2), lv0 = lv_of(pg0), lv1 = lv_of(pg1), lv2 = lv_of(pg2);
-  asm volatile("" ::"v"(ks0), "v"(ks1), "v"(ks2), "v"(lv0), "v"(lv1), "v"(lv2));  // (arrived: from here on only tiles are under way)
+  // Scales of the slice's pages to LDS, behind the ring: the waves take turns with the windows of 64.
+  float2* const scales = (float2*)(smem + WG_RING * PLACE);
+  const int mine64 = w < 3 ? w : 0, pgs = mine64 == 0 ? pg0 : mine64 == 1 ? pg1 : pg2;
+  const float ks_here = c.k_scale[(size_t)pgs * c.hkv + hk] * fabsf(sc), vs_here = c.v_scale[(size_t)pgs * c.hkv + hk];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) asm volatile("" ::"v"(q[s]));
-  auto pick = [&](auto x, auto y, auto z, int i) __attribute__((always_inline)) {
-    const auto v = i < 64 ? x : i < 128 ? y : z;
-    return __builtin_bit_cast(decltype(x), __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i & 63));
-  };
-  auto of_pages = [&](float x, float y, float z, int rel) __attribute__((always_inline)) {  // of page rel + H
-    const float a = pick(x, y, z, rel), b = pick(x, y, z, min(rel + 1, np - 1));
-    return H ? b : a;
-  };
   // A wave brings 1 KiB of the keys and of the values of a page of the tile, at dimension 64 of either.
   constexpr int LOADS = D / 64;
   const int mine = D == 128 ? w >> 1 : w & 3, at = D == 128 ? (w & 1) * 1024 : 0;
+  auto pick = [](int x, int y, int z, int i) __attribute__((always_inline)) {  // (by value: a choice between captured ones is one of addresses)
+    return __builtin_amdgcn_readlane(i < 64 ? x : i < 128 ? y : z, i & 63);
+  };
   auto issue = [&](int t) __attribute__((always_inline)) {
     if (t >= nt) return;
     const size_t src = ((size_t)pick(pg0, pg1, pg2, min(WG_TILE * t + mine, np - 1)) * c.hkv + hk) * PB + at + lane * 16;
@@ -452,70 +466,115 @@ __device__ __forceinline__ void wg_stream(const Q8Cache& c, const int32_t* pages
     if (D == 128 || w < 4) __builtin_amdgcn_global_load_lds((from_t)(c.k_pool + src), (to_t)(place + mine * KB + at), 16, 0, 0);
     if (D == 128 || w >= 4) __builtin_amdgcn_global_load_lds((from_t)(c.v_pool + src), (to_t)(place + WG_TILE * KB + mine * PB + at), 16, 0, 0);
   };
-  // Tile t is there for everybody, and everybody has left tile t - 1.
+  // Tile t is there for everybody.  A wave still has to read the values of its last unit, `parts` units in front of its next one: in a tile
+  // up to (parts + 1) / 2 in front of t, which no tile may replace that is asked for up to here.
+  const int ahead = WG_RING - 1 - (most_parts + 1) / 2;
   auto arrive = [&](int t) __attribute__((always_inline)) {
-    static_assert(WG_RING == 6, "");
-    const int behind = nt - 1 - t;  // tiles under way behind it, four at most
-    if (behind >= 4) wait_vmcnt<4 * LOADS>();
-    else if (behind == 3) wait_vmcnt<3 * LOADS>();
-    else if (behind == 2) wait_vmcnt<2 * LOADS>();
-    else if (behind == 1) wait_vmcnt<LOADS>();
-    else wait_vmcnt<0>();
+    static_assert(WG_RING == 8, "");
+    switch (min(nt - 1 - t, ahead - 1)) {  // tiles under way behind it
+      case 0: wait_vmcnt<0>(); break;
+      case 1: wait_vmcnt<LOADS>(); break;
+      case 2: wait_vmcnt<2 * LOADS>(); break;
+      case 3: wait_vmcnt<3 * LOADS>(); break;
+      case 4: wait_vmcnt<4 * LOADS>(); break;
+      default: wait_vmcnt<5 * LOADS>();
+    }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    issue(t + ahead);
   };
-  for (int t = 0; t < WG_RING - 1; ++t) issue(t);
+  for (int t = 0; t < ahead; ++t) issue(t);
+  if (w < 3) scales[64 * w + lane] = make_float2(ks_here, __builtin_amdgcn_logf(vs_here));
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)smem;
   const uint32_t koff = ring + ((L >> 2) & 1) * KB + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = ring + WG_TILE * KB + H * PB + L * 16;
-  // Units behind the slice are its last page again, hidden like what lies behind the list.
+  const uint32_t soff = ring + WG_RING * PLACE + H * 8;
+  // What lies behind the slice in its last unit is its last page again, hidden like what lies behind the list.
   len = min(len, p1 * PAGE);
   lim = min(lim, p1 * PAGE);
-  auto units = [&](auto u_c, int t, int h) __attribute__((always_inline)) {  // from half h of tile t on
-    constexpr int U = decltype(u_c)::value;
-    const uint32_t place = t % WG_RING * PLACE;
-    Block<D> b[U];
-    float ks[U], lv[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      lds_read<512>(b[u].k, koff + place + 2 * (h + u) * KB);
-      const int rel = min(2 * (2 * t + h + u), np - 1);
-      ks[u] = of_pages(ks0, ks1, ks2, rel);
-      lv[u] = of_pages(lv0, lv1, lv2, rel);
-    }
-    auto values = [&](auto& x) __attribute__((always_inline)) {  // (read behind the scores, where the keys' registers are free)
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = 0; u < U; ++u) lds_read<512>(x[u].v, voff + place + 2 * (h + u) * PB);
-    };
-    compute_blocks<D, U, LIMITS>(b, [&](int s) { return q[s]; }, values, O, m, l, ks, lv, (p0 + 2 * (2 * t + h)) * PAGE, len, lim, vlen, H);
-  };
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
   m = -1e30f;
   l = 0.f;
-  if (parts == 1) {
-#pragma unroll 1
-    for (int t = 0; t < nt; ++t) {
-      arrive(t);
-      issue(t + WG_RING - 1);
-      units(std::integral_constant<int, 2>{}, t, 0);
+  f32x16 S;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) S[r] = -INFINITY;
+  float ks = 1.f, lv = 0.f;
+  // This wave's unit u, whose scores are in S, and the scores of unit n behind it.  (The first call has no unit u yet: hidden scores, and the
+  // values of unit n.)
+  auto unit = [&](int u, int n) __attribute__((always_inline)) {
+    Block<D> b[1];
+    u32x2 next;
+    const int tu = u >> 1, tn = n >> 1;
+    lds_unit(next, b[0].k, b[0].v, soff + 16 * n, koff + tn % WG_RING * PLACE + (n & 1) * 2 * KB, voff + tu % WG_RING * PLACE + (u & 1) * 2 * PB);
+    const float ref = lv - m;
+    f32x16 T;
+    f32x8 x[2];
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) T[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      T = mfma32(codes_to_bf16(b[0].k[s >> 1][2 * (s & 1)], b[0].k[s >> 1][2 * (s & 1) + 1]), q[s], T);
+#pragma unroll
+      for (int r = s * 256 / D; r < (s + 1) * 256 / D; ++r) {
+        x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], ks, ref));
+        sum[r >> 3] += x[r >> 3][r & 7];
+      }
     }
-  } else {
-    int next = sub;  // unit
-#pragma unroll 1
-    for (int t = 0; t < nt; ++t) {
-      arrive(t);
-      issue(t + WG_RING - 1);
-#pragma unroll 1
-      for (; next < min(2 * t + 2, nu); next += parts) units(std::integral_constant<int, 1>{}, t, next - 2 * t);  // (one or two)
+    l = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-lv), l);
+    bf16x8 p[2] = {__builtin_convertvector(x[0], bf16x8), __builtin_convertvector(x[1], bf16x8)};
+    // (done here, beside the scores: the compiler would move it behind the branches below, to where it is used)
+    asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(l));
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {  // vector instructions (0x2), one MFMA (0x8), in turn
+      __builtin_amdgcn_sched_group_barrier(0x002, 4 + 64 / (D / 16), 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     }
+    ks = __uint_as_float(next[0]);
+    lv = __uint_as_float(next[1]);
+    const int key_n = (p0 + 2 * n) * PAGE, key_u = (p0 + 2 * u) * PAGE;
+    if (key_n + 32 > len) {
+      asm volatile("");
+#pragma unroll
+      for (int r = 0; r < 16; ++r) T[r] = key_n + 16 * H + r < lim ? T[r] : -INFINITY;
+    }
+    if (key_u + 32 > vlen) {
+      asm volatile("");
+      clear_behind<D>(b[0], key_u, vlen, H);
+    }
+    if constexpr (LIMITS)
+      if (key_u + 32 > len && len < vlen) hide_not_numbers<D>(b[0], O, key_u, lim, H);
+    float bm = T[0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(b[0].v[db][2 * i], b[0].v[db][2 * i + 1]), p[i], O[db]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) bm = fmaxf(bm, T[r]);
+    bm *= ks;
+    bm = fmaxf(bm, other_half(bm));
+    if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) raise<D>(O, m, l, bm);
+    S = T;
+  };
+  int u = -1, n = sub, t = 0;  // (a unit past the last one: nothing but the end of the pipeline)
+  auto reach = [&](int tile) __attribute__((always_inline)) {
+    for (; t <= tile; ++t) arrive(t);
+  };
+#pragma unroll 1
+  for (; n < nu; n += parts) {
+    reach(n >> 1);
+    unit(u < 0 ? n : u, n);
+    u = n;
   }
+  reach(nt - 1);
+  if (u >= 0) unit(u, u);
   __syncthreads();
 }
 
-// The rest of an item: sums of the waves of a block put together, a range of dimensions each, and stored.  (The tiles' places are free.)
+// The rest of an item: sums of the waves of a block put together, a range of dimensions each, and stored.  (The ring is free.)
 template <int D>
 __device__ __forceinline__ void wg_store(float* smem, const WgShare& s, int w, int lane, f32x16* O, float m, float l, bool row_ok, float* part_o,
                                          float* part_ml, size_t at) {
@@ -565,21 +624,23 @@ __device__ __forceinline__ void wg_store(float* smem, const WgShare& s, int w, i
   if (H == 0 && s.sub == 0) *(float2*)(part_ml + at * 2) = make_float2(m, l);
 }
 
-// Workgroups with shared items, then with own ones, a wave each.
+// Workgroups with own items, a wave each, then with shared ones.
 template <int D>
 __global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_wg(Q8DecodeArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 31;
   f32x16 O[D / 32];
   float m, l;
-  if ((int)blockIdx.x < a.items_a) {
-    int x = blockIdx.x;
+  const int own = gridDim.x - a.items_a;
+  if ((int)blockIdx.x >= own) {
+    int x = blockIdx.x - own;
     const int hk = x % a.hkv;
     x /= a.hkv;
-    const int split = x % a.splits_a;
-    x /= a.splits_a;
-    const int row0 = x % a.rb_max * WG_ROWS, g = x / a.rb_max;
+    const int rb = x % a.rb_max;
+    x /= a.rb_max;
+    const int split = x % a.splits_a, g = x / a.splits_a;
     const int branch0 = a.group_branch_off[g], nrows = (a.group_branch_off[g + 1] - branch0) * a.G, len = a.shared_len[g];
+    const int row0 = rb * WG_ROWS;
     if (row0 >= nrows) return;
     const int p0 = split * a.chunk_a, p1 = min(p0 + a.chunk_a, (len + PAGE - 1) / PAGE);
     const WgShare s = wg_share(w, min((nrows - row0 + 31) / 32, WG_WAVES));
@@ -593,11 +654,11 @@ __global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_wg(Q8DecodeArgs 
     }
     bf16x8 q[D / 16];
     load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-    wg_stream<D, false>(a.kv, a.shared_pages + a.shared_page_off[g], p0, p1, len, len, len, hk, a.sc, smem, w, lane, s.sub, s.parts, q, O, m, l);
+    wg_stream<D, false>(a.kv, a.shared_pages + a.shared_page_off[g], p0, p1, len, len, len, hk, a.sc, smem, w, lane, s.sub, s.parts, s.most, q, O, m, l);
     wg_store<D>((float*)smem, s, w, lane, O, m, l, row_ok, a.part_o, a.part_ml, at);
     return;
   }
-  int x = (blockIdx.x - a.items_a) * WG_WAVES + w;
+  int x = blockIdx.x * WG_WAVES + w;
   const int hk = x % a.hkv;
   x /= a.hkv;
   const int split = x % a.splits_b, branch = x / a.splits_b;
@@ -625,11 +686,12 @@ __global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_seg_wg(Q8SegArgs
   const SegItem it = a.items[idx];
   const int slice = (it.nsplit >> 23) & 0x1fe, nsplit = it.nsplit & 0xffffff;
   const int npages = min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits), p1 = min(it.p0 + slice, npages);  // (a slice has 9 << 4 pages at most)
-  if (it.row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
-  const WgShare s = wg_share(w, min((it.nrows - it.row0 + 31) / 32, WG_WAVES));
-  const int row = it.row0 + 32 * s.block + L;
+  const int row0 = it.row0;
+  if (row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
+  const WgShare s = wg_share(w, min((it.nrows - row0 + 31) / 32, WG_WAVES));
+  const int row = row0 + 32 * s.block + L;
   const bool row_ok = row < it.nrows;
-  const int rr = row_ok ? row : it.row0;
+  const int rr = row_ok ? row : row0;
   const int entry = it.e0 + rr / a.G, head = hk * a.G + rr % a.G, place = it.place + rr / a.G * nsplit;
   const bool there = entry >= 0 && entry < a.total_readers;
   const bool store_ok = row_ok && there && place < a.splits * a.total_readers;
@@ -646,7 +708,7 @@ __global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_seg_wg(Q8SegArgs
   load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
   f32x16 O[D / 32];
   float m, l;
-  wg_stream<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, smem, w, lane, s.sub, s.parts, q, O, m, l);
+  wg_stream<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, smem, w, lane, s.sub, s.parts, s.most, q, O, m, l);
   wg_store<D>((float*)smem, s, w, lane, O, m, l, store_ok, a.part_o, a.part_ml, at);
 }
 
