@@ -309,10 +309,15 @@ _DECODE_ARRAYS = ("group_branch_off", "shared_page_off", "shared_pages", "shared
                   "branch_pages", "branch_len", "branch_pos")
 
 
+def _int32(x, name):
+    if x.dtype != torch.int32 or not x.is_contiguous():
+        raise TypeError("%s has to be a contiguous int32 tensor" % name)
+
+
 def _device_arrays(arrays):
     for name, x in arrays.items():
-        if x is not None and (x.dtype != torch.int32 or not x.is_contiguous()):
-            raise TypeError("%s has to be a contiguous int32 tensor" % name)
+        if x is not None:
+            _int32(x, name)
     return arrays
 
 
@@ -490,6 +495,7 @@ class KvCacheQ8:
         self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
         self.hkv, self.head_dim = hkv, d
         self.c = dag_kv_q8_t(k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, hkv, d)
+        self.ref = C.byref(self.c)
 
     @classmethod
     def empty(cls, n_pages, hkv, head_dim, device):
@@ -500,28 +506,26 @@ class KvCacheQ8:
         return cls(pool(head_dim // 16, PAGE, 16), pool(head_dim, PAGE), one(), one())
 
 
-def _on_current_device(*tensors):
+def _here(*tensors):
+    """The current stream's handle; every tensor has to be on its device."""
     here = torch.cuda.current_device()
     for x in tensors:
-        if x is not None and x.numel() and x.get_device() != here:
+        if x.get_device() != here and x.numel():
             raise ValueError("tensors have to be on the current device, cuda:%d: got %s" % (here, x.device))
-
-
-def _rows_of(x, heads, dim, what):
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim or not x.is_contiguous():
-        raise ValueError("%s has to be a contiguous [rows][%d][%d]" % (what, heads, dim))
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 def dag_kv_append_rope_q8(cache, slots, pos, k_new, v_new, theta):
     n = slots.numel()
-    _rows_of(k_new, cache.hkv, cache.head_dim, "k_new")
-    _rows_of(v_new, cache.hkv, cache.head_dim, "v_new")
-    if not (k_new.shape[0] == v_new.shape[0] == pos.numel() == n) or k_new.dtype != v_new.dtype:
-        raise ValueError("slots, pos, k_new and v_new are of one length, k_new and v_new of one type")
-    _device_arrays({"slots": slots, "pos": pos})
-    _on_current_device(slots, pos, k_new, v_new, cache.k_pool)
-    _check(lib().dag_kv_append_rope_q8(C.byref(cache.c), slots.data_ptr(), pos.data_ptr(), n, k_new.data_ptr(),
-                                       v_new.data_ptr(), theta, _dtype_code(k_new), _stream()))
+    shape = (n, cache.hkv, cache.head_dim)
+    if k_new.shape != shape or v_new.shape != shape or pos.numel() != n or k_new.dtype != v_new.dtype:
+        raise ValueError("k_new and v_new are [tokens][%d][%d] of one type, slots and pos as long" % shape[1:])
+    if not k_new.is_contiguous() or not v_new.is_contiguous():
+        raise ValueError("k_new and v_new have to be contiguous")
+    _int32(slots, "slots")
+    _int32(pos, "pos")
+    _check(lib().dag_kv_append_rope_q8(cache.ref, slots.data_ptr(), pos.data_ptr(), n, k_new.data_ptr(), v_new.data_ptr(),
+                                       theta, _dtype_code(k_new), _here(slots, pos, k_new, v_new, cache.k_pool)))
 
 
 def dag_decode_q8_workspace_bytes(ddesc, cache, hq):
@@ -538,9 +542,8 @@ def _decode_q8(call, desc, q, cache, out, workspace, softmax_scale):
         raise ValueError("q and out are [n_live][heads][head_dim]")
     if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous():
         raise TypeError("q and out are contiguous bfloat16")
-    _on_current_device(q, out, cache.k_pool, workspace)
-    _check(call(C.byref(desc.c), C.byref(cache.c), q.data_ptr(), out.data_ptr(), hq,
-                d ** -0.5 if softmax_scale is None else softmax_scale, workspace.data_ptr(), workspace.numel(), _stream()))
+    _check(call(desc.c, cache.ref, q.data_ptr(), out.data_ptr(), hq, d ** -0.5 if softmax_scale is None else softmax_scale,
+                workspace.data_ptr(), workspace.numel(), _here(q, out, cache.k_pool, workspace)))
 
 
 def dag_attn_decode_q8(ddesc, q, cache, out, workspace, softmax_scale=None):
@@ -567,37 +570,48 @@ def _at(x):
     return 0 if x is None else x.data_ptr()
 
 
-def _lengths(rows, **arrays):
-    n = {"slots": None, "pos": None, "pages": None, "free_count": 1, "free_count_out": 1, "refused": 1,
-         "new_off": rows.c.n_rows + 1, "page_off": rows.c.n_rows + 1}
+def _ints(n, **arrays):
+    """int32 tensors of n elements each."""
     for name, x in arrays.items():
-        want = n.get(name, rows.c.n_rows)
-        if x is not None and want is not None and x.numel() != want:
-            raise ValueError("%s has %d elements, not %d" % (name, x.numel(), want))
-    _device_arrays(arrays)
-    _on_current_device(rows.table, *arrays.values())
+        if x.numel() != n:
+            raise ValueError("%s has %d elements, not %d" % (name, x.numel(), n))
+        _int32(x, name)
 
 
 def dag_kv_release(rows, ended, row_len, row_len_out, free_count, free_count_out):
-    _lengths(rows, ended=ended, row_len=row_len, row_len_out=row_len_out, free_count=free_count, free_count_out=free_count_out)
-    _check(lib().dag_kv_release(C.byref(rows.c), ended.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(),
-                                free_count.data_ptr(), free_count_out.data_ptr(), rows.workspace.data_ptr(),
-                                rows.workspace.numel(), _stream()))
+    _ints(rows.c.n_rows, ended=ended, row_len=row_len, row_len_out=row_len_out)
+    _ints(1, free_count=free_count, free_count_out=free_count_out)
+    _check(lib().dag_kv_release(rows.c, ended.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(), free_count.data_ptr(),
+                                free_count_out.data_ptr(), rows.workspace.data_ptr(), rows.workspace.numel(),
+                                _here(rows.table, ended, row_len, row_len_out, free_count, free_count_out)))
 
 
 def dag_kv_tables(rows, new_len, row_len, row_len_out, free_count, free_count_out, new_off, slots, pos0=None, pos=None,
                   page_off=None, pages=None, refused=None):
     """`pos` is as long as `slots`; entries past the ends of `slots` and `pages` are dropped."""
-    if pos is not None and pos.numel() != slots.numel():
-        raise ValueError("pos and slots are of one length")
-    _lengths(rows, new_len=new_len, row_len=row_len, row_len_out=row_len_out, free_count=free_count,
-             free_count_out=free_count_out, new_off=new_off, slots=slots, pos0=pos0, pos=pos, page_off=page_off, pages=pages,
-             refused=refused)
-    _check(lib().dag_kv_tables(C.byref(rows.c), new_len.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(),
-                               free_count.data_ptr(), free_count_out.data_ptr(), new_off.data_ptr(), slots.data_ptr(),
-                               slots.numel(), _at(pos0), _at(pos), _at(page_off), _at(pages),
-                               0 if pages is None else pages.numel(), _at(refused), rows.workspace.data_ptr(),
-                               rows.workspace.numel(), _stream()))
+    n_rows, n_slots, n_pages = rows.c.n_rows, slots.numel(), 0
+    _ints(n_rows, new_len=new_len, row_len=row_len, row_len_out=row_len_out)
+    _ints(1, free_count=free_count, free_count_out=free_count_out)
+    _ints(n_rows + 1, new_off=new_off)
+    _int32(slots, "slots")
+    optional = [x for x in (pos0, pos, page_off, pages, refused) if x is not None]
+    if pos0 is not None:
+        _ints(n_rows, pos0=pos0)
+    if pos is not None:
+        _ints(n_slots, pos=pos)
+    if page_off is not None:
+        _ints(n_rows + 1, page_off=page_off)
+    if pages is not None:
+        n_pages = pages.numel()
+        _int32(pages, "pages")
+    if refused is not None:
+        _ints(1, refused=refused)
+    _check(lib().dag_kv_tables(rows.c, new_len.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(), free_count.data_ptr(),
+                               free_count_out.data_ptr(), new_off.data_ptr(), slots.data_ptr(), n_slots, _at(pos0), _at(pos),
+                               _at(page_off), _at(pages), n_pages, _at(refused), rows.workspace.data_ptr(),
+                               rows.workspace.numel(),
+                               _here(rows.table, new_len, row_len, row_len_out, free_count, free_count_out, new_off, slots,
+                                     *optional)))
 
 
 class Scheduler:

@@ -1637,7 +1637,6 @@ extern "C" int dag_attn_decode_segments(const dag_decode_seg_desc_t* d, const vo
   a.hkv = hkv;
   a.G = hq / hkv;
   a.rb_max = p.rb_max;
-  a.row_shift = 5;
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.total_readers = d->total_readers;

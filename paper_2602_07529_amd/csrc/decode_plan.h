@@ -221,7 +221,7 @@ struct SegPlan {
 
 // What the lists have room for: one split size for all segments (their lengths live in device memory), as long as possible while the
 // launch still has about a thousand items if every segment were the longest one.  k_seg_plan settles the slices that are taken.
-inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D, const DecodeKnobs& knobs, SegPlan* p, int block_rows = 32) {
+inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D, const DecodeKnobs& knobs, SegPlan* p) {
   if (!d) return DAG_ERR_NULL;
   if (d->n_live < 0 || d->n_segments < 0 || d->max_seg_pages < 0 || d->max_readers < 0 || d->total_readers < 0)
     return DAG_ERR_BAD_LEN;
@@ -229,7 +229,7 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
   if (hq < 1 || hkv < 1 || hq % hkv != 0 || hq / hkv > 32) return DAG_ERR_UNSUPPORTED;
   if (D != 64 && D != 128) return DAG_ERR_UNSUPPORTED;
   const int G = hq / hkv;
-  p->rb_max = (int)dag_ceil_div((int64_t)d->max_readers * G, block_rows);
+  p->rb_max = (int)dag_ceil_div((int64_t)d->max_readers * G, 32);
   if (p->rb_max < 1) p->rb_max = 1;
   const int knob = knobs.chunk_seg;
   int c = knob ? knob : 128;
@@ -255,12 +255,29 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
 }
 
 // Decode over an 8-bit cache: slices of about one length, so that there are Q8_WAVES of them and all run at once (what was measured
-// stands at stream_slice), no shorter than Q8_LEAST_PAGES.
-constexpr int Q8_WAVES = 1536, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
-// More than 32 rows of a KV head in some group: workgroups for up to WG_ROWS of them, whose page ids sit in three registers.
-constexpr int WG_ROWS = 256, WG_MOST_PAGES = 144, WG_LEAST_PAGES = 16, WG_GROUPS = 256;
+// stands at stream_slice; more of them where groups have more than 32 rows, 88 -> 86 us for two groups of 32 over 32768 | 640), no shorter than
+// Q8_LEAST_PAGES.
+constexpr int Q8_WAVES = 1536, Q8_WIDE_WAVES = 1920, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
+// Segments: slices by the rules of the bf16 cache, but for more than 32 rows, whose pages weigh less: shorter slices (nine new tokens of 48 nodes 95 -> 69 us).
+constexpr float Q8_SEG_WIDE = 0.5f;
+// Short contexts: a workgroup to a (branch, KV head) takes them whole, one launch.  Its lines, from 112 steps of 1 to 64 branches on 8 KV heads
+// (4 query heads each) in graphs, items and merge : whole.  Pages that a branch reads: dimension 128, up to 28 of them 1.1 to 1.4, 41 0.96 to
+// 1.02, 63 0.9, 101 0.76; dimension 64 41 1.03 to 1.1, 63 0.94 to 1.  With 256 workgroups, which fill the device, 1.1 to 1.4 up to
+// 101 pages; with 512 dimension 64 1.04 to 1.36 up to 41 pages, dimension 128 0.66 to 0.92.
+// Segments, whose items take a launch more: 1.0 to 1.9 at dimension 128, 1.2 to 1.9 at 64, up to 106 pages (four entries to a branch,
+// 63 pages in the longest segment: what the host knows is 252).
+constexpr int WHOLE_Q8_GROUPS = 256, WHOLE_Q8_FULL = 192, WHOLE_Q8_FULL_PAGES = 101;
+inline bool q8_whole(int64_t groups, int64_t pages, int D) {
+  const int few = D == 64 ? 52 : 41;
+  return (groups <= WHOLE_Q8_GROUPS && pages <= (groups >= WHOLE_Q8_FULL ? WHOLE_Q8_FULL_PAGES : few)) ||
+         (D == 64 && groups <= 2 * WHOLE_Q8_GROUPS && pages <= 41);
+}
+inline bool q8_whole_segments(const dag_decode_seg_desc_t* d, int hkv, int D) {
+  return d->n_segments <= 64 && (int64_t)d->n_live * hkv <= WHOLE_Q8_GROUPS &&
+         dag_ceil_div(d->total_readers, d->n_live) * d->max_seg_pages <= (D == 64 ? 384 : 256);
+}
 struct Q8Plan {
-  bool wg;
+  bool whole;  // no items
   int rb_max, chunk_a, splits_a, chunk_b, splits_b, items_a, items_b;
   size_t off_ml, bytes;
 };
@@ -272,33 +289,24 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
   if (D != 64 && D != 128) return DAG_ERR_UNSUPPORTED;
   const int shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages;
   const int64_t most_rows = (int64_t)d->max_group_size * (hq / hkv);
-  p->wg = shared > 0 && most_rows > 32;
-  p->rb_max = (int)dag_ceil_div(most_rows, p->wg ? WG_ROWS : 32);
+  p->rb_max = (int)dag_ceil_div(most_rows, 32);
   const int64_t base_a = (int64_t)d->n_groups * hkv * p->rb_max, base_b = (int64_t)d->n_live * hkv;
   auto cut = [](int pages, int64_t most, int* splits, int* chunk) {  // slices of one length, of whole pairs of pages
     *splits = (int)dag_ceil_div(pages, most);
     *chunk = *splits > 0 ? (int)dag_ceil_div(dag_ceil_div(pages, *splits), 2) * 2 : 2;
     *splits = (int)dag_ceil_div(pages, *chunk);
   };
-  auto within = [](int64_t x, int least, int most) { return x < least ? least : x > most ? most : x; };
-  const int64_t own_waves = p->wg ? Q8_WAVES / 2 : Q8_WAVES;
-  const int64_t share_a = p->wg ? within(dag_ceil_div(base_a * shared, WG_GROUPS), WG_LEAST_PAGES, WG_MOST_PAGES)
-                                : within(dag_ceil_div(base_a * shared + base_b * own, Q8_WAVES), Q8_LEAST_PAGES, Q8_MOST_PAGES);
-  const int64_t share_b = p->wg ? within(dag_ceil_div(base_b * own, own_waves), Q8_LEAST_PAGES, Q8_MOST_PAGES) : share_a;
-  cut(base_a > 0 ? shared : 0, share_a, &p->splits_a, &p->chunk_a);
-  cut(own, share_b, &p->splits_b, &p->chunk_b);
+  const int64_t share = dag_ceil_div(base_a * shared + base_b * own, p->rb_max > 1 ? Q8_WIDE_WAVES : Q8_WAVES);
+  const int64_t most = share < Q8_LEAST_PAGES ? Q8_LEAST_PAGES : share > Q8_MOST_PAGES ? Q8_MOST_PAGES : share;
+  cut(base_a > 0 ? shared : 0, most, &p->splits_a, &p->chunk_a);
+  cut(own, most, &p->splits_b, &p->chunk_b);
   const int64_t ia = base_a * p->splits_a, ib = base_b * p->splits_b;
   const int64_t rows = (int64_t)d->n_live * ((int64_t)p->splits_a + p->splits_b) * hq;
   if (ia + ib > INT32_MAX || rows > INT32_MAX || (int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;
   p->items_a = (int)ia;
   p->items_b = (int)ib;
+  p->whole = ia + ib > 0 && q8_whole(base_b, (int64_t)shared + own, D);
   p->off_ml = dag_align_up((size_t)rows * D * 4, 256);
   p->bytes = p->off_ml + dag_align_up((size_t)rows * 2 * 4, 256) + 256;
   return DAG_OK;
-}
-
-inline int make_q8_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D, SegPlan* p, bool* wg) {
-  const int rc = make_seg_plan(d, hq, hkv, D, DecodeKnobs{0, 0, 0}, p);
-  *wg = rc == DAG_OK && p->rb_max > 1;
-  return *wg ? make_seg_plan(d, hq, hkv, D, DecodeKnobs{0, 0, 0}, p, WG_ROWS) : rc;
 }

@@ -75,24 +75,56 @@ struct Block {         // 32 keys (two pages)
   u32x4 v[D / 32];     // v[db]: the slots of page H of dimension 32 db + L
 };
 
-template <int D>
-__device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pages, int rel, int last_rel, int hk, int L, int H) {
-  const int pg0 = __builtin_amdgcn_readlane(pages, min(rel, last_rel) & 63), pg1 = __builtin_amdgcn_readlane(pages, min(rel + 1, last_rel) & 63);
-  const int slot = (L & 3) + 4 * (L >> 3);
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const uint8_t* p) {  // ONCE: nobody else reads it
+  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4*)p);
+  else return *(const u32x4*)p;
+}
+// pages: of 64 pages, a lane each; rel, rel + 1: the two of the block, last: the slice's last one
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pages, int rel, int last, int hk, int L, int H) {
+  const int pg0 = __builtin_amdgcn_readlane(pages, min(rel, last) & 63), pg1 = __builtin_amdgcn_readlane(pages, min(rel + 1, last) & 63);
   const size_t base0 = ((size_t)pg0 * c.hkv + hk) * (D * PAGE), base1 = ((size_t)pg1 * c.hkv + hk) * (D * PAGE);
-  const uint8_t* const kp = c.k_pool + ((L >> 2) & 1 ? base1 : base0) + H * 256 + slot * 16;
+  const uint8_t* const kp = c.k_pool + (L >> 2 & 1 ? base1 : base0) + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16;
   const uint8_t* const vp = c.v_pool + (H ? base1 : base0) + L * 16;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.k[s] = __builtin_nontemporal_load((const u32x4*)(kp + s * 512));
+  for (int s = 0; s < D / 32; ++s) b.k[s] = load16<ONCE>(kp + s * 512);
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) b.v[s] = __builtin_nontemporal_load((const u32x4*)(vp + s * 512));
+  for (int s = 0; s < D / 32; ++s) b.v[s] = load16<ONCE>(vp + s * 512);
+}
+
+// Sums of a wave: 32 rows, a lane has a column (row L) of them.
+template <int D>
+struct Sums {
+  f32x16 O[D / 32];
+  float m, l;
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+    m = -1e30f;
+    l = 0.f;
+  }
+};
+
+// Slots from vlen on hold no token: their codes may be no numbers, which a probability of zero does not keep from the sums.
+template <int D>
+__device__ __forceinline__ void clear_behind(Block<D>& b, int key0, int vlen, int H) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int n = vlen - (key0 + 16 * H + 4 * w);  // slots of this word that hold one
+    const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) b.v[db][w] &= mask;
+  }
 }
 
 // A block some of whose tokens are hidden from some rows only (the new tokens of a node): a value that is no number may not reach the rows
 // that do not see it, and a probability of zero does not keep it from them.  Such codes are cleared, and the sums of the rows that
 // see one become no number: a product of "is none" and "is seen" finds them.
 template <int D>
-__device__ __forceinline__ void hide_not_numbers(Block<D>& b, f32x16* O, int key0, int lim, int H) {
+__device__ __forceinline__ void hide_not_numbers(Block<D>& b, Sums<D>& sums, int key0, int lim, int H) {
   uint32_t any = 0;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -117,178 +149,153 @@ __device__ __forceinline__ void hide_not_numbers(Block<D>& b, f32x16* O, int key
     n = mfma32(codes_to_bf16(one[0], one[1]), __builtin_convertvector(seen[0], bf16x8), n);
     n = mfma32(codes_to_bf16(one[2], one[3]), __builtin_convertvector(seen[1], bf16x8), n);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) O[db][r] = n[r] > 0.f ? NAN : O[db][r];
+    for (int r = 0; r < 16; ++r) sums.O[db][r] = n[r] > 0.f ? NAN : sums.O[db][r];
   }
 }
 
 // The exponent's reference m is raised only where a score is more than this above it (log2): the rescale of the sums stays rare.
 constexpr float Q8_TH = 3.f;
 
-// The reference to at least bm, the sums with it.
-template <int D>
-__device__ __forceinline__ void raise(f32x16* O, float& m, float& l, float bm) {
-  const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
-  l *= alpha;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
-  m = m_new;
-}
-
-// Slots from vlen on hold no token: their codes may be no numbers, which a probability of zero does not keep from the sums.
-template <int D>
-__device__ __forceinline__ void clear_behind(Block<D>& b, int key0, int vlen, int H) {
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int n = vlen - (key0 + 16 * H + 4 * w);  // slots of this word that hold one
-    const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) b.v[db][w] &= mask;
-  }
-}
-
-// U blocks together: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
-// lv: log2 of its value scale.  A lane's 16 scores of a block are of one page, so their largest is found among the plain products, one
+// A block: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
+// lv: log2 of its value scale.  A lane's 16 scores are of one page, so their largest is found among the plain products, one
 // multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.
-// key0: first key of the first block; keys from `lim` on are hidden from this lane's row; len: the smallest lim of the wave; slots from vlen on
-// hold no token.  What bounds a wave by itself is the chain from the scores to the second product: two blocks share it.
-template <int D, int U, bool LIMITS, typename QF, typename VF>
-__device__ __forceinline__ void compute_blocks(Block<D> (&b)[U], QF&& q, VF&& values, f32x16* O, float& m, float& l, const float (&ks)[U],
-                                               const float (&lv)[U], int key0, int len, int lim, int vlen, int H) {
-  f32x16 S[U];
+// key0: first key of the block; keys from `lim` on are hidden from the lane's row; len: the smallest lim of the wave; slots from vlen on hold
+// no token.  A wave by itself takes 1,005 cycles for a block at head dimension 128, two waves of a SIMD 512 each, as long as the 16 MFMAs.
+template <int D, bool LIMITS>
+__device__ __forceinline__ void compute_block(Block<D>& b, const bf16x8 (&q)[D / 16], Sums<D>& sums, float ks, float lv, int key0, int len, int lim,
+                                              int vlen, int H) {
+  f32x16 S;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) S[u][r] = 0.f;
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) S[u] = mfma32(codes_to_bf16(b[u].k[s][0], b[u].k[s][1]), q(2 * s), S[u]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) S[u] = mfma32(codes_to_bf16(b[u].k[s][2], b[u].k[s][3]), q(2 * s + 1), S[u]);
-  }
-  values(b);
-  if (key0 + 32 * U > len) {
+  for (int s = 0; s < D / 16; ++s) S = mfma32(codes_to_bf16(b.k[s >> 1][2 * (s & 1)], b.k[s >> 1][2 * (s & 1) + 1]), q[s], S);
+  if (key0 + 32 > len) {
     asm volatile("");  // (a branch: the compiler would compare and select in every block)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) S[u][r] = key0 + 32 * u + 16 * H + r < lim ? S[u][r] : -INFINITY;
+    for (int r = 0; r < 16; ++r) S[r] = key0 + 16 * H + r < lim ? S[r] : -INFINITY;
   }
-  float bm = -INFINITY;
+  float bm = S[0];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float x = S[u][0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) x = fmaxf(x, S[u][r]);
-    bm = fmaxf(bm, x * ks[u]);
-  }
+  for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
+  bm *= ks;
   bm = fmaxf(bm, other_half(bm));
-  if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) raise<D>(O, m, l, bm);
-  bf16x8 p[U][2];
+  if (__builtin_amdgcn_ballot_w64(bm > sums.m + Q8_TH) != 0) {
+    const float m_new = fmaxf(sums.m, bm), alpha = __builtin_amdgcn_exp2f(sums.m - m_new);
+    sums.l *= alpha;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const float ref = lv[u] - m;
-    f32x8 x[2];
-    float sum[2] = {0.f, 0.f};
+    for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[u][r], ks[u], ref));
-      sum[r >> 3] += x[r >> 3][r & 7];
-    }
-    l = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-lv[u]), l);
-    // (rounded to bf16, as the probabilities over a bf16 cache are)
-    p[u][0] = __builtin_convertvector(x[0], bf16x8);
-    p[u][1] = __builtin_convertvector(x[1], bf16x8);
+      for (int r = 0; r < 16; ++r) sums.O[db][r] *= alpha;
+    sums.m = m_new;
   }
+  const float ref = lv - sums.m;
+  f32x8 x[2];
+  float sum[2] = {0.f, 0.f};
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int first = key0 + 32 * u;
-    if (first + 32 > vlen) clear_behind<D>(b[u], first, vlen, H);
-    if constexpr (LIMITS)
-      if (first + 32 > len && len < vlen) hide_not_numbers<D>(b[u], O, first, lim, H);
+  for (int r = 0; r < 16; ++r) {
+    x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], ks, ref));
+    sum[r >> 3] += x[r >> 3][r & 7];
   }
+  sums.l = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-lv), sums.l);
+  // (rounded to bf16, as the probabilities over a bf16 cache are)
+  const bf16x8 p[2] = {__builtin_convertvector(x[0], bf16x8), __builtin_convertvector(x[1], bf16x8)};
+  if (key0 + 32 > vlen) clear_behind<D>(b, key0, vlen, H);
+  if constexpr (LIMITS)
+    if (key0 + 32 > len && len < vlen) hide_not_numbers<D>(b, sums, key0, lim, H);
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int e = 0; e < 2; ++e)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(b[u].v[db][2 * i], b[u].v[db][2 * i + 1]), p[u][i], O[db]);
+    for (int db = 0; db < D / 32; ++db) sums.O[db] = mfma32(codes_to_bf16(b.v[db][2 * e], b.v[db][2 * e + 1]), p[e], sums.O[db]);
 }
 
-// Pages [p0, p1) of one list against the wave's 32 rows, two pages at a time, the next two on their way meanwhile (four of them are no
-// faster).  What bounds it is how the pages come from memory: pages that nobody else reads pass the caches by (ONCE; 16 groups of 8 over
-// 8192 | 1024 tokens 114 -> 101 us), and 1,300 to 1,800 waves ask for them, those of the KV heads of a page next to each other (-> 94 us =
-// 5.7 TB/s; 2,048 waves 99, 3,072 102 to 123; the loads alone of 2,048 waves take 98.6).
-template <int D, bool LIMITS>
-__device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk,
-                                             float sc, int lane, const bf16x8 (&q)[D / 16], f32x16* O, float& m, float& l) {
-  const int L = lane & 31, H = lane >> 5, np = p1 - p0;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
-  m = -1e30f;
-  l = 0.f;
-  int pg = 0;
-  float ksv = 0.f, lvv = 0.f;
-  auto window = [&](int rel) __attribute__((always_inline)) {  // of 64 pages, a lane each: id (clamped to the pool) and scales
-    pg = min(max(pages[p0 + min(rel + lane, np - 1)], 0), c.n_pages - 1);
-    ksv = c.k_scale[(size_t)pg * c.hkv + hk] * fabsf(sc);
-    lvv = __builtin_amdgcn_logf(c.v_scale[(size_t)pg * c.hkv + hk]);
-  };
-  auto of_page = [&](float x, int rel) __attribute__((always_inline)) {  // of page rel + H
+// Page ids (clamped to the pool) and scales of 64 pages of a slice, a lane each.
+struct Window {
+  int pg;
+  float ks, lv;
+  __device__ __forceinline__ void ask(const Q8Cache& c, const int32_t* pages, int rel, int np, int hk, int lane) {
+    pg = min(max(pages[min(rel + lane, np - 1)], 0), c.n_pages - 1);
+    ks = c.k_scale[(size_t)pg * c.hkv + hk];
+    lv = c.v_scale[(size_t)pg * c.hkv + hk];
+  }
+  __device__ __forceinline__ void have(float sc) {
+    ks *= fabsf(sc);
+    lv = __builtin_amdgcn_logf(lv);
+    asm volatile("" ::"v"(ks), "v"(lv));  // (arrived: a wait for them later would also wait for the blocks in flight)
+  }
+  static __device__ __forceinline__ float of(float x, int rel, int np, int H) {  // of page rel + H
     const float a = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), min(rel, np - 1) & 63));
     const float b = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), min(rel + 1, np - 1) & 63));
     return H ? b : a;
-  };
+  }
+};
+
+// Pages [p0, p1) of one list against the wave's 32 rows, added to its sums, two pages at a time, the next two on their way meanwhile.
+// What bounds it is how the pages come from memory: a page that nobody else reads (ONCE) passes the caches by (16 groups of 8 over
+// 8192 | 1024 tokens 114 -> 101 us), and 1,300 to 1,800 waves ask for them, those of the KV heads of a page next to each other (-> 94 us =
+// 5.7 TB/s; 2,048 waves 99, 3,072 102 to 123; the loads alone of 2,048 waves take 98.6).  Four pages ahead are no faster.
+template <int D, bool LIMITS, bool ONCE>
+__device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk,
+                                             float sc, int lane, const bf16x8 (&q)[D / 16], Sums<D>& sums) {
+  const int L = lane & 31, H = lane >> 5, np = p1 - p0;
+  Window win;
   struct Ahead {
-    Block<D> b[1];
-    float ks[1], lv[1];
+    Block<D> b;
+    float ks, lv;
   };
-  Ahead x0, x1;
-  auto load = [&](Ahead& x, int rel) __attribute__((always_inline)) {
-    if ((rel & 63) == 0 && rel < np) {
-      window(rel);
-      asm volatile("" ::"v"(ksv), "v"(lvv));  // arrived: a wait for them later would also wait for the blocks in flight
+  Ahead x[2];
+  auto load = [&](Ahead& y, int rel) __attribute__((always_inline)) {
+    const bool first = (rel & 63) == 0 && rel < np;
+    if (first) win.ask(c, pages + p0, rel, np, hk, lane);
+    load_block<D, ONCE>(y.b, c, win.pg, rel, np - 1, hk, L, H);
+    if (first) win.have(sc);
+    y.ks = Window::of(win.ks, rel, np, H);
+    y.lv = Window::of(win.lv, rel, np, H);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto compute = [&](Ahead& y, int rel) __attribute__((always_inline)) {
+    compute_block<D, LIMITS>(y.b, q, sums, y.ks, y.lv, (p0 + rel) * PAGE, len, lim, vlen, H);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // No load behind a condition: the wait for a block would then be one for the block behind it as well (107 us instead of 98 for three levels
+  // of segments).  What is loaded behind the slice is its last page again, which nobody uses.
+  load(x[0], 0);
+  for (int rel = 0;;) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      load(x[1 - i], rel + 2);
+      compute(x[i], rel);
+      if ((rel += 2) >= np) return;
     }
-    x.ks[0] = of_page(ksv, rel);
-    x.lv[0] = of_page(lvv, rel);
-    load_block<D>(x.b[0], c, pg, rel, np - 1, hk, L, H);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  auto compute = [&](Ahead& x, int rel) __attribute__((always_inline)) {
-    compute_blocks<D, 1, LIMITS>(x.b, [&](int s) { return q[s]; }, [](auto&) {}, O, m, l, x.ks, x.lv, (p0 + rel) * PAGE, len, lim, vlen, H);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  // No load behind a condition: the wait for a block would then be one for the block behind it as well.  What is loaded behind the slice is
-  // its last page again, which nobody uses.
-  load(x0, 0);
-  for (int rel = 0; rel < np; rel += 4) {
-    load(x1, rel + 2);
-    compute(x0, rel);
-    load(x0, rel + 4);
-    if (rel + 2 < np) compute(x1, rel + 2);
   }
 }
 
 // Query operands of the lane's row: step 2 s + u has dims 16 (2 s + H) + 8 u .., with the sign of the softmax scale.
 template <int D>
-__device__ __forceinline__ void load_q(bf16x8 (&q)[D / 16], const uint16_t* row, float sc, int lane) {
-  const uint16_t* const p = row + 16 * (lane >> 5);
+__device__ __forceinline__ void fetch_q(bf16x8 (&q)[D / 16], const uint16_t* row, int lane) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) q[s] = *(const bf16x8*)(row + 16 * (lane >> 5) + 32 * (s >> 1) + 8 * (s & 1));
+}
+template <int D>
+__device__ __forceinline__ void sign_q(bf16x8 (&q)[D / 16], float sc) {
   const uint32_t sign = sc < 0.f ? 0x80008000u : 0u;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
-    u32x4 x = *(const u32x4*)(p + 32 * (s >> 1) + 8 * (s & 1));
+    u32x4 x = __builtin_bit_cast(u32x4, q[s]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] ^= sign;
     q[s] = __builtin_bit_cast(bf16x8, x);
   }
 }
+template <int D>
+__device__ __forceinline__ void load_q(bf16x8 (&q)[D / 16], const uint16_t* row, float sc, int lane) {
+  fetch_q<D>(q, row, lane);
+  sign_q<D>(q, sc);
+}
 
 template <int D>
-__device__ __forceinline__ void store_part(float* part_o, float* part_ml, size_t at, const f32x16* O, float m, float l, int H) {
+__device__ __forceinline__ void store_part(float* part_o, float* part_ml, size_t at, const Sums<D>& sums, int H) {
+  const f32x16(&O)[D / 32] = sums.O;
+  const float m = sums.m, l = sums.l + other_half(sums.l);
   float* const po = part_o + at * D;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -298,418 +305,196 @@ __device__ __forceinline__ void store_part(float* part_o, float* part_ml, size_t
   if (H == 0) *(float2*)(part_ml + at * 2) = make_float2(m, l);
 }
 
-// A wave to a work item: a slice of a group's shared pages against 32 of its (branch, query head) rows of a KV head, or a slice of a
-// branch's own pages against its rows.
-template <int D>
+// A slice of one list against 32 of its rows, those from row0 on: rows(i) says which query row the i-th is and where its partial goes.
+struct Row {
+  const uint16_t* q;
+  size_t at;   // of its partial
+  int lim;     // tokens of the list that it sees
+  bool store;
+};
+template <int D, bool LIMITS, bool ONCE, typename RF>
+__device__ __forceinline__ void run_item(const Q8Cache& c, const int32_t* pages, int p0, int p1, int vlen, int hk, float sc, int row0, int nrows, float* part_o,
+                                         float* part_ml, int lane, RF&& rows) {
+  const int L = lane & 31, H = lane >> 5;
+  const bool there = row0 + L < nrows;
+  const Row row = rows(there ? row0 + L : row0);
+  int len = vlen;
+  if constexpr (LIMITS) {  // the slice ends where its rows see no further
+    int most = row.lim;
+    len = row.lim;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      len = min(len, __shfl_xor(len, o));
+      most = max(most, __shfl_xor(most, o));
+    }
+    p1 = __builtin_amdgcn_readfirstlane(min(p1, (most + PAGE - 1) / PAGE));
+  }
+  if (p0 >= p1) {  // nothing there: a partial without weight
+    if (there && row.store && H == 0) *(float2*)(part_ml + row.at * 2) = make_float2(-1e30f, 0.f);
+    return;
+  }
+  bf16x8 q[D / 16];
+  load_q<D>(q, row.q, sc, lane);
+  Sums<D> sums;
+  sums.start();
+  stream_slice<D, LIMITS, ONCE>(c, pages, p0, p1, len, LIMITS ? row.lim : vlen, vlen, hk, sc, lane, q, sums);
+  if (there && row.store) store_part<D>(part_o, part_ml, row.at, sums, H);
+}
+
+// A wave to a work item: a slice of a group's shared pages against 32 of its (branch, query head) rows of a KV head, or a slice of a branch's
+// own pages against its rows.  WIDE: groups have more rows; their waves read the same pages at about the same time, and what they wait for is
+// memory: each has two pages on their way, so five blocks of rows have ten, of which two are different.  Two groups of 32 over
+// 32768 | 640, 5 heads on one: 88 us; workgroups of a wave to a block that find the pages in the L1 98, the pages in a ring
+// in LDS (80 KB on their way) 95, because the waves of a SIMD then do the same at the same time, 64 rows to a wave 90 to 101.
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
-  const int lane = threadIdx.x, L = lane & 31, H = lane >> 5;
+  const int lane = threadIdx.x;
   const bool shared = (int)blockIdx.x < a.items_a;
   int x = shared ? blockIdx.x : blockIdx.x - a.items_a;
   const int hk = x % a.hkv;
   x /= a.hkv;
-  const int splits = shared ? a.splits_a : a.splits_b, split = x % splits;
-  x /= splits;
   int row0 = 0;
   if (shared) {
     row0 = x % a.rb_max * 32;
     x /= a.rb_max;
   }
+  const int splits = shared ? a.splits_a : a.splits_b, split = x % splits;
+  x /= splits;
   const int branch0 = shared ? a.group_branch_off[x] : x;
   const int nrows = shared ? (a.group_branch_off[x + 1] - branch0) * a.G : a.G;
   const int32_t* const pages = shared ? a.shared_pages + a.shared_page_off[x] : a.branch_pages + a.branch_page_off[x];
   const int len = shared ? a.shared_len[x] : a.branch_len[x], chunk = shared ? a.chunk_a : a.chunk_b;
   if (row0 >= nrows) return;
-  const int npages = (len + PAGE - 1) / PAGE, p0 = split * chunk, p1 = min(p0 + chunk, npages);
-  const int row = row0 + L;
-  const bool row_ok = row < nrows;
-  const int rr = row_ok ? row : row0, branch = branch0 + rr / a.G, head = hk * a.G + rr % a.G;
-  if (branch < 0 || branch >= a.n_live) return;  // (offsets that point behind the branches)
-  const size_t at = (size_t)((shared ? 0 : a.first_own) + branch * splits + split) * a.hq + head;
-  if (p0 >= p1) {  // nothing there: a partial without weight
-    if (row_ok && H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
-    return;
-  }
-  bf16x8 q[D / 16];
-  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-  f32x16 O[D / 32];
-  float m, l;
-  stream_slice<D, false>(a.kv, pages, p0, p1, len, len, len, hk, a.sc, lane, q, O, m, l);
-  l += other_half(l);
-  if (row_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
+  const int p0 = split * chunk, p1 = min(p0 + chunk, (len + PAGE - 1) / PAGE);
+  auto rows = [&](int row) __attribute__((always_inline)) {
+    const int branch = min(max(branch0 + row / a.G, 0), a.n_live - 1), head = hk * a.G + row % a.G;
+    return Row{a.q + ((size_t)branch * a.hq + head) * D, (size_t)((shared ? 0 : a.first_own) + branch * splits + split) * a.hq + head, len, true};
+  };
+  run_item<D, false, !WIDE>(a.kv, pages, p0, p1, len, hk, a.sc, row0, nrows, a.part_o, a.part_ml, lane, rows);
 }
 
 // The same for the items that k_seg_plan listed.
-template <int D, bool LIMITS>
+template <int D, bool WIDE, bool LIMITS>
 __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
   const SegArgs& a = args.s;
-  const int lane = threadIdx.x, L = lane & 31, H = lane >> 5;
-  const int hk = blockIdx.x % a.hkv, idx = blockIdx.x / a.hkv;
+  const int lane = threadIdx.x, hk = blockIdx.x % a.hkv, idx = blockIdx.x / a.hkv;
   if (idx >= a.totals[0]) return;
   const SegItem it = a.items[idx];
   const int slice = (it.nsplit >> 23) & 0x1fe, nsplit = it.nsplit & 0xffffff;
-  const int npages = min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits);
-  int p1 = __builtin_amdgcn_readfirstlane(min(it.p0 + slice, npages));
+  const int p1 = min(it.p0 + slice, min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits));
   if (it.row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
-  const int row = it.row0 + L;
-  const bool row_ok = row < it.nrows;
-  const int rr = row_ok ? row : it.row0;
-  const int entry = it.e0 + rr / a.G, head = hk * a.G + rr % a.G, place = it.place + rr / a.G * nsplit;
-  const bool there = entry >= 0 && entry < a.total_readers;
-  const bool store_ok = row_ok && there && place < a.splits * a.total_readers;  // (reader lists longer than announced: no partial)
-  const size_t at = (size_t)place * a.hq + head;
-  int lim = it.len, lim_min = it.len;
-  if constexpr (LIMITS) {
-    lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
-    int lim_max = lim;
-    lim_min = lim;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      lim_max = max(lim_max, __shfl_xor(lim_max, o));
-      lim_min = min(lim_min, __shfl_xor(lim_min, o));
-    }
-    p1 = min(p1, (lim_max + PAGE - 1) / PAGE);
-    if (it.p0 >= p1) {
-      if (store_ok && H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
-      return;
-    }
+  auto rows = [&](int row) __attribute__((always_inline)) {
+    const int entry = it.e0 + row / a.G, head = hk * a.G + row % a.G, place = it.place + row / a.G * nsplit;
+    const bool there = entry >= 0 && entry < a.total_readers;  // (reader lists longer than announced: no partial)
+    const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
+    int lim = it.len;
+    if constexpr (LIMITS) lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
+    return Row{a.q + ((size_t)branch * a.hq + head) * D, (size_t)place * a.hq + head, lim, there && place < a.splits * a.total_readers};
+  };
+  run_item<D, LIMITS, !WIDE>(args.kv, a.seg_pages + it.page_off, it.p0, p1, it.len, hk, a.sc, it.row0, it.nrows, a.part_o, a.part_ml, lane, rows);
+}
+
+constexpr int WHOLE_WAVES = 8;
+
+// Steps over short contexts: a workgroup to a (branch, KV head), whose eight waves share the pages of all lists that the branch reads and put
+// their sums together in LDS: one launch and no partials in memory, which is what such steps consist of otherwise.  Every branch reads
+// the shared pages for itself.  Lane i of a wave knows list i.
+// What bounds it is the chain of loads up to the first page, each of which takes about as long as the arithmetic of a wave: they stand
+// in as few steps as the description allows, none behind a condition.
+template <int D, typename A>
+__device__ __forceinline__ void whole_branch(const A& a, const Q8Cache& kv, const int32_t* pages, int seen, bf16x8 (&q)[D / 16], int r, int hk, float* smem,
+                                             int w, int lane) {
+  const int L = lane & 31, G = a.G, np = (seen + PAGE - 1) / PAGE, units = (np + 1) / 2;
+  const int behind = dag_wave_scan(units), all = __builtin_amdgcn_readlane(behind, 63), front = behind - units;
+  const int u0 = (int)((int64_t)all * w / WHOLE_WAVES), u1 = (int)((int64_t)all * (w + 1) / WHOLE_WAVES);
+  Sums<D> sums;
+  sums.start();
+  sign_q<D>(q, a.sc);
+  for (uint64_t left = __builtin_amdgcn_ballot_w64(max(front, u0) < min(behind, u1)); left; left &= left - 1) {
+    const int i = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(front, i);
+    const int n = __builtin_amdgcn_readlane(np, i), tokens = __builtin_amdgcn_readlane(seen, i);
+    const int32_t* const list = (const int32_t*)dag_readlane((int64_t)(uintptr_t)pages, i);
+    const int p0 = 2 * max(u0 - at, 0), p1 = min(2 * (u1 - at), n);
+    stream_slice<D, false, true>(kv, list, p0, p1, tokens, tokens, tokens, hk, a.sc, lane, q, sums);
   }
-  const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
-  bf16x8 q[D / 16];
-  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-  f32x16 O[D / 32];
-  float m, l;
-  stream_slice<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, lane, q, O, m, l);
-  l += other_half(l);
-  if (store_ok) store_part<D>(a.part_o, a.part_ml, at, O, m, l, H);
-}
-
-// Lists with more than 32 rows of a KV head: a workgroup of eight waves takes up to eight blocks of 32 rows together, so that a page comes
-// from memory once for all of them.  Tiles of four pages (two units of 32 keys) go straight into a ring in LDS, codes as they are (a page is
-// the operand image), and every wave makes its own operands of them.  Up to four blocks: the waves w, w + blocks, .. share a block, its
-// units in turn; five to seven: waves 0 to 3 have one each and the others share what is left, so that the SIMDs have the same
-// to do.  Waves of one block put their sums together in LDS at the end.
-// A wave is a pipeline: in one run of instructions the scores of its next unit and the exponentials of this one, in the next run
-// this one's product with the values and the next one's maximum.  One after the other, the matrix and the vector pipe take turns in both waves of a
-// SIMD, which the tiles keep in step: 1,700 cycles a unit, of which they need 520 and 960 (two groups of 32 over 32768 | 640,
-// 5 heads on one: 93 us, so FIGURE).
-constexpr int WG_WAVES = 8, WG_TILE = 4, WG_RING = 8;
-static_assert(WG_ROWS == 32 * WG_WAVES && WG_MOST_PAGES >= 9 << 4, "");
-constexpr int WG_SCALES = 192;  // pages of a slice: three windows of 64
-constexpr int K_PAD = 128;  // bytes behind a page's keys: the 16 slots of two pages that are read together lie on all banks
-template <int D>
-constexpr int wg_lds_bytes() {  // the ring, or the sums of the waves in its place
-  constexpr int tiles = WG_RING * WG_TILE * (2 * D * PAGE + K_PAD) + WG_SCALES * 8, sums = WG_WAVES * (D / 2 + 2) * 64 * 4;
-  return tiles > sums ? tiles : sums;
-}
-
-struct WgShare {  // of a wave: its block, which of the waves of the block it is, how many there are, the first one, what lies between them
-  int block, sub, parts, first, step;
-  int most;  // largest number of waves of a block
-};
-__device__ __forceinline__ WgShare wg_share(int w, int blocks) {
-  if (blocks > 4) {
-    const int left = blocks - 4, b = (w - 4) % left;
-    const int most = (WG_WAVES - 4 + left - 1) / left;
-    return w < 4 ? WgShare{w, 0, 1, w, 1, most} : WgShare{4 + b, (w - 4) / left, (WG_WAVES - 4 - b + left - 1) / left, 4 + b, left, most};
-  }
-  return WgShare{w % blocks, w / blocks, (WG_WAVES - w % blocks + blocks - 1) / blocks, w % blocks, blocks, (WG_WAVES + blocks - 1) / blocks};
-}
-
-// What a unit needs of LDS in one round trip: the next unit's scales and keys, this one's values.  (Reads and their wait in one block: to the
-// compiler a register that a read has been told to fill holds its value already.)
-__device__ __forceinline__ void lds_unit(u32x2& scales, u32x4 (&k)[4], u32x4 (&v)[4], uint32_t s_at, uint32_t k_at, uint32_t v_at) {
-  asm volatile(
-      "ds_read_b64 %0, %9\n\t"
-      "ds_read_b128 %1, %10\n\tds_read_b128 %2, %10 offset:512\n\tds_read_b128 %3, %10 offset:1024\n\tds_read_b128 %4, %10 offset:1536\n\t"
-      "ds_read_b128 %5, %11\n\tds_read_b128 %6, %11 offset:512\n\tds_read_b128 %7, %11 offset:1024\n\tds_read_b128 %8, %11 offset:1536\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(scales), "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-      : "v"(s_at), "v"(k_at), "v"(v_at));
-}
-__device__ __forceinline__ void lds_unit(u32x2& scales, u32x4 (&k)[2], u32x4 (&v)[2], uint32_t s_at, uint32_t k_at, uint32_t v_at) {
-  asm volatile(
-      "ds_read_b64 %0, %5\n\tds_read_b128 %1, %6\n\tds_read_b128 %2, %6 offset:512\n\t"
-      "ds_read_b128 %3, %7\n\tds_read_b128 %4, %7 offset:512\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(scales), "=&v"(k[0]), "=&v"(k[1]), "=&v"(v[0]), "=&v"(v[1])
-      : "v"(s_at), "v"(k_at), "v"(v_at));
-}
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
-
-template <int D, bool LIMITS>
-__device__ __forceinline__ void wg_stream(const Q8Cache& c, const int32_t* pages, int p0, int p1, int len, int lim, int vlen, int hk, float sc,
-                                          unsigned char* smem, int w, int lane, int sub, int parts, int most_parts, const bf16x8 (&q)[D / 16], f32x16* O, float& m,
-                                          float& l) {
-  constexpr int PB = D * PAGE, KB = PB + K_PAD, PLACE = WG_TILE * (KB + PB);
-  const int L = lane & 31, H = lane >> 5, np = p1 - p0, nt = (np + WG_TILE - 1) / WG_TILE, nu = (np + 1) / 2;
-  static_assert(WG_MOST_PAGES <= WG_SCALES, "");
-  auto page_of = [&](int i) { return min(max(pages[p0 + min(i + lane, np - 1)], 0), c.n_pages - 1); };
-  const int pg0 = page_of(0), pg1 = page_of(64), pg2 = page_of(128);
-  // Scales of the slice's pages to LDS, behind the ring: the waves take turns with the windows of 64.
-  float2* const scales = (float2*)(smem + WG_RING * PLACE);
-  const int mine64 = w < 3 ? w : 0, pgs = mine64 == 0 ? pg0 : mine64 == 1 ? pg1 : pg2;
-  const float ks_here = c.k_scale[(size_t)pgs * c.hkv + hk] * fabsf(sc), vs_here = c.v_scale[(size_t)pgs * c.hkv + hk];
+  const float m = sums.m, l = sums.l + other_half(sums.l);
+  const f32x16(&O)[D / 32] = sums.O;
+  constexpr int ROW = D + 4;
+  float* const ml = smem + WHOLE_WAVES * G * ROW;
+  if (L < G) {
+    if (u0 < u1) {
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) asm volatile("" ::"v"(q[s]));
-  // A wave brings 1 KiB of the keys and of the values of a page of the tile, at dimension 64 of either.
-  constexpr int LOADS = D / 64;
-  const int mine = D == 128 ? w >> 1 : w & 3, at = D == 128 ? (w & 1) * 1024 : 0;
-  auto pick = [](int x, int y, int z, int i) __attribute__((always_inline)) {  // (by value: a choice between captured ones is one of addresses)
-    return __builtin_amdgcn_readlane(i < 64 ? x : i < 128 ? y : z, i & 63);
-  };
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    if (t >= nt) return;
-    const size_t src = ((size_t)pick(pg0, pg1, pg2, min(WG_TILE * t + mine, np - 1)) * c.hkv + hk) * PB + at + lane * 16;
-    unsigned char* const place = smem + t % WG_RING * PLACE;
-    typedef __attribute__((address_space(1))) const void* from_t;
-    typedef __attribute__((address_space(3))) void* to_t;
-    if (D == 128 || w < 4) __builtin_amdgcn_global_load_lds((from_t)(c.k_pool + src), (to_t)(place + mine * KB + at), 16, 0, 0);
-    if (D == 128 || w >= 4) __builtin_amdgcn_global_load_lds((from_t)(c.v_pool + src), (to_t)(place + WG_TILE * KB + mine * PB + at), 16, 0, 0);
-  };
-  // Tile t is there for everybody.  A wave still has to read the values of its last unit, `parts` units in front of its next one: in a tile
-  // up to (parts + 1) / 2 in front of t, which no tile may replace that is asked for up to here.
-  const int ahead = WG_RING - 1 - (most_parts + 1) / 2;
-  auto arrive = [&](int t) __attribute__((always_inline)) {
-    static_assert(WG_RING == 8, "");
-    switch (min(nt - 1 - t, ahead - 1)) {  // tiles under way behind it
-      case 0: wait_vmcnt<0>(); break;
-      case 1: wait_vmcnt<LOADS>(); break;
-      case 2: wait_vmcnt<2 * LOADS>(); break;
-      case 3: wait_vmcnt<3 * LOADS>(); break;
-      case 4: wait_vmcnt<4 * LOADS>(); break;
-      default: wait_vmcnt<5 * LOADS>();
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          *(f32x4*)(smem + (w * G + L) * ROW + 32 * db + 8 * r4 + 4 * (lane >> 5)) = f32x4{O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
     }
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    issue(t + ahead);
-  };
-  for (int t = 0; t < ahead; ++t) issue(t);
-  if (w < 3) scales[64 * w + lane] = make_float2(ks_here, __builtin_amdgcn_logf(vs_here));
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)smem;
-  const uint32_t koff = ring + ((L >> 2) & 1) * KB + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = ring + WG_TILE * KB + H * PB + L * 16;
-  const uint32_t soff = ring + WG_RING * PLACE + H * 8;
-  // What lies behind the slice in its last unit is its last page again, hidden like what lies behind the list.
-  len = min(len, p1 * PAGE);
-  lim = min(lim, p1 * PAGE);
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
-  m = -1e30f;
-  l = 0.f;
-  f32x16 S;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) S[r] = -INFINITY;
-  float ks = 1.f, lv = 0.f;
-  // This wave's unit u, whose scores are in S, and the scores of unit n behind it.  (The first call has no unit u yet: hidden scores, and the
-  // values of unit n.)
-  auto unit = [&](int u, int n) __attribute__((always_inline)) {
-    Block<D> b[1];
-    u32x2 next;
-    const int tu = u >> 1, tn = n >> 1;
-    lds_unit(next, b[0].k, b[0].v, soff + 16 * n, koff + tn % WG_RING * PLACE + (n & 1) * 2 * KB, voff + tu % WG_RING * PLACE + (u & 1) * 2 * PB);
-    const float ref = lv - m;
-    f32x16 T;
-    f32x8 x[2];
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int r = 0; r < 16; ++r) T[r] = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      T = mfma32(codes_to_bf16(b[0].k[s >> 1][2 * (s & 1)], b[0].k[s >> 1][2 * (s & 1) + 1]), q[s], T);
-#pragma unroll
-      for (int r = s * 256 / D; r < (s + 1) * 256 / D; ++r) {
-        x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], ks, ref));
-        sum[r >> 3] += x[r >> 3][r & 7];
-      }
-    }
-    l = fmaf(sum[0] + sum[1], __builtin_amdgcn_exp2f(-lv), l);
-    bf16x8 p[2] = {__builtin_convertvector(x[0], bf16x8), __builtin_convertvector(x[1], bf16x8)};
-    // (done here, beside the scores: the compiler would move it behind the branches below, to where it is used)
-    asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(l));
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {  // vector instructions (0x2), one MFMA (0x8), in turn
-      __builtin_amdgcn_sched_group_barrier(0x002, 4 + 64 / (D / 16), 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    }
-    ks = __uint_as_float(next[0]);
-    lv = __uint_as_float(next[1]);
-    const int key_n = (p0 + 2 * n) * PAGE, key_u = (p0 + 2 * u) * PAGE;
-    if (key_n + 32 > len) {
-      asm volatile("");
-#pragma unroll
-      for (int r = 0; r < 16; ++r) T[r] = key_n + 16 * H + r < lim ? T[r] : -INFINITY;
-    }
-    if (key_u + 32 > vlen) {
-      asm volatile("");
-      clear_behind<D>(b[0], key_u, vlen, H);
-    }
-    if constexpr (LIMITS)
-      if (key_u + 32 > len && len < vlen) hide_not_numbers<D>(b[0], O, key_u, lim, H);
-    float bm = T[0];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(b[0].v[db][2 * i], b[0].v[db][2 * i + 1]), p[i], O[db]);
-#pragma unroll
-    for (int r = 1; r < 16; ++r) bm = fmaxf(bm, T[r]);
-    bm *= ks;
-    bm = fmaxf(bm, other_half(bm));
-    if (__builtin_amdgcn_ballot_w64(bm > m + Q8_TH) != 0) raise<D>(O, m, l, bm);
-    S = T;
-  };
-  int u = -1, n = sub, t = 0;  // (a unit past the last one: nothing but the end of the pipeline)
-  auto reach = [&](int tile) __attribute__((always_inline)) {
-    for (; t <= tile; ++t) arrive(t);
-  };
-#pragma unroll 1
-  for (; n < nu; n += parts) {
-    reach(n >> 1);
-    unit(u < 0 ? n : u, n);
-    u = n;
-  }
-  reach(nt - 1);
-  if (u >= 0) unit(u, u);
-  __syncthreads();
-}
-
-// The rest of an item: sums of the waves of a block put together, a range of dimensions each, and stored.  (The ring is free.)
-template <int D>
-__device__ __forceinline__ void wg_store(float* smem, const WgShare& s, int w, int lane, f32x16* O, float m, float l, bool row_ok, float* part_o,
-                                         float* part_ml, size_t at) {
-  constexpr int DB = D / 32, EACH = (16 * DB + 2) * 64;
-  const int H = lane >> 5;
-  l += other_half(l);
-  if (s.parts > 1) {
-    float* const mine = smem + w * EACH + lane;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mine[(16 * db + r) * 64] = O[db][r];
-    mine[16 * DB * 64] = m;
-    mine[(16 * DB + 1) * 64] = l;
+    if (lane < 32) *(float2*)(ml + (w * G + L) * 2) = make_float2(m, u0 < u1 ? l : 0.f);
   }
   __syncthreads();
-  if (s.parts > 1) {
-    float top = -1e30f;
-    for (int p = 0; p < s.parts; ++p) top = fmaxf(top, smem[(s.first + p * s.step) * EACH + 16 * DB * 64 + lane]);
-    float total = 0.f;
+  for (int x = w * 64 + lane; x < G * (D / 4); x += 64 * WHOLE_WAVES) {
+    const int row = x / (D / 4), c = x % (D / 4) * 4;
+    float top = -1e30f, total = 0.f;
+    for (int i = 0; i < WHOLE_WAVES; ++i) top = fmaxf(top, ml[(i * G + row) * 2]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < WHOLE_WAVES; ++i) {
+      const float2 of = *(const float2*)(ml + (i * G + row) * 2);
+      if (of.y == 0.f) continue;
+      const float wgt = __builtin_amdgcn_exp2f(of.x - top);
+      const f32x4 o = *(const f32x4*)(smem + (i * G + row) * ROW + c);
+      total = fmaf(of.y, wgt, total);
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-      if (db % s.parts == s.sub)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
-    for (int p = 0; p < s.parts; ++p) {
-      const float* const theirs = smem + (s.first + p * s.step) * EACH + lane;
-      const float wgt = __builtin_amdgcn_exp2f(theirs[16 * DB * 64] - top);
-      total = fmaf(theirs[(16 * DB + 1) * 64], wgt, total);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-        if (db % s.parts == s.sub)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) O[db][r] = fmaf(theirs[(16 * db + r) * 64], wgt, O[db][r]);
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(o[e], wgt, acc[e]);
     }
-    m = top;
-    l = total;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    *(u32x2*)(a.out + ((size_t)r * a.hq + hk * G + row) * D + c) = u32x2{dag_pack_bf2(acc[0] * inv, acc[1] * inv), dag_pack_bf2(acc[2] * inv, acc[3] * inv)};
   }
-  if (!row_ok) return;
-  float* const po = part_o + at * D;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-    if (db % s.parts == s.sub)
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4)
-        *(f32x4*)(po + 32 * db + 8 * r4 + 4 * H) = f32x4{O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
-  if (H == 0 && s.sub == 0) *(float2*)(part_ml + at * 2) = make_float2(m, l);
+}
+inline int whole_lds_bytes(int G, int D) { return WHOLE_WAVES * G * (D + 6) * 4; }
+
+template <int D, typename A>
+__device__ __forceinline__ const uint16_t* whole_row(const A& a, int r, int hk, int lane) {
+  return a.q + ((size_t)r * a.hq + hk * a.G + min(lane & 31, a.G - 1)) * D;
 }
 
-// Workgroups with own items, a wave each, then with shared ones.
+// (Arrays that the description does not have are replaced by q, whose memory may be read, by the host.)
 template <int D>
-__global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_wg(Q8DecodeArgs a) {
+__global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole(Q8DecodeArgs a, int n_groups) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 31;
-  f32x16 O[D / 32];
-  float m, l;
-  const int own = gridDim.x - a.items_a;
-  if ((int)blockIdx.x >= own) {
-    int x = blockIdx.x - own;
-    const int hk = x % a.hkv;
-    x /= a.hkv;
-    const int rb = x % a.rb_max;
-    x /= a.rb_max;
-    const int split = x % a.splits_a, g = x / a.splits_a;
-    const int branch0 = a.group_branch_off[g], nrows = (a.group_branch_off[g + 1] - branch0) * a.G, len = a.shared_len[g];
-    const int row0 = rb * WG_ROWS;
-    if (row0 >= nrows) return;
-    const int p0 = split * a.chunk_a, p1 = min(p0 + a.chunk_a, (len + PAGE - 1) / PAGE);
-    const WgShare s = wg_share(w, min((nrows - row0 + 31) / 32, WG_WAVES));
-    const int row = row0 + 32 * s.block + L;
-    const bool row_ok = row < nrows;
-    const int rr = row_ok ? row : row0, branch = min(max(branch0 + rr / a.G, 0), a.n_live - 1), head = hk * a.G + rr % a.G;
-    const size_t at = (size_t)(branch * a.splits_a + split) * a.hq + head;
-    if (p0 >= p1) {
-      if (row_ok && s.sub == 0 && lane < 32) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
-      return;
-    }
-    bf16x8 q[D / 16];
-    load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-    wg_stream<D, false>(a.kv, a.shared_pages + a.shared_page_off[g], p0, p1, len, len, len, hk, a.sc, smem, w, lane, s.sub, s.parts, s.most, q, O, m, l);
-    wg_store<D>((float*)smem, s, w, lane, O, m, l, row_ok, a.part_o, a.part_ml, at);
-    return;
-  }
-  int x = blockIdx.x * WG_WAVES + w;
-  const int hk = x % a.hkv;
-  x /= a.hkv;
-  const int split = x % a.splits_b, branch = x / a.splits_b;
-  if (branch >= a.n_live) return;
-  const int len = a.branch_len[branch], p0 = split * a.chunk_b, p1 = min(p0 + a.chunk_b, (len + PAGE - 1) / PAGE);
-  const size_t at = (size_t)(a.first_own + branch * a.splits_b + split) * a.hq + hk * a.G + min(L, a.G - 1);
-  if (p0 >= p1) {
-    if (lane < a.G) *(float2*)(a.part_ml + at * 2) = make_float2(-1e30f, 0.f);
-    return;
-  }
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hk = blockIdx.x % a.hkv, r = blockIdx.x / a.hkv;
   bf16x8 q[D / 16];
-  load_q<D>(q, a.q + ((size_t)branch * a.hq + hk * a.G + min(L, a.G - 1)) * D, a.sc, lane);
-  stream_slice<D, false>(a.kv, a.branch_pages + a.branch_page_off[branch], p0, p1, len, len, len, hk, a.sc, lane, q, O, m, l);
-  l += other_half(l);
-  if (L < a.G) store_part<D>(a.part_o, a.part_ml, at, O, m, l, lane >> 5);
+  fetch_q<D>(q, whole_row<D>(a, r, hk, lane), lane);
+  const int own_at = a.branch_page_off[r], own_len = a.branch_len[r];
+  int g = -1;  // the group of the branch
+  for (int base = 0; base < n_groups; base += 64) {
+    const int at = min(base + lane, n_groups - 1), from = a.group_branch_off[at], to = a.group_branch_off[at + 1];
+    const uint64_t found = __builtin_amdgcn_ballot_w64((from <= r) & (r < to));
+    if (found) g = min(base + __builtin_ctzll(found), n_groups - 1);
+  }
+  const int shared_at = a.shared_page_off[max(g, 0)], shared_len = a.shared_len[max(g, 0)];
+  const int seen = max(lane == 0 ? (g >= 0 && a.splits_a > 0 ? shared_len : 0) : lane == 1 && a.splits_b > 0 ? own_len : 0, 0);
+  whole_branch<D>(a, a.kv, lane == 0 ? a.shared_pages + shared_at : a.branch_pages + own_at, seen, q, r, hk, (float*)smem, w, lane);
 }
 
-template <int D, bool LIMITS>
-__global__ void __launch_bounds__(64 * WG_WAVES, 2) k_q8_decode_seg_wg(Q8SegArgs args) {
+// Over segments, up to 64 of them: lane i has entry i of the branch.
+template <int D>
+__global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole_seg(Q8SegArgs args) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const SegArgs& a = args.s;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, L = lane & 31;
-  const int hk = blockIdx.x % a.hkv, idx = blockIdx.x / a.hkv;
-  if (idx >= a.totals[0]) return;
-  const SegItem it = a.items[idx];
-  const int slice = (it.nsplit >> 23) & 0x1fe, nsplit = it.nsplit & 0xffffff;
-  const int npages = min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits), p1 = min(it.p0 + slice, npages);  // (a slice has 9 << 4 pages at most)
-  const int row0 = it.row0;
-  if (row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
-  const WgShare s = wg_share(w, min((it.nrows - row0 + 31) / 32, WG_WAVES));
-  const int row = row0 + 32 * s.block + L;
-  const bool row_ok = row < it.nrows;
-  const int rr = row_ok ? row : row0;
-  const int entry = it.e0 + rr / a.G, head = hk * a.G + rr % a.G, place = it.place + rr / a.G * nsplit;
-  const bool there = entry >= 0 && entry < a.total_readers;
-  const bool store_ok = row_ok && there && place < a.splits * a.total_readers;
-  const size_t at = (size_t)place * a.hq + head;
-  int lim = it.len, lim_min = it.len;
-  if constexpr (LIMITS) {
-    lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
-    lim_min = lim;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) lim_min = min(lim_min, __shfl_xor(lim_min, o));
-  }
-  const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hk = blockIdx.x % a.hkv, r = blockIdx.x / a.hkv;
   bf16x8 q[D / 16];
-  load_q<D>(q, a.q + ((size_t)branch * a.hq + head) * D, a.sc, lane);
-  f32x16 O[D / 32];
-  float m, l;
-  wg_stream<D, LIMITS>(args.kv, a.seg_pages + it.page_off, it.p0, p1, lim_min, lim, it.len, hk, a.sc, smem, w, lane, s.sub, s.parts, s.most, q, O, m, l);
-  wg_store<D>((float*)smem, s, w, lane, O, m, l, store_ok, a.part_o, a.part_ml, at);
+  fetch_q<D>(q, whole_row<D>(a, r, hk, lane), lane);
+  const int last = a.seg_reader_off[min(lane, a.n_segments - 1) + 1], end = lane < a.n_segments ? last : INT32_MAX;  // of the entries of segment `lane`
+  const int e0 = a.branch_entry_off[r], n = min(max(a.branch_entry_off[r + 1] - e0, 0), 64);
+  const int entry = n > 0 ? a.branch_entries[e0 + min(lane, n - 1)] : -1;
+  int seg = -1;
+  for (int i = 0; i < n; ++i) {
+    const int e = __builtin_amdgcn_readlane(entry, i), s = __popcll(__builtin_amdgcn_ballot_w64(end <= e));
+    if (lane == i && e >= 0 && e < a.total_readers && s < a.n_segments) seg = s;
+  }
+  const int at = max(seg, 0), page_off = a.seg_page_off[at], len = a.seg_len[at];
+  const int sees = a.seg_reader_len && n > 0 && a.total_readers > 0 ? a.seg_reader_len[min(max(entry, 0), a.total_readers - 1)] : len;
+  whole_branch<D>(a, args.kv, a.seg_pages + page_off, seg >= 0 ? max(min(sees, len), 0) : 0, q, r, hk, (float*)smem, w, lane);
 }
 
 // A wave to a (branch, query head): its partials are put together by their references, 64 at a time a lane each has reference and
@@ -850,15 +635,19 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   a.items_a = p.items_a;
   a.sc = softmax_scale * 1.4426950408889634f;
   hipStream_t stream = (hipStream_t)stream_;
+  if (p.whole) {
+    if (p.items_b == 0) a.branch_page_off = a.branch_len = (const int32_t*)q;
+    if (p.items_a == 0) a.shared_page_off = a.shared_len = (const int32_t*)q;
+    auto* const kernel = D == 128 ? k_q8_whole<128> : k_q8_whole<64>;
+    const int lds = whole_lds_bytes(a.G, D);
+    if (lds > 65536) DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(d->n_live * a.hkv)), dim3(64 * WHOLE_WAVES), lds, stream, a, p.items_a > 0 ? d->n_groups : 0);
+    DAG_LAUNCH_CHECK();
+    return DAG_OK;
+  }
   if (p.items_a + p.items_b > 0) {
-    if (p.wg) {
-      auto* const kernel = D == 128 ? k_q8_decode_wg<128> : k_q8_decode_wg<64>;
-      const int lds = D == 128 ? wg_lds_bytes<128>() : wg_lds_bytes<64>();
-      DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items_a + dag_ceil_div(p.items_b, WG_WAVES))), dim3(64 * WG_WAVES), lds, stream, a);
-    } else {
-      hipLaunchKernelGGL((D == 128 ? k_q8_decode<128> : k_q8_decode<64>), dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
-    }
+    auto* const kernel = p.rb_max > 1 ? (D == 128 ? k_q8_decode<128, true> : k_q8_decode<64, true>) : (D == 128 ? k_q8_decode<128, false> : k_q8_decode<64, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items_a + p.items_b)), dim3(64), 0, stream, a);
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge<128> : k_q8_merge<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, a);
@@ -868,8 +657,7 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
 
 extern "C" size_t dag_decode_segments_q8_workspace_bytes(const dag_decode_seg_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim) {
   SegPlan p;
-  bool wg;
-  return make_q8_seg_plan(desc, hq, hkv, head_dim, &p, &wg) == DAG_OK ? p.bytes : 0;
+  return make_seg_plan(desc, hq, hkv, head_dim, DecodeKnobs{0, 0, 0}, &p) == DAG_OK ? p.bytes : 0;
 }
 
 extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
@@ -879,8 +667,7 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   if (rc != DAG_OK) return rc;
   SegPlan p;
   const int D = kv->head_dim, hkv = kv->hkv;
-  bool wg;
-  rc = make_q8_seg_plan(d, hq, hkv, D, &p, &wg);
+  rc = make_seg_plan(d, hq, hkv, D, DecodeKnobs{0, 0, 0}, &p);
   if (rc != DAG_OK) return rc;
   if (d->n_live == 0) return DAG_OK;
   if (!q || !out || !d->branch_entry_off || !d->branch_entries) return DAG_ERR_NULL;
@@ -917,31 +704,35 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   a.hkv = hkv;
   a.G = hq / hkv;
   a.rb_max = p.rb_max;
-  a.row_shift = wg ? 8 : 5;
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.total_readers = d->total_readers;
   a.fixed = false;
-  a.weight = (float)hkv * (float)D / 128.f;
+  const bool wide = p.rb_max > 1;
+  a.weight = (float)hkv * (float)D / 128.f * (wide ? Q8_SEG_WIDE : 1.f);
   const int64_t most_pages = (int64_t)d->n_segments * p.rb_max * d->max_seg_pages * hkv * D;
   a.few = p.chunk == 8 && most_pages < (d->max_seg_pages <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) * 128;
   a.sc = softmax_scale * 1.4426950408889634f;
   hipStream_t stream = (hipStream_t)stream_;
+  if (p.items > 0 && q8_whole_segments(d, hkv, D)) {
+    auto* const kernel = D == 128 ? k_q8_whole_seg<128> : k_q8_whole_seg<64>;
+    const int lds = whole_lds_bytes(a.G, D);
+    if (lds > 65536) DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(d->n_live * hkv)), dim3(64 * WHOLE_WAVES), lds, stream, args);
+    DAG_LAUNCH_CHECK();
+    return DAG_OK;
+  }
   if (p.items > 0) {
     const int64_t waves = dag_ceil_div(d->n_segments, 64);
     hipLaunchKernelGGL(k_seg_plan, dim3(1), dim3((unsigned)(waves * 64 < PLAN_THREADS ? waves * 64 : PLAN_THREADS)), 0, stream, a);
     DAG_LAUNCH_CHECK();
-    if (wg) {
-      auto* const kernel = a.seg_reader_len ? (D == 128 ? k_q8_decode_seg_wg<128, true> : k_q8_decode_seg_wg<64, true>)
-                                            : (D == 128 ? k_q8_decode_seg_wg<128, false> : k_q8_decode_seg_wg<64, false>);
-      const int lds = D == 128 ? wg_lds_bytes<128>() : wg_lds_bytes<64>();
-      DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64 * WG_WAVES), lds, stream, args);
-    } else {
-      auto* const kernel = a.seg_reader_len ? (D == 128 ? k_q8_decode_seg<128, true> : k_q8_decode_seg<64, true>)
-                                            : (D == 128 ? k_q8_decode_seg<128, false> : k_q8_decode_seg<64, false>);
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
-    }
+    auto pick = [&](auto d_c) {
+      constexpr int N = decltype(d_c)::value;
+      return a.seg_reader_len ? (wide ? k_q8_decode_seg<N, true, true> : k_q8_decode_seg<N, false, true>)
+                              : (wide ? k_q8_decode_seg<N, true, false> : k_q8_decode_seg<N, false, false>);
+    };
+    auto* const kernel = D == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.items * hkv)), dim3(64), 0, stream, args);
     DAG_LAUNCH_CHECK();
   }
   hipLaunchKernelGGL(D == 128 ? k_q8_merge_seg<128> : k_q8_merge_seg<64>, dim3((unsigned)(d->n_live * hq)), dim3(64), 0, stream, args);

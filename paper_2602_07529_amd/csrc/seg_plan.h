@@ -8,7 +8,7 @@ namespace {
 
 // Decode over lists of KV segments: a segment is a page list with a token count and the set of
 // live branches that read it; a branch's context is the union of the segments it reads.
-struct SegItem {  // one work item: a slice of a segment's pages against one block of its readers' rows
+struct SegItem {  // one work item: a slice of a segment's pages against one 32-row block of its readers' rows
   int32_t page_off, len, e0, nrows, row0;
   int32_t p0, place;  // first page of the slice; place of its partial of reader e0
   int32_t nsplit;     // slices of the segment, pages of a slice / 2 in the highest eight bits (unless SegArgs::fixed)
@@ -34,8 +34,7 @@ struct SegArgs {
   int32_t* entry_first;  // [total_readers] place of the first partial of each reader-list entry (the next one's: behind its last)
   int item_cap;
   int n_segments, n_live, hq, hkv, G;
-  int rb_max;      // row blocks per (segment, kv head)
-  int row_shift;   // log2 of the rows of one
+  int rb_max;      // 32-row blocks per (segment, kv head)
   int chunk, splits, total_readers;  // pages of a slice and slices of a segment that the workspace has room for
   bool fixed;      // slices of `chunk` pages, whatever there is to read
   bool few;        // by the host's bounds the slices have eight pages
@@ -67,7 +66,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_seg_plan(SegArgs a) {
       g.e0 = a.seg_reader_off[s];
       g.nr = max(a.seg_reader_off[s + 1] - g.e0, 0);
       g.npages = min((g.len + PAGE - 1) / PAGE, a.chunk * a.splits);
-      g.rbs = min((g.nr * a.G + (1 << a.row_shift) - 1) >> a.row_shift, a.rb_max);
+      g.rbs = min((g.nr * a.G + 31) / 32, a.rb_max);
     }
     return g;
   };
@@ -173,7 +172,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_seg_plan(SegArgs a) {
       const int page_off = a.seg_page_off[s], code = a.fixed ? nsp : nsp | slice << 23;
       for (int sp = nsp - 1; sp >= 0; --sp)
         for (int rb = 0; rb < g.rbs; ++rb, ++at)
-          if (at < a.item_cap) a.items[at] = SegItem{page_off, g.len, g.e0, g.nr * a.G, rb << a.row_shift, sp * slice, first + sp, code};
+          if (at < a.item_cap) a.items[at] = SegItem{page_off, g.len, g.e0, g.nr * a.G, rb * 32, sp * slice, first + sp, code};
       for (int e = 0; e < g.nr; ++e) {
         if (g.e0 + e >= 0 && g.e0 + e < a.total_readers) a.entry_first[g.e0 + e] = first + e * nsp;
         if (g.e0 + e == a.total_readers - 1) a.totals[1] = first + (e + 1) * nsp;
