@@ -436,7 +436,8 @@ typedef struct {
   int32_t* free_pages;       /* [n_pages]                                                        */
 } dag_kv_rows_t;
 
-/* Bytes of DEVICE workspace (4-byte aligned) of the two calls below; they may share one if they are on one stream. */
+/* Bytes of DEVICE workspace (4-byte aligned) of the two calls below.  Its first four bytes have to be zero before its first use and are
+ * zero again behind every call.  The two may share one, but calls that overlap may not. */
 size_t dag_kv_tables_workspace_bytes(int32_t n_rows);
 
 /* Rows with ended[r] != 0 give their pages back: free_pages[*free_count ..] gets them in the order of rows and tokens,

@@ -563,7 +563,7 @@ class KvRows:
         _device_arrays({"table": table, "free_pages": free_pages})
         n_rows, width = table.shape
         self.c = dag_kv_rows_t(n_rows, PAGE, width, free_pages.numel(), table.data_ptr(), free_pages.data_ptr())
-        self.workspace = torch.empty(int(lib().dag_kv_tables_workspace_bytes(n_rows)), dtype=torch.uint8, device=table.device)
+        self.workspace = torch.zeros(int(lib().dag_kv_tables_workspace_bytes(n_rows)), dtype=torch.uint8, device=table.device)
 
 
 def _at(x):
