@@ -411,14 +411,14 @@ int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int
  * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), and a branch
  * that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
  * never followed; the host bounds are trusted.  softmax_scale may be of either sign.  Sums, maxima and partial results are
- * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches); the call
+ * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches; one for short contexts); the call
  * allocates nothing and does not synchronise; calls that overlap need a workspace each. */
 size_t dag_decode_q8_workspace_bytes(const dag_decode_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);
 int dag_attn_decode_q8(const dag_decode_desc_t* desc, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
                        float softmax_scale, void* ws, size_t ws_bytes, void* stream);
 
 /* dag_attn_decode_segments over an 8-bit cache: same description (seg_reader_len included: the incremental prefill of a few new
- * tokens), otherwise as dag_attn_decode_q8 (three launches). */
+ * tokens), otherwise as dag_attn_decode_q8 (three launches; one for short contexts). */
 size_t dag_decode_segments_q8_workspace_bytes(const dag_decode_seg_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);
 int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* desc, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
                                 float softmax_scale, void* ws, size_t ws_bytes, void* stream);
