@@ -442,7 +442,7 @@ size_t dag_kv_tables_workspace_bytes(int32_t n_rows);
 
 /* Rows with ended[r] != 0 give their pages back: free_pages[*free_count ..] gets them in the order of rows and tokens,
  * row_len_out is 0 for them and row_len for the others, free_count_out the new number of free pages.  row_len_out may be row_len and
- * free_count_out may be free_count. */
+ * free_count_out may be free_count; no other output may overlap an input. */
 int dag_kv_release(const dag_kv_rows_t* rows, const int32_t* ended, const int32_t* row_len, int32_t* row_len_out,
                    const int32_t* free_count, int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream);
 
@@ -458,7 +458,7 @@ int dag_kv_release(const dag_kv_rows_t* rows, const int32_t* ended, const int32_
  * ones included that would fit their line) are more than are free: its slots are -1 and its length stays.  Rows that need no page are never
  * refused for want of pages.  max_new and max_pages are HOST values, the lengths of the arrays; entries past them are dropped.
  * The sums of new_len and of the listed pages have to fit an int32.  Negative lengths count as 0.  row_len_out may be row_len and
- * free_count_out may be free_count.  Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE,
+ * free_count_out may be free_count; no other output may overlap an input.  Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE,
  * DAG_ERR_HIP. */
 int dag_kv_tables(const dag_kv_rows_t* rows, const int32_t* new_len, const int32_t* row_len, int32_t* row_len_out,
                   const int32_t* free_count, int32_t* free_count_out, int32_t* new_off, int32_t* slots, int64_t max_new,
