@@ -380,7 +380,7 @@ int dag_attn_prefill_paged(const dag_paged_prefill_desc_t* desc, const void* q, 
  * Storage formats (page size 16), P = n_pages:
  *   K pool [P][hkv][head_dim/16][16][16]  element (page, h, slot, d) at [page][h][d/16][slot][d%16]
  *   V pool [P][hkv][head_dim][16]         element (page, h, slot, d) at [page][h][d][slot]
- *   scales [P][hkv], finite and positive for every page that holds tokens
+ *   scales [P][hkv], finite and at least 2^-100 for every page that holds tokens
  * The struct lives on the HOST, its pointers are DEVICE memory (pools 16-byte aligned). */
 typedef struct {
   void* k_pool;
@@ -408,9 +408,9 @@ int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int
 
 /* dag_attn_decode over an 8-bit cache: same description, same attention of every live branch's query over (shared context, own
  * tokens).  q / out [n_live][hq][head_dim] bf16 DEVICE, q already rotated; hq a multiple of kv->hkv, hq / hkv <= 32.
- * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), and a branch
- * that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
- * never followed; the host bounds are trusted.  softmax_scale may be of either sign.  Sums, maxima and partial results are
+ * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), otherwise every branch is in a
+ * group; a branch that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
+ * never followed; the host bounds are trusted.  softmax_scale may be of either sign, or zero.  Sums, maxima and partial results are
  * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches; one for short contexts); the call
  * allocates nothing and does not synchronise; calls that overlap need a workspace each. */
 size_t dag_decode_q8_workspace_bytes(const dag_decode_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);

@@ -256,7 +256,8 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
 
 // Decode over an 8-bit cache: slices of about one length, so that there are Q8_WAVES of them and all run at once (what was measured
 // stands at stream_slice; more of them where groups have more than 32 rows, 88 -> 86 us for two groups of 32 over 32768 | 640), no shorter than
-// Q8_LEAST_PAGES.
+// Q8_LEAST_PAGES.  Dimension 64, with half the bytes on their way: 16 groups of 8 over 16384 | 1024 tokens 72.2 us, with 2048 waves 75.4, with 4096 83.2,
+// with four pages more on their way 72.6.
 constexpr int Q8_WAVES = 1536, Q8_WIDE_WAVES = 1920, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
 // Segments: slices by the rules of the bf16 cache, but for more than 32 rows, whose pages weigh less: shorter slices (nine new tokens of 48 nodes 95 -> 69 us).
 constexpr float Q8_SEG_WIDE = 0.5f;

@@ -218,7 +218,7 @@ struct Window {
     lv = c.v_scale[(size_t)pg * c.hkv + hk];
   }
   __device__ __forceinline__ void have(float sc) {
-    ks *= fabsf(sc);
+    ks = fmaxf(ks * fabsf(sc), 1.2e-38f);  // (not zero: hidden keys have scores of minus infinity)
     lv = __builtin_amdgcn_logf(lv);
     asm volatile("" ::"v"(ks), "v"(lv));  // (arrived: a wait for them later would also wait for the blocks in flight)
   }

@@ -118,3 +118,14 @@ def test_tables_of_graphs_that_share_rows(n_rows):
         outs.append([o[k] for k in ("l1", "c1", "l2", "c2", "off", "page_off", "refused")])
     replay_in_turn(calls, outs)
     assert int(rows.workspace[:4].sum()) == 0
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-30])
+@pytest.mark.parametrize("spare", [0, 400])
+def test_a_softmax_scale_of_nothing_gives_the_mean(scale, spare):
+    c = Cascade([(70, [20, 33]), (0, [0, 1])], 8, 2, 128, 27, spare=spare)
+    s = Segments(4, [(200, [(r, 200 - 50 * r) for r in range(4)]), (9, [(2, 9)])], 8, 2, 64, 28, spare=spare)
+    for x in (c, s):
+        x.call(softmax_scale=scale)
+        torch.cuda.synchronize()
+        check(x.out, x.q, x.contexts, x.cache, scale)
