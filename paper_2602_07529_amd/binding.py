@@ -314,11 +314,22 @@ def _int32(x, name):
         raise TypeError("%s has to be a contiguous int32 tensor" % name)
 
 
-def _device_arrays(arrays):
+def _device_arrays(arrays, least=()):
+    """int32 tensors on one device, `least` elements long."""
+    least, devices = dict(least), set()
     for name, x in arrays.items():
         if x is not None:
             _int32(x, name)
+            if x.numel() < least.get(name, 0):
+                raise ValueError("%s has %d elements, not %d" % (name, x.numel(), least[name]))
+            devices.add(x.device)
+    _one_device(devices)
     return arrays
+
+
+def _one_device(devices):
+    if len(devices) > 1:
+        raise ValueError("tensors are on %s" % ", ".join(sorted(map(str, devices))))
 
 
 class DecodeDesc:
@@ -352,7 +363,9 @@ class DecodeDesc:
         self = cls.__new__(cls)
         arrays = (group_branch_off, shared_page_off, shared_pages, shared_len, branch_page_off, branch_pages, branch_len,
                   branch_pos)
-        self.t = _device_arrays(dict(zip(_DECODE_ARRAYS, arrays)))
+        self.t = _device_arrays(dict(zip(_DECODE_ARRAYS, arrays)), dict(
+            group_branch_off=n_groups + 1, shared_page_off=n_groups + 1, shared_len=n_groups, branch_page_off=n_live + 1,
+            branch_len=n_live, branch_pos=n_live) if n_groups else dict(branch_page_off=n_live + 1, branch_len=n_live, branch_pos=n_live))
         self.c = dag_decode_desc_t(n_groups, n_live, PAGE, max_shared_pages, max_branch_pages, max_group_size,
                                    *[0 if x is None else x.data_ptr() for x in arrays])
         return self
@@ -421,7 +434,9 @@ class SegDecodeDesc:
         self = cls.__new__(cls)
         arrays = (seg_page_off, seg_pages, seg_len, seg_reader_off, seg_readers, branch_entry_off, branch_entries,
                   seg_reader_len)
-        self.t = _device_arrays(dict(zip(_SEG_ARRAYS + ("seg_reader_len",), arrays)))
+        self.t = _device_arrays(dict(zip(_SEG_ARRAYS + ("seg_reader_len",), arrays)), dict(
+            seg_page_off=n_segments + 1, seg_len=n_segments, seg_reader_off=n_segments + 1, branch_entry_off=n_live + 1,
+            seg_reader_len=total_readers))
         self.c = dag_decode_seg_desc_t(n_live, n_segments, PAGE, max_seg_pages, max_readers, total_readers,
                                        *[0 if x is None else x.data_ptr() for x in arrays])
         return self
@@ -492,6 +507,7 @@ class KvCacheQ8:
                       (v_scale, torch.float32)):
             if x.dtype != dt or not x.is_contiguous():
                 raise TypeError("pools are contiguous float8_e4m3fn, scales contiguous float32")
+        _one_device({k_pool.device, v_pool.device, k_scale.device, v_scale.device})
         self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
         self.hkv, self.head_dim = hkv, d
         self.c = dag_kv_q8_t(k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, hkv, d)
@@ -542,8 +558,9 @@ def _decode_q8(call, desc, q, cache, out, workspace, softmax_scale):
         raise ValueError("q and out are [n_live][heads][head_dim]")
     if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous():
         raise TypeError("q and out are contiguous bfloat16")
+    lens = desc.t["branch_len" if type(desc) is DecodeDesc else "seg_len"]  # (its arrays are on one device)
     _check(call(desc.c, cache.ref, q.data_ptr(), out.data_ptr(), hq, d ** -0.5 if softmax_scale is None else softmax_scale,
-                workspace.data_ptr(), workspace.numel(), _here(q, out, cache.k_pool, workspace)))
+                workspace.data_ptr(), workspace.numel(), _here(q, out, cache.k_pool, workspace, q if lens is None else lens)))
 
 
 def dag_attn_decode_q8(ddesc, q, cache, out, workspace, softmax_scale=None):

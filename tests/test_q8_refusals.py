@@ -137,3 +137,26 @@ def test_the_binding_looks_at_shapes_types_and_devices():
             B.dag_kv_tables(rows, *bad)
     with pytest.raises(ValueError):
         B.dag_kv_tables(rows, n, n, n, one, one, off, n, pos=one)
+
+
+def test_descriptions_whose_arrays_are_too_short_or_on_several_devices():
+    a = lambda n, device="cpu": torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
+    good = dict(group_branch_off=a(3), shared_page_off=a(3), shared_pages=a(1), shared_len=a(2), branch_page_off=a(5), branch_pages=a(1), branch_len=a(4))
+    B.DecodeDesc.on_device(2, 4, 1, 1, 2, **good)
+    B.DecodeDesc.on_device(0, 4, 0, 1, 0, **{k: v for k, v in good.items() if k[:6] == "branch"})
+    for name in ("group_branch_off", "shared_page_off", "shared_len", "branch_page_off", "branch_len"):
+        for bad in (a(good[name].numel() - 1), good[name].to("meta")):
+            with pytest.raises(ValueError):
+                B.DecodeDesc.on_device(2, 4, 1, 1, 2, **{**good, name: bad})
+    good = dict(seg_page_off=a(4), seg_pages=a(1), seg_len=a(3), seg_reader_off=a(4), seg_readers=a(5), branch_entry_off=a(3), branch_entries=a(5),
+                seg_reader_len=a(5))
+    B.SegDecodeDesc.on_device(2, 3, 1, 2, 5, **good)
+    for name in ("seg_page_off", "seg_len", "seg_reader_off", "branch_entry_off", "seg_reader_len"):
+        for bad in (a(good[name].numel() - 1), good[name].to("meta")):
+            with pytest.raises(ValueError):
+                B.SegDecodeDesc.on_device(2, 3, 1, 2, 5, **{**good, name: bad})
+    e4 = torch.zeros(4, 2, 4, 16, 16).to(torch.float8_e4m3fn), torch.zeros(4, 2, 64, 16).to(torch.float8_e4m3fn)
+    with pytest.raises(ValueError):
+        B.KvCacheQ8(*e4, torch.ones(4, 2), torch.ones(4, 2, device="meta"))
+    with pytest.raises(ValueError):
+        B.KvRows(a((3, 5)), a(7, "meta"))
