@@ -59,26 +59,38 @@ __device__ __forceinline__ void block_scan(int64_t (&x)[N], int64_t (&all)[N]) {
   __syncthreads();
 }
 
+// Sums of many rows by one workgroup, PER_THREAD of them to a thread, as a turn is loads and scans behind one another (release and tables of 4096
+// rows, replayed: 29.6 us with one to a thread, 25.1 with four).
+constexpr int PER_THREAD = 4;
+
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_release_rows(TableArgs a) {
-  const int width = a.rows.max_row_pages;
+  const int width = a.rows.max_row_pages, n_rows = a.rows.n_rows;
   const int64_t count = min(max(a.free_count[0], 0), a.rows.n_pages);
   int64_t front = 0;
-  for (int base = 0; base < a.rows.n_rows; base += blockDim.x) {
-    const int r = base + threadIdx.x;
-    int64_t gone[1] = {0}, all[1];
-    int len = 0;
-    bool end = false;
-    if (r < a.rows.n_rows) {
-      len = max(a.row_len[r], 0);
-      end = a.ended[r] != 0;
-      if (end) gone[0] = min(pages_of(len), (int64_t)width);
+  for (int64_t base = 0; base < n_rows; base += PER_THREAD * ROW_THREADS) {
+    const int64_t r0 = base + PER_THREAD * threadIdx.x;
+    int len[PER_THREAD];
+    bool end[PER_THREAD];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      const int64_t r = min(r0 + i, (int64_t)n_rows - 1);
+      len[i] = max(a.row_len[r], 0);
+      end[i] = r0 + i < n_rows && a.ended[r] != 0;
     }
-    const int n = (int)gone[0];
+    int64_t gone[1] = {0}, all[1];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) gone[0] += end[i] ? min(pages_of(len[i]), (int64_t)width) : 0;
     block_scan(gone, all);
-    if (r < a.rows.n_rows) {
-      a.first[r] = (int32_t)(count + front + gone[0]);
-      a.held[r] = n;
-      a.row_len_out[r] = end ? 0 : len;
+    int64_t at = count + front + gone[0];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      const int64_t r = r0 + i;
+      if (r >= n_rows) break;
+      const int64_t n = end[i] ? min(pages_of(len[i]), (int64_t)width) : 0;
+      a.first[r] = (int32_t)at;
+      a.held[r] = (int32_t)n;
+      a.row_len_out[r] = end[i] ? 0 : len[i];
+      at += n;
     }
     front += all[0];
   }
@@ -93,34 +105,55 @@ __global__ void __launch_bounds__(LIST_THREADS) k_kv_release_pages(TableArgs a) 
 }
 
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_table_rows(TableArgs a) {
-  const int width = a.rows.max_row_pages;
+  const int width = a.rows.max_row_pages, n_rows = a.rows.n_rows;
   const int64_t count = min(max(a.free_count[0], 0), a.rows.n_pages);
   int64_t front_need = 0, front_new = 0, front_pages = 0, taken = 0, refused = 0;
-  for (int base = 0; base < a.rows.n_rows; base += blockDim.x) {
-    const int r = base + threadIdx.x;
-    const bool there = r < a.rows.n_rows;
-    int64_t len = 0, want = 0, need = 0;
-    bool fits = true;
-    if (there) {
-      len = max(a.row_len[r], 0);
-      want = max(a.new_len[r], 0);
-      fits = len + want <= (int64_t)width * PAGE;
-      if (fits) need = pages_of(len + want) - pages_of(len);
+  for (int64_t base = 0; base < n_rows; base += PER_THREAD * ROW_THREADS) {
+    const int64_t r0 = base + PER_THREAD * threadIdx.x;
+    int64_t len[PER_THREAD], want[PER_THREAD], need[PER_THREAD];
+    bool fits[PER_THREAD];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      const int64_t r = min(r0 + i, (int64_t)n_rows - 1);
+      const int x = a.row_len[r], y = a.new_len[r];
+      const bool there = r0 + i < n_rows;
+      len[i] = there ? max(x, 0) : 0;
+      want[i] = there ? max(y, 0) : 0;
     }
-    int64_t x[2] = {need, want}, all[2];
+    int64_t x[2] = {0, 0}, all[2];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      fits[i] = len[i] + want[i] <= (int64_t)width * PAGE;
+      need[i] = fits[i] ? pages_of(len[i] + want[i]) - pages_of(len[i]) : 0;
+      x[0] += need[i];
+      x[1] += want[i];
+    }
     block_scan(x, all);
-    const int64_t start = front_need + x[0];
-    const bool ok = fits && (need == 0 || start + need <= count);
-    const int64_t now = len + (ok ? want : 0), listed = there ? min(pages_of(now), (int64_t)width) : 0;
-    int64_t y[3] = {listed, there && !ok && want > 0 ? 1 : 0, ok ? need : 0}, sums[3];
+    int64_t y[3] = {0, 0, 0}, sums[3], start = front_need + x[0];
+    int32_t first[PER_THREAD], now[PER_THREAD];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      const bool ok = fits[i] && (need[i] == 0 || start + need[i] <= count);
+      first[i] = !ok ? -1 : need[i] == 0 ? 0 : (int32_t)(count - 1 - start);
+      now[i] = (int32_t)(len[i] + (ok ? want[i] : 0));
+      start += need[i];
+      y[0] += min(pages_of(now[i]), (int64_t)width);
+      y[1] += !ok && want[i] > 0 ? 1 : 0;
+      y[2] += ok ? need[i] : 0;
+    }
     block_scan(y, sums);
-    if (there) {
-      a.row_len_out[r] = (int32_t)now;
-      a.new_off[r] = (int32_t)(front_new + x[1]);
-      if (a.page_off) a.page_off[r] = (int32_t)(front_pages + y[0]);
-      a.first[r] = ok ? (int32_t)(count - 1 - start) : -1;
-      if (ok && need == 0) a.first[r] = 0;
-      a.held[r] = (int32_t)len;
+    int64_t at = front_new + x[1], page_at = front_pages + y[0];
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; ++i) {
+      const int64_t r = r0 + i;
+      if (r >= n_rows) break;
+      a.row_len_out[r] = now[i];
+      a.new_off[r] = (int32_t)at;
+      if (a.page_off) a.page_off[r] = (int32_t)page_at;
+      a.first[r] = first[i];
+      a.held[r] = (int32_t)len[i];
+      at += want[i];
+      page_at += min(pages_of(now[i]), (int64_t)width);
     }
     front_need += all[0];
     front_new += all[1];
@@ -129,8 +162,8 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_table_rows(TableArgs a) {
     taken += sums[2];
   }
   if (threadIdx.x == 0) {
-    a.new_off[a.rows.n_rows] = (int32_t)front_new;
-    if (a.page_off) a.page_off[a.rows.n_rows] = (int32_t)front_pages;
+    a.new_off[n_rows] = (int32_t)front_new;
+    if (a.page_off) a.page_off[n_rows] = (int32_t)front_pages;
     if (a.refused) a.refused[0] = (int32_t)refused;
     a.free_count_out[0] = (int32_t)(count - taken);
   }
@@ -187,7 +220,7 @@ __device__ __forceinline__ bool comes_last(uint32_t* ticket) {
 
 // All in one launch, per_row waves to a row.  Release and tables together, replayed from a graph, one launch each against two:
 // 128 rows of one new token 10.5 us against 11.3, 256 prompts of 4099 tokens 15.4 / 16.7, 1024 rows of 1 12.0 / 12.6, 4096 rows (scans of four
-// turns in every workgroup) 30.0 / 29.7; called one by one, where a launch costs the host 3.4 us, 128 rows 16.2 / 20.7.
+// turns in every workgroup) 30.0 / 25.1; called one by one, where a launch costs the host 3.4 us, 128 rows 16.2 / 20.7.
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_tables_one(TableArgs a, int per_row) {
   struct Mine {
     int64_t t0, p0;

@@ -74,7 +74,7 @@ class Book:
 @pytest.mark.parametrize("n_rows,old,new", [(1, 0, 1), (1, 15, 1), (1, 16, 1), (1, 5, 3000), (7, 100, 40), (64, 300, 1), (200, 31, 2), (1024, 90, 1),
                                             (1025, 40, 20), (2500, 20, 3), (1024, 60, 1), (1025, 60, 1),
                                             (1024, 1500, 900), (257, 1500, 900),
-                                            (5000, 40, 3), (3, 5, 40000), (40, 3000, 1), (30, 9000, 700)])
+                                            (5000, 40, 3), (4096, 40, 3), (4097, 40, 20), (9000, 20, 3), (3, 5, 40000), (40, 3000, 1), (30, 9000, 700)])
 def test_rows_grow_and_end(in_place, n_rows, old, new):
     rng = np.random.default_rng(n_rows + new)
     lens = rng.integers(0, old + 1, n_rows)
