@@ -129,3 +129,35 @@ def test_a_softmax_scale_of_nothing_gives_the_mean(scale, spare):
         x.call(softmax_scale=scale)
         torch.cuda.synchronize()
         check(x.out, x.q, x.contexts, x.cache, scale)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (16, 2, 64)])
+def test_one_branch_over_a_very_long_context(hq, hkv, d):
+    """Hundreds of partial results to a row, more than a merging wave takes at a time."""
+    c = Cascade([(60001, [5])], hq, hkv, d, 29)
+    assert q8_rules.plan(c.desc.c, hq, hkv, d).splits_a > 64
+    s = Segments(2, [(60001, [(0, 60001), (1, 33333)]), (5, [(0, 5)])], hq, hkv, d, 30)
+    for x in (c, s):
+        x.call()
+        torch.cuda.synchronize()
+        check(x.out, x.q, x.contexts, x.cache)
+
+
+def test_calls_at_once_on_two_streams_with_a_workspace_each():
+    a = Cascade([(4000, [300] * 6)], 8, 2, 128, 31)
+    b = Segments(6, [(3000, [(r, 3000) for r in range(6)])] + [(100, [(r, 100)]) for r in range(6)], 8, 2, 128, 32, limits=False)
+    a.call()
+    b.call()
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(4):
+        a.out.zero_()
+        b.out.zero_()
+        torch.cuda.synchronize()
+        for stream, x in zip(streams, (a, b)):
+            with torch.cuda.stream(stream):
+                for _ in range(3):
+                    x.call()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
