@@ -158,7 +158,8 @@ constexpr float Q8_TH = 3.f;
 
 // A block: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
 // lv: log2 of its value scale.  A lane's 16 scores are of one page, so their largest is found among the plain products, one
-// multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.
+// multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.  (The exponential's results
+// reach down to 2^-149: on a page of zeros, scale 2^-100, a key loses at most 2^-50 of the largest in the sum, 2^31 of them 2^-19.)
 // key0: first key of the block; keys from `lim` on are hidden from the lane's row; len: the smallest lim of the wave; slots from vlen on hold
 // no token.  A wave by itself takes 1,005 cycles for a block at head dimension 128, two waves of a SIMD 512 each, as long as the 16 MFMAs.
 template <int D, bool LIMITS>

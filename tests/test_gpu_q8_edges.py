@@ -1,0 +1,64 @@
+"""GPU: attention over the 8-bit cache at the edges of what the descriptions, scales and lengths may be (tolerances: q8_cases, or beside the
+test)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_07529_amd import binding as B
+from tests.gpu_util import DEV
+from tests.q8_cases import Cascade, Segments, check, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def _call(desc, cache, q, **kw):
+    form = "decode" if type(desc) is B.DecodeDesc else "decode_segments"
+    out = torch.full_like(q, float("nan"))
+    ws = torch.empty(max(256, getattr(B, "dag_%s_q8_workspace_bytes" % form)(desc, cache, q.shape[1])), dtype=torch.uint8, device=DEV)
+    getattr(B, "dag_attn_%s_q8" % form)(desc, q, cache, out, ws, **kw)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", ["cascade", "segments", "limits"])
+def test_keys_on_pages_of_zeros_count_in_the_sum(form, d):
+    """2^24 keys of one page that holds zeros (value scale 2^-100), each 2^-28 of the one key that has a value: out = v / (1 + 2^-4).
+
+    The scores are 28 and 0 but for their rounding (28 * 2^-23), the sums take 128 blocks to a slice and a tree of slices: far below the result's
+    rounding to bf16, 2^-8."""
+    n, hq = 1 << 24, 4
+    cache = B.KvCacheQ8.empty(2, 1, d, DEV)
+    cache.k_pool[1, 0, 0, 0, 0] = 28.0
+    v = torch.randn(d, generator=torch.Generator().manual_seed(1)).to(torch.float8_e4m3fn)
+    cache.v_pool.view(torch.uint8)[1, 0, :, 0] = v.view(torch.uint8).to(DEV)
+    cache.v_scale[0] = 2.0 ** -100
+    q = torch.zeros((1, hq, d), dtype=torch.bfloat16, device=DEV)
+    q[:, :, 0] = 1.0
+    far, most = torch.zeros(n // 16 + 1, dtype=torch.int32, device=DEV), n // 16
+    if form == "cascade":
+        desc = B.DecodeDesc.on_device(1, 1, most, 1, 1, ints([0, 1]), ints([0, most]), far, ints([n]), ints([0, 1]), ints([1]), ints([1]), ints([0]))
+    else:
+        far[-1] = 1
+        desc = B.SegDecodeDesc.on_device(1, 2, most, 1, 2, ints([0, most, most + 1]), far, ints([n, 1]), ints([0, 1, 2]), ints([0, 0]), ints([0, 2]),
+                                         ints([0, 1]), ints([n, 1]) if form == "limits" else None)
+    out = _call(desc, cache, q, softmax_scale=math.log(2.0))
+    want = v.double() / (1 + 2.0 ** -4)
+    assert ((out[0].double().cpu() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -14)).all()
+
+
+@pytest.mark.parametrize("spare", [0, 400])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 1, 64)])
+def test_value_scales_from_the_smallest_to_large_ones(hq, hkv, d, spare):
+    scale = 2.0 ** torch.tensor([-100.0, 110.0, -70.0, -64.0, 64.0, 90.0, 0.0])
+    c = Cascade([(160, [40, 18]), (300, [5])], hq, hkv, d, 41, spare=spare)
+    s = Segments(3, [(160, [(0, 160), (1, 100)]), (77, [(2, 77), (1, 9)]), (40, [(0, 40)])], hq, hkv, d, 42, spare=spare)
+    for x in (c, s):
+        n = x.cache.v_scale.numel()
+        for turn in range(2):  # (another page has the largest values, and no page large ones)
+            x.cache.v_scale.copy_(scale[(torch.arange(n) + 3 * turn) % 7].clamp(max=2.0 ** (110 - 170 * turn)).reshape(x.cache.v_scale.shape))
+            x.call()
+            torch.cuda.synchronize()
+            check(x.out, x.q, x.contexts, x.cache)
