@@ -174,6 +174,10 @@ __device__ __forceinline__ void compute_block(Block<D>& b, const bf16x8 (&q)[D /
     asm volatile("");  // (a branch: the compiler would compare and select in every block)
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[r] = key0 + 16 * H + r < lim ? S[r] : -INFINITY;
+    if (key0 + 16 * H >= lim) {  // (scales of a page that the row sees nothing of)
+      ks = 1.f;
+      lv = 0.f;
+    }
   }
   float bm = S[0];
 #pragma unroll
@@ -219,7 +223,8 @@ struct Window {
     lv = c.v_scale[(size_t)pg * c.hkv + hk];
   }
   __device__ __forceinline__ void have(float sc) {
-    ks = fmaxf(ks * fabsf(sc), 1.2e-38f);  // (not zero: hidden keys have scores of minus infinity)
+    ks *= fabsf(sc);
+    ks = ks < 1.2e-38f ? 1.2e-38f : ks;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
     lv = __builtin_amdgcn_logf(lv);
     asm volatile("" ::"v"(ks), "v"(lv));  // (arrived: a wait for them later would also wait for the blocks in flight)
   }
@@ -579,6 +584,8 @@ int q8_cache(const dag_kv_q8_t* kv, Q8Cache* c) {
   *c = Q8Cache{(const uint8_t*)kv->k_pool, (const uint8_t*)kv->v_pool, kv->k_scale, kv->v_scale, kv->n_pages, kv->hkv};
   return DAG_OK;
 }
+// (of a softmax scale that is infinite no score is a number)
+float q8_softmax_scale(float x) { return fabsf(x) < INFINITY ? x * 1.4426950408889634f : NAN; }
 int q8_pointers(const Q8Cache& c) {
   if (!c.k_pool || !c.v_pool || !c.k_scale || !c.v_scale) return DAG_ERR_NULL;
   return dag_aligned16(c.k_pool) && dag_aligned16(c.v_pool) && ((uintptr_t)c.k_scale & 3) == 0 && ((uintptr_t)c.v_scale & 3) == 0 ? DAG_OK : DAG_ERR_ALIGN;
@@ -634,7 +641,7 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   a.chunk_b = p.chunk_b;
   a.splits_b = p.splits_b;
   a.items_a = p.items_a;
-  a.sc = softmax_scale * 1.4426950408889634f;
+  a.sc = q8_softmax_scale(softmax_scale);
   hipStream_t stream = (hipStream_t)stream_;
   if (p.whole) {
     if (p.items_b == 0) a.branch_page_off = a.branch_len = (const int32_t*)q;
@@ -713,7 +720,7 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   a.weight = (float)hkv * (float)D / 128.f * (wide ? Q8_SEG_WIDE : 1.f);
   const int64_t most_pages = (int64_t)d->n_segments * p.rb_max * d->max_seg_pages * hkv * D;
   a.few = p.chunk == 8 && most_pages < (d->max_seg_pages <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) * 128;
-  a.sc = softmax_scale * 1.4426950408889634f;
+  a.sc = q8_softmax_scale(softmax_scale);
   hipStream_t stream = (hipStream_t)stream_;
   if (p.items > 0 && q8_whole_segments(d, hkv, D)) {
     auto* const kernel = D == 128 ? k_q8_whole_seg<128> : k_q8_whole_seg<64>;

@@ -62,3 +62,33 @@ def test_value_scales_from_the_smallest_to_large_ones(hq, hkv, d, spare):
             x.call()
             torch.cuda.synchronize()
             check(x.out, x.q, x.contexts, x.cache)
+
+
+@pytest.mark.parametrize("spare", [0, 400])
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf")])
+def test_a_softmax_scale_that_is_no_number(scale, spare):
+    """Rows that see a token get no numbers, rows that see none zeros."""
+    c = Cascade([(70, [20, 33]), (0, [0, 1])], 8, 2, 128, 43, spare=spare)
+    s = Segments(4, [(200, [(0, 200), (1, 0), (2, 30)]), (50, [(1, 0), (3, 17)])], 8, 2, 64, 44, spare=spare)
+    for x, empty in ((c, 2), (s, 1)):
+        x.call(softmax_scale=scale)
+        torch.cuda.synchronize()
+        rows = torch.arange(4) != empty
+        assert torch.isnan(x.out[rows.to(DEV)]).all() and (x.out[empty] == 0).all()
+
+
+@pytest.mark.parametrize("name", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("spare", [0, 400])
+def test_a_scale_that_is_no_number_reaches_the_rows_that_see_its_page_and_no_others(name, spare):
+    n = 20
+    sees = [33 + r * 7 % n for r in range(n)]  # (rows of either kind side by side)
+    s = Segments(n, [(200, [(r, 200) for r in range(n)]), (60, list(enumerate(sees)))], 8, 2, 128, 45, spare=spare)
+    s.call()
+    good = s.out.clone()
+    getattr(s.cache, name)[int(s.contexts[0][1][0][3]), 1] = float("nan")  # tokens 48 .. of the second segment
+    s.call()
+    torch.cuda.synchronize()
+    want = torch.zeros_like(good, dtype=torch.bool)
+    want[[r for r in range(n) if sees[r] > 48], 4:] = True
+    assert torch.equal(torch.isnan(s.out), want)
+    assert torch.equal(s.out[~want], good[~want])
