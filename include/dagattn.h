@@ -410,7 +410,7 @@ int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int
  * tokens).  q / out [n_live][hq][head_dim] bf16 DEVICE, q already rotated; hq a multiple of kv->hkv, hq / hkv <= 32.
  * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), otherwise every branch is in a
  * group; a branch that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
- * never followed; the host bounds are trusted.  softmax_scale may be of either sign, or zero.  Sums, maxima and partial results are
+ * never followed; a list that is longer than its host bound is read up to the bound.  softmax_scale may be of either sign, or zero.  Sums, maxima and partial results are
  * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches; one for short contexts); the call
  * allocates nothing and does not synchronise; calls that overlap need a workspace each. */
 size_t dag_decode_q8_workspace_bytes(const dag_decode_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);

@@ -45,12 +45,14 @@ struct Q8DecodeArgs {
   int first_own;
   int n_live, hq, hkv, G;
   int rb_max, chunk_a, splits_a, chunk_b, splits_b, items_a;
+  int most_a, most_b;  // tokens of a list by the host's bounds: what a length has beyond them is not read
   float sc;        // softmax_scale * log2(e)
 };
 
 struct Q8SegArgs {
   SegArgs s;
   Q8Cache kv;
+  int most;  // tokens of a segment by the host's bound
 };
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -369,7 +371,7 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
   const int branch0 = shared ? a.group_branch_off[x] : x;
   const int nrows = shared ? (a.group_branch_off[x + 1] - branch0) * a.G : a.G;
   const int32_t* const pages = shared ? a.shared_pages + a.shared_page_off[x] : a.branch_pages + a.branch_page_off[x];
-  const int len = shared ? a.shared_len[x] : a.branch_len[x], chunk = shared ? a.chunk_a : a.chunk_b;
+  const int len = shared ? min(a.shared_len[x], a.most_a) : min(a.branch_len[x], a.most_b), chunk = shared ? a.chunk_a : a.chunk_b;
   if (row0 >= nrows) return;
   const int p0 = split * chunk, p1 = min(p0 + chunk, (len + PAGE - 1) / PAGE);
   auto rows = [&](int row) __attribute__((always_inline)) {
@@ -387,17 +389,17 @@ __global__ void __launch_bounds__(64, 2) k_q8_decode_seg(Q8SegArgs args) {
   if (idx >= a.totals[0]) return;
   const SegItem it = a.items[idx];
   const int slice = (it.nsplit >> 23) & 0x1fe, nsplit = it.nsplit & 0xffffff;
-  const int p1 = min(it.p0 + slice, min((it.len + PAGE - 1) / PAGE, a.chunk * a.splits));
-  if (it.row0 >= it.nrows || it.p0 >= p1) return;  // (never listed)
+  const int len = min(it.len, args.most), p1 = min(it.p0 + slice, (len + PAGE - 1) / PAGE);
+  if (it.row0 >= it.nrows) return;  // (never listed)
   auto rows = [&](int row) __attribute__((always_inline)) {
     const int entry = it.e0 + row / a.G, head = hk * a.G + row % a.G, place = it.place + row / a.G * nsplit;
     const bool there = entry >= 0 && entry < a.total_readers;  // (reader lists longer than announced: no partial)
     const int branch = there ? min(max(a.seg_readers[entry], 0), a.n_live - 1) : 0;
-    int lim = it.len;
-    if constexpr (LIMITS) lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), it.len);
+    int lim = len;
+    if constexpr (LIMITS) lim = min(max(there ? a.seg_reader_len[entry] : 0, 0), len);
     return Row{a.q + ((size_t)branch * a.hq + head) * D, (size_t)place * a.hq + head, lim, there && place < a.splits * a.total_readers};
   };
-  run_item<D, LIMITS, !WIDE>(args.kv, a.seg_pages + it.page_off, it.p0, p1, it.len, hk, a.sc, it.row0, it.nrows, a.part_o, a.part_ml, lane, rows);
+  run_item<D, LIMITS, !WIDE>(args.kv, a.seg_pages + it.page_off, it.p0, p1, len, hk, a.sc, it.row0, it.nrows, a.part_o, a.part_ml, lane, rows);
 }
 
 constexpr int WHOLE_WAVES = 8;
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole(Q8DecodeArgs a
     if (found) g = min(base + __builtin_ctzll(found), n_groups - 1);
   }
   const int shared_at = a.shared_page_off[max(g, 0)], shared_len = a.shared_len[max(g, 0)];
-  const int seen = max(lane == 0 ? (g >= 0 && a.splits_a > 0 ? shared_len : 0) : lane == 1 && a.splits_b > 0 ? own_len : 0, 0);
+  const int seen = max(lane == 0 ? (g >= 0 ? min(shared_len, a.most_a) : 0) : lane == 1 ? min(own_len, a.most_b) : 0, 0);
   whole_branch<D>(a, a.kv, lane == 0 ? a.shared_pages + shared_at : a.branch_pages + own_at, seen, q, r, hk, (float*)smem, w, lane);
 }
 
@@ -498,7 +500,7 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole_seg(Q8SegArgs 
     const int e = __builtin_amdgcn_readlane(entry, i), s = __popcll(__builtin_amdgcn_ballot_w64(end <= e));
     if (lane == i && e >= 0 && e < a.total_readers && s < a.n_segments) seg = s;
   }
-  const int at = max(seg, 0), page_off = a.seg_page_off[at], len = a.seg_len[at];
+  const int at = max(seg, 0), page_off = a.seg_page_off[at], len = min(a.seg_len[at], args.most);
   const int sees = a.seg_reader_len && n > 0 && a.total_readers > 0 ? a.seg_reader_len[min(max(entry, 0), a.total_readers - 1)] : len;
   whole_branch<D>(a, args.kv, a.seg_pages + page_off, seg >= 0 ? max(min(sees, len), 0) : 0, q, r, hk, (float*)smem, w, lane);
 }
@@ -586,6 +588,8 @@ int q8_cache(const dag_kv_q8_t* kv, Q8Cache* c) {
 }
 // (of a softmax scale that is infinite no score is a number)
 float q8_softmax_scale(float x) { return fabsf(x) < INFINITY ? x * 1.4426950408889634f : NAN; }
+// Tokens of so many pages (sums of a few more stay in 32 bits).
+int tokens_of(int pages) { return (pages < (INT32_MAX - 64) / PAGE ? pages : (INT32_MAX - 64) / PAGE) * PAGE; }
 int q8_pointers(const Q8Cache& c) {
   if (!c.k_pool || !c.v_pool || !c.k_scale || !c.v_scale) return DAG_ERR_NULL;
   return dag_aligned16(c.k_pool) && dag_aligned16(c.v_pool) && ((uintptr_t)c.k_scale & 3) == 0 && ((uintptr_t)c.v_scale & 3) == 0 ? DAG_OK : DAG_ERR_ALIGN;
@@ -641,6 +645,8 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   a.chunk_b = p.chunk_b;
   a.splits_b = p.splits_b;
   a.items_a = p.items_a;
+  a.most_a = p.items_a > 0 ? tokens_of(d->max_shared_pages) : 0;
+  a.most_b = tokens_of(d->max_branch_pages);
   a.sc = q8_softmax_scale(softmax_scale);
   hipStream_t stream = (hipStream_t)stream_;
   if (p.whole) {
@@ -705,6 +711,7 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   a.items = (SegItem*)(base + p.off_items);
   a.totals = (int32_t*)(base + p.off_total);
   a.entry_first = (int32_t*)(base + p.off_first);
+  args.most = tokens_of(d->max_seg_pages);
   a.item_cap = (int)p.items;
   a.n_segments = d->n_segments;
   a.n_live = d->n_live;

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_seg_plan(SegArgs a) {
       g.len = max(a.seg_len[s], 0);
       g.e0 = a.seg_reader_off[s];
       g.nr = max(a.seg_reader_off[s + 1] - g.e0, 0);
-      g.npages = min((g.len + PAGE - 1) / PAGE, a.chunk * a.splits);
+      g.npages = min((int)(((uint32_t)g.len + PAGE - 1) / PAGE), a.chunk * a.splits);
       g.rbs = min((g.nr * a.G + 31) / 32, a.rb_max);
     }
     return g;

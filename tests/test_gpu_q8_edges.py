@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2602_07529_amd import binding as B
+from tests import q8_rules
 from tests.gpu_util import DEV
 from tests.q8_cases import Cascade, Segments, check, ints
 
@@ -92,3 +93,24 @@ def test_a_scale_that_is_no_number_reaches_the_rows_that_see_its_page_and_no_oth
     want[[r for r in range(n) if sees[r] > 48], 4:] = True
     assert torch.equal(torch.isnan(s.out), want)
     assert torch.equal(s.out[~want], good[~want])
+
+
+@pytest.mark.parametrize("shared,own,whole", [(64, 32, True), (1600, 64, False)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("more", [1, 1000, 2 ** 31 - 9000])
+def test_a_length_past_its_bound_counts_as_the_bound(more, d, shared, own, whole):
+    c = Cascade([(shared, [own, own]), (shared, [own])], 8, 2, d, 46)
+    assert bool(q8_rules.plan(c.desc.c, 8, 2, d).whole) is whole
+    for name in ("shared_len", "branch_len"):
+        c.desc.t[name] += more
+    c.call()
+    torch.cuda.synchronize()
+    check(c.out, c.q, c.contexts, c.cache)
+    for limits in (False, True):
+        n = shared * (1 if whole else 5)
+        s = Segments(4, [(n, [(r, 2 ** 31 - 1) for r in range(4)])] + [(n, [(r, n)]) for r in range(4)], 8, 2, d, 47, limits=limits)
+        assert q8_rules.segments_whole(s.desc.c, 2, d) is whole
+        s.desc.t["seg_len"] += more
+        s.call()
+        torch.cuda.synchronize()
+        check(s.out, s.q, s.contexts, s.cache)
