@@ -78,6 +78,9 @@ class Fork:
         dev = cache.k_pool.device
         self.cache, self.theta, self.scale, self.n = cache, float(theta), softmax_scale, n_branches
         prefix, self.max_len = k.shape[0], max_len
+        need = (prefix + 15) // 16 + n_branches * ((max_len + 15) // 16)
+        if need > cache.c.n_pages:  # (so no step is ever refused a page)
+            raise ValueError("the cache has %d pages, not the %d of the prefix and its branches" % (cache.c.n_pages, need))
         width = max((prefix + 15) // 16, (max_len + 15) // 16)
         ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)  # noqa: E731
         # row 0 holds the prefix, row 1 + b branch b, whose first position is the fork's
@@ -91,8 +94,6 @@ class Fork:
             slots, pos = ints([0] * prefix), ints([0] * prefix)
             B.dag_kv_tables(self.rows, ints([prefix] + [0] * n_branches), self.len, self.len, self.free, self.free, self.off, slots,
                             pos0=self.pos0, pos=pos, refused=self.refused)
-            if self.refused.item():
-                raise ValueError("the cache has too few pages for the prefix")
             B.dag_kv_append_rope_q8(cache, slots, pos, k, v, self.theta)
         line = torch.arange(1 + n_branches, dtype=torch.int32, device=dev) * width
         self.desc = B.DecodeDesc.on_device(
