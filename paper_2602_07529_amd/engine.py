@@ -121,6 +121,8 @@ class Fork:
         step overwrites."""
         if self.tokens == self.max_len:
             raise ValueError("the branches are full")
+        if q.shape != self.q.shape or k.shape != self.k.shape or v.shape != self.v.shape:
+            raise ValueError("q is %s, k and v are %s" % (list(self.q.shape), list(self.k.shape)))
         self.tokens += 1
         self.q.copy_(q)
         self.k.copy_(k)

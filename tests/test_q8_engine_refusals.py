@@ -19,3 +19,12 @@ def test_a_cache_that_cannot_hold_the_prefix_and_its_branches(n_pages, prefix, n
 
 def test_a_cache_that_just_holds_them():
     fork(6, 0, 3, 17)
+
+
+def test_a_step_takes_a_token_of_every_branch():
+    f = fork(6, 0, 3, 17)
+    q, k = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    for bad in ((q[:1], k, k), (q, k[:1], k), (q, k, k[:, :1]), (q[0], k, k), (q[..., :1], k, k)):
+        with pytest.raises(ValueError):
+            f.step(*bad)
+    assert f.tokens == 0
