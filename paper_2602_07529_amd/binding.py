@@ -558,9 +558,9 @@ def _decode_q8(call, desc, q, cache, out, workspace, softmax_scale):
         raise ValueError("q and out are [n_live][heads][head_dim]")
     if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous():
         raise TypeError("q and out are contiguous bfloat16")
-    lens = desc.t["branch_len" if type(desc) is DecodeDesc else "seg_len"]  # (its arrays are on one device)
+    array = next((x for x in desc.t.values() if x is not None), q)  # (its arrays are on one device)
     _check(call(desc.c, cache.ref, q.data_ptr(), out.data_ptr(), hq, d ** -0.5 if softmax_scale is None else softmax_scale,
-                workspace.data_ptr(), workspace.numel(), _here(q, out, cache.k_pool, workspace, q if lens is None else lens)))
+                workspace.data_ptr(), workspace.numel(), _here(q, out, cache.k_pool, workspace, array)))
 
 
 def dag_attn_decode_q8(ddesc, q, cache, out, workspace, softmax_scale=None):
