@@ -176,10 +176,11 @@ __device__ __forceinline__ void compute_block(Block<D>& b, const bf16x8 (&q)[D /
     asm volatile("");  // (a branch: the compiler would compare and select in every block)
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[r] = key0 + 16 * H + r < lim ? S[r] : -INFINITY;
-    if (key0 + 16 * H >= lim) {  // (scales of a page that the row sees nothing of)
-      ks = 1.f;
-      lv = 0.f;
-    }
+    if constexpr (LIMITS)
+      if (key0 + 16 * H >= lim) {  // (scales of a page that the row sees nothing of)
+        ks = 1.f;
+        lv = 0.f;
+      }
   }
   float bm = S[0];
 #pragma unroll
@@ -406,38 +407,46 @@ constexpr int WHOLE_WAVES = 8;
 
 // Steps over short contexts: a workgroup to a (branch, KV head), whose eight waves share the pages of all lists that the branch reads and put
 // their sums together in LDS: one launch and no partials in memory, which is what such steps consist of otherwise.  Every branch reads
-// the shared pages for itself.  Lane i of a wave knows list i.
+// the shared pages for itself.  lists(base, pages, seen): pages of list base + lane, and how many tokens the branch sees of it.
 // What bounds it is the chain of loads up to the first page, each of which takes about as long as the arithmetic of a wave: they stand
 // in as few steps as the description allows, none behind a condition.
-template <int D, typename A>
-__device__ __forceinline__ void whole_branch(const A& a, const Q8Cache& kv, const int32_t* pages, int seen, bf16x8 (&q)[D / 16], int r, int hk, float* smem,
-                                             int w, int lane) {
-  const int L = lane & 31, G = a.G, np = (seen + PAGE - 1) / PAGE, units = (np + 1) / 2;
-  const int behind = dag_wave_scan(units), all = __builtin_amdgcn_readlane(behind, 63), front = behind - units;
-  const int u0 = (int)((int64_t)all * w / WHOLE_WAVES), u1 = (int)((int64_t)all * (w + 1) / WHOLE_WAVES);
+template <int D, typename A, typename F>
+__device__ __forceinline__ void whole_branch(const A& a, const Q8Cache& kv, int n_lists, F&& lists, bf16x8 (&q)[D / 16], int r, int hk, float* smem, int w,
+                                             int lane) {
+  const int L = lane & 31, G = a.G;
   Sums<D> sums;
   sums.start();
-  sign_q<D>(q, a.sc);
-  for (uint64_t left = __builtin_amdgcn_ballot_w64(max(front, u0) < min(behind, u1)); left; left &= left - 1) {
-    const int i = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(front, i);
-    const int n = __builtin_amdgcn_readlane(np, i), tokens = __builtin_amdgcn_readlane(seen, i);
-    const int32_t* const list = (const int32_t*)dag_readlane((int64_t)(uintptr_t)pages, i);
-    const int p0 = 2 * max(u0 - at, 0), p1 = min(2 * (u1 - at), n);
-    stream_slice<D, false, true>(kv, list, p0, p1, tokens, tokens, tokens, hk, a.sc, lane, q, sums);
+  bool some = false;
+  for (int base = 0; base == 0 || base < n_lists; base += 64) {
+    const int32_t* pages;
+    int seen;
+    lists(base, pages, seen);
+    if (base == 0) sign_q<D>(q, a.sc);
+    const int np = (seen + PAGE - 1) / PAGE, units = (np + 1) / 2;
+    const int behind = dag_wave_scan(units), all = __builtin_amdgcn_readlane(behind, 63), front = behind - units;
+    const int u0 = (int)((int64_t)all * w / WHOLE_WAVES), u1 = (int)((int64_t)all * (w + 1) / WHOLE_WAVES);
+    some |= u0 < u1;
+    for (uint64_t left = __builtin_amdgcn_ballot_w64(max(front, u0) < min(behind, u1)); left; left &= left - 1) {
+      const int i = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(front, i);
+      const int n = __builtin_amdgcn_readlane(np, i), tokens = __builtin_amdgcn_readlane(seen, i);
+      const int32_t* const list = (const int32_t*)dag_readlane((int64_t)(uintptr_t)pages, i);
+      const int p0 = 2 * max(u0 - at, 0), p1 = min(2 * (u1 - at), n);
+      stream_slice<D, false, true>(kv, list, p0, p1, tokens, tokens, tokens, hk, a.sc, lane, q, sums);
+    }
   }
   const float m = sums.m, l = sums.l + other_half(sums.l);
   const f32x16(&O)[D / 32] = sums.O;
   constexpr int ROW = D + 4;
   float* const ml = smem + WHOLE_WAVES * G * ROW;
   if (L < G) {
-    if (u0 < u1) {
+    if (some) {
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *(f32x4*)(smem + (w * G + L) * ROW + 32 * db + 8 * r4 + 4 * (lane >> 5)) = f32x4{O[db][4 * r4], O[db][4 * r4 + 1], O[db][4 * r4 + 2], O[db][4 * r4 + 3]};
     }
-    if (lane < 32) *(float2*)(ml + (w * G + L) * 2) = make_float2(m, u0 < u1 ? l : 0.f);
+    if (lane < 32) *(float2*)(ml + (w * G + L) * 2) = make_float2(m, some ? l : 0.f);
   }
   __syncthreads();
   for (int x = w * 64 + lane; x < G * (D / 4); x += 64 * WHOLE_WAVES) {
@@ -481,10 +490,14 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole(Q8DecodeArgs a
   }
   const int shared_at = a.shared_page_off[max(g, 0)], shared_len = a.shared_len[max(g, 0)];
   const int seen = max(lane == 0 ? (g >= 0 ? min(shared_len, a.most_a) : 0) : lane == 1 ? min(own_len, a.most_b) : 0, 0);
-  whole_branch<D>(a, a.kv, lane == 0 ? a.shared_pages + shared_at : a.branch_pages + own_at, seen, q, r, hk, (float*)smem, w, lane);
+  auto lists = [&](int, const int32_t*& list, int& n) __attribute__((always_inline)) {
+    list = lane == 0 ? a.shared_pages + shared_at : a.branch_pages + own_at;
+    n = seen;
+  };
+  whole_branch<D>(a, a.kv, 2, lists, q, r, hk, (float*)smem, w, lane);
 }
 
-// Over segments, up to 64 of them: lane i has entry i of the branch.
+// Over segments, up to 64 of them: lane i has entry i of the branch (of the next 64, if it names segments more than once).
 template <int D>
 __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole_seg(Q8SegArgs args) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -493,16 +506,20 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole_seg(Q8SegArgs 
   bf16x8 q[D / 16];
   fetch_q<D>(q, whole_row<D>(a, r, hk, lane), lane);
   const int last = a.seg_reader_off[min(lane, a.n_segments - 1) + 1], end = lane < a.n_segments ? last : INT32_MAX;  // of the entries of segment `lane`
-  const int e0 = a.branch_entry_off[r], n = min(max(a.branch_entry_off[r + 1] - e0, 0), 64);
-  const int entry = n > 0 ? a.branch_entries[e0 + min(lane, n - 1)] : -1;
-  int seg = -1;
-  for (int i = 0; i < n; ++i) {
-    const int e = __builtin_amdgcn_readlane(entry, i), s = __popcll(__builtin_amdgcn_ballot_w64(end <= e));
-    if (lane == i && e >= 0 && e < a.total_readers && s < a.n_segments) seg = s;
-  }
-  const int at = max(seg, 0), page_off = a.seg_page_off[at], len = min(a.seg_len[at], args.most);
-  const int sees = a.seg_reader_len && n > 0 && a.total_readers > 0 ? a.seg_reader_len[min(max(entry, 0), a.total_readers - 1)] : len;
-  whole_branch<D>(a, args.kv, a.seg_pages + page_off, seg >= 0 ? max(min(sees, len), 0) : 0, q, r, hk, (float*)smem, w, lane);
+  const int e0 = a.branch_entry_off[r], entries = max(a.branch_entry_off[r + 1] - e0, 0);
+  auto lists = [&](int base, const int32_t*& list, int& seen) __attribute__((always_inline)) {
+    const int n = min(entries - base, 64), entry = n > 0 ? a.branch_entries[e0 + base + min(lane, n - 1)] : -1;
+    int seg = -1;
+    for (int i = 0; i < n; ++i) {
+      const int e = __builtin_amdgcn_readlane(entry, i), s = __popcll(__builtin_amdgcn_ballot_w64(end <= e));
+      if (lane == i && e >= 0 && e < a.total_readers && s < a.n_segments) seg = s;
+    }
+    const int at = max(seg, 0), page_off = a.seg_page_off[at], len = min(a.seg_len[at], args.most);
+    const int sees = a.seg_reader_len && n > 0 && a.total_readers > 0 ? a.seg_reader_len[min(max(entry, 0), a.total_readers - 1)] : len;
+    list = a.seg_pages + page_off;
+    seen = seg >= 0 ? max(min(sees, len), 0) : 0;
+  };
+  whole_branch<D>(a, args.kv, entries, lists, q, r, hk, (float*)smem, w, lane);
 }
 
 // A wave to a (branch, query head): its partials are put together by their references, 64 at a time a lane each has reference and

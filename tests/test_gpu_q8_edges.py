@@ -114,3 +114,14 @@ def test_a_length_past_its_bound_counts_as_the_bound(more, d, shared, own, whole
         s.call()
         torch.cuda.synchronize()
         check(s.out, s.q, s.contexts, s.cache)
+
+
+@pytest.mark.parametrize("limits", [False, True])
+@pytest.mark.parametrize("spare", [0, 400])
+@pytest.mark.parametrize("times", [64, 65, 150])
+def test_a_branch_that_names_a_segment_many_times_reads_it_as_often(times, spare, limits):
+    s = Segments(2, [(9, [(0, 9)] * times + [(1, 9)]), (20, [(1, 20), (0, 13 if limits else 20)])], 8, 2, 128, 48, spare=spare, limits=limits, shuffle=True)
+    assert q8_rules.segments_whole(s.desc.c, 2, 128) is (spare == 0)
+    s.call()
+    torch.cuda.synchronize()
+    check(s.out, s.q, s.contexts, s.cache)
