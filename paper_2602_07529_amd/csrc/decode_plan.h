@@ -265,14 +265,27 @@ constexpr float Q8_SEG_WIDE = 0.5f;
 // (4 query heads each) in graphs, items and merge : whole.  Pages that a branch reads: dimension 128, up to 28 of them 1.1 to 1.4, 41 0.96 to
 // 1.02, 63 0.9, 101 0.76; dimension 64 41 1.03 to 1.1, 63 0.94 to 1.  With 256 workgroups, which fill the device, 1.1 to 1.4 up to
 // 101 pages; with 512 dimension 64 1.04 to 1.36 up to 41 pages, dimension 128 0.66 to 0.92.
+// Every branch reads the shared pages for itself, so these last lines hold only where that is at most twice the pages of the items, or the merge
+// costs as much (8 query heads to a KV head), or, from 4 query heads on, the KV heads are a multiple of 8, so that the workgroups of siblings
+// meet in one L2 (they go to the eight XCDs in turn).  From 1,792 steps of 1 to 512 branches in groups of 1 to 512 on 1, 2, 4 and 8 KV heads,
+// 1, 4 and 8 query heads each, pages that no cache holds, items : whole at 90 shared and 5 own pages, dimension 128: 4 query heads in groups of 4
+// on 8 KV heads 1.07, on 1 and 2 0.66 to 0.75; 1 query head on 8 KV heads 0.81 to 0.86, on 2 0.56 to 0.9.  All steps that are taken whole:
+// geometric mean 1.19, the least 0.85.
+constexpr int WHOLE_Q8_GROUPS = 256, WHOLE_Q8_FULL = 192, WHOLE_Q8_FULL_PAGES = 101;
+inline bool q8_whole(const dag_decode_desc_t* d, int G, int hkv, int D, int rb_max) {
+  const int64_t groups = (int64_t)d->n_live * hkv, shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages, pages = shared + own;
+  const int few = D == 64 ? 52 : 41;
+  if (groups > 2 * WHOLE_Q8_GROUPS || pages > WHOLE_Q8_FULL_PAGES) return false;
+  const bool many = d->n_live * pages <= 2 * ((int64_t)d->n_groups * rb_max * shared + d->n_live * own) || G >= 8 || (G >= 4 && hkv % 8 == 0);
+  return (groups <= WHOLE_Q8_GROUPS && (pages <= few || (groups >= WHOLE_Q8_FULL && many))) || (D == 64 && pages <= (many ? 41 : 22));
+}
+// Whether the pages that a branch takes whole go through the caches.  Shared pages do where the workgroups of siblings are on several XCDs: cached : not
+// 0.98 on 4 KV heads, 0.92 to 0.95 on 2, 0.82 to 0.92 on 1; on 8 1.02 to 1.03, pages that nobody shares 1.05.
+inline bool q8_whole_cached(const dag_decode_desc_t* d, int hkv) {
+  return d->n_groups > 0 && d->max_group_size > 1 && hkv % 8 != 0 && d->max_shared_pages > d->max_branch_pages;
+}
 // Segments, whose items take a launch more: 1.0 to 1.9 at dimension 128, 1.2 to 1.9 at 64, up to 106 pages (four entries to a branch,
 // 63 pages in the longest segment: what the host knows is 252).
-constexpr int WHOLE_Q8_GROUPS = 256, WHOLE_Q8_FULL = 192, WHOLE_Q8_FULL_PAGES = 101;
-inline bool q8_whole(int64_t groups, int64_t pages, int D) {
-  const int few = D == 64 ? 52 : 41;
-  return (groups <= WHOLE_Q8_GROUPS && pages <= (groups >= WHOLE_Q8_FULL ? WHOLE_Q8_FULL_PAGES : few)) ||
-         (D == 64 && groups <= 2 * WHOLE_Q8_GROUPS && pages <= 41);
-}
 inline bool q8_whole_segments(const dag_decode_seg_desc_t* d, int hkv, int D) {
   return d->n_segments <= 64 && (int64_t)d->n_live * hkv <= WHOLE_Q8_GROUPS &&
          dag_ceil_div(d->total_readers, d->n_live) * d->max_seg_pages <= (D == 64 ? 384 : 256);
@@ -306,7 +319,7 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
   if (ia + ib > INT32_MAX || rows > INT32_MAX || (int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;
   p->items_a = (int)ia;
   p->items_b = (int)ib;
-  p->whole = ia + ib > 0 && q8_whole(base_b, (int64_t)shared + own, D);
+  p->whole = ia + ib > 0 && q8_whole(d, hq / hkv, hkv, D, p->rb_max);
   p->off_ml = dag_align_up((size_t)rows * D * 4, 256);
   p->bytes = p->off_ml + dag_align_up((size_t)rows * 2 * 4, 256) + 256;
   return DAG_OK;

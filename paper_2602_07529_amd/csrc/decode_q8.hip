@@ -78,7 +78,7 @@ struct Block {         // 32 keys (two pages)
 };
 
 template <bool ONCE>
-__device__ __forceinline__ u32x4 load16(const uint8_t* p) {  // ONCE: nobody else reads it
+__device__ __forceinline__ u32x4 load16(const uint8_t* p) {  // ONCE: passes the caches by
   if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4*)p);
   else return *(const u32x4*)p;
 }
@@ -410,7 +410,7 @@ constexpr int WHOLE_WAVES = 8;
 // the shared pages for itself.  lists(base, pages, seen): pages of list base + lane, and how many tokens the branch sees of it.
 // What bounds it is the chain of loads up to the first page, each of which takes about as long as the arithmetic of a wave: they stand
 // in as few steps as the description allows, none behind a condition.
-template <int D, typename A, typename F>
+template <int D, bool ONCE, typename A, typename F>
 __device__ __forceinline__ void whole_branch(const A& a, const Q8Cache& kv, int n_lists, F&& lists, bf16x8 (&q)[D / 16], int r, int hk, float* smem, int w,
                                              int lane) {
   const int L = lane & 31, G = a.G;
@@ -431,7 +431,7 @@ __device__ __forceinline__ void whole_branch(const A& a, const Q8Cache& kv, int 
       const int n = __builtin_amdgcn_readlane(np, i), tokens = __builtin_amdgcn_readlane(seen, i);
       const int32_t* const list = (const int32_t*)dag_readlane((int64_t)(uintptr_t)pages, i);
       const int p0 = 2 * max(u0 - at, 0), p1 = min(2 * (u1 - at), n);
-      stream_slice<D, false, true>(kv, list, p0, p1, tokens, tokens, tokens, hk, a.sc, lane, q, sums);
+      stream_slice<D, false, ONCE>(kv, list, p0, p1, tokens, tokens, tokens, hk, a.sc, lane, q, sums);
     }
   }
   const float m = sums.m, l = sums.l + other_half(sums.l);
@@ -474,8 +474,8 @@ __device__ __forceinline__ const uint16_t* whole_row(const A& a, int r, int hk, 
   return a.q + ((size_t)r * a.hq + hk * a.G + min(lane & 31, a.G - 1)) * D;
 }
 
-// (Arrays that the description does not have are replaced by q, whose memory may be read, by the host.)
-template <int D>
+// (ONCE: q8_whole_cached.  Arrays that the description does not have are replaced by q, whose memory may be read, by the host.)
+template <int D, bool ONCE>
 __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole(Q8DecodeArgs a, int n_groups) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hk = blockIdx.x % a.hkv, r = blockIdx.x / a.hkv;
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole(Q8DecodeArgs a
     list = lane == 0 ? a.shared_pages + shared_at : a.branch_pages + own_at;
     n = seen;
   };
-  whole_branch<D>(a, a.kv, 2, lists, q, r, hk, (float*)smem, w, lane);
+  whole_branch<D, ONCE>(a, a.kv, 2, lists, q, r, hk, (float*)smem, w, lane);
 }
 
 // Over segments, up to 64 of them: lane i has entry i of the branch (of the next 64, if it names segments more than once).
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(64 * WHOLE_WAVES, 2) k_q8_whole_seg(Q8SegArgs 
     list = a.seg_pages + page_off;
     seen = seg >= 0 ? max(min(sees, len), 0) : 0;
   };
-  whole_branch<D>(a, args.kv, entries, lists, q, r, hk, (float*)smem, w, lane);
+  whole_branch<D, true>(a, args.kv, entries, lists, q, r, hk, (float*)smem, w, lane);
 }
 
 // A wave to a (branch, query head): its partials are put together by their references, 64 at a time a lane each has reference and
@@ -669,7 +669,8 @@ extern "C" int dag_attn_decode_q8(const dag_decode_desc_t* d, const dag_kv_q8_t*
   if (p.whole) {
     if (p.items_b == 0) a.branch_page_off = a.branch_len = (const int32_t*)q;
     if (p.items_a == 0) a.shared_page_off = a.shared_len = (const int32_t*)q;
-    auto* const kernel = D == 128 ? k_q8_whole<128> : k_q8_whole<64>;
+    auto* const kernel = q8_whole_cached(d, a.hkv) ? (D == 128 ? k_q8_whole<128, false> : k_q8_whole<64, false>)
+                                                   : (D == 128 ? k_q8_whole<128, true> : k_q8_whole<64, true>);
     const int lds = whole_lds_bytes(a.G, D);
     if (lds > 65536) DAG_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(d->n_live * a.hkv)), dim3(64 * WHOLE_WAVES), lds, stream, a, p.items_a > 0 ? d->n_groups : 0);
