@@ -285,10 +285,14 @@ inline bool q8_whole_cached(const dag_decode_desc_t* d, int hkv) {
   return d->n_groups > 0 && d->max_group_size > 1 && hkv % 8 != 0 && d->max_shared_pages > d->max_branch_pages;
 }
 // Segments, whose items take a launch more: 1.0 to 1.9 at dimension 128, 1.2 to 1.9 at 64, up to 106 pages (four entries to a branch,
-// 63 pages in the longest segment: what the host knows is 252).
+// 63 pages in the longest segment: what the host knows is 252).  That is an average: a branch by itself may have all segments but the other
+// branches' own, and one workgroup to a KV head then reads for it what items share out.  A branch of many long segments beside branches of a short one,
+// items : whole, 252 pages 0.62 to 0.68 (dimension 64 0.85 to 0.93), 504 0.43 (0.62 to 0.7), 1,008 0.27 to 0.34 (0.4 to 0.5), 4,096 0.13 (0.23); so no more than
+// four times the line, as where a root is the longest segment (what is usual) a branch has far fewer pages than the host has to assume.
 inline bool q8_whole_segments(const dag_decode_seg_desc_t* d, int hkv, int D) {
-  return d->n_segments <= 64 && (int64_t)d->n_live * hkv <= WHOLE_Q8_GROUPS &&
-         dag_ceil_div(d->total_readers, d->n_live) * d->max_seg_pages <= (D == 64 ? 384 : 256);
+  if (d->n_segments > 64 || (int64_t)d->n_live * hkv > WHOLE_Q8_GROUPS) return false;
+  const int64_t line = D == 64 ? 384 : 256, alone = d->n_segments - d->n_live + 1;
+  return dag_ceil_div(d->total_readers, d->n_live) * d->max_seg_pages <= line && alone * d->max_seg_pages <= 4 * line;
 }
 struct Q8Plan {
   bool whole;  // no items

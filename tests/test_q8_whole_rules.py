@@ -18,3 +18,11 @@ def whole(groups, live, shared, own, size, hq, hkv, d):
     (64, 256, 36, 5, 4, 8, 2, 64, False), (16, 256, 20, 2, 16, 8, 2, 64, True), (4, 64, 36, 5, 16, 32, 8, 64, True), (4, 64, 36, 5, 16, 8, 8, 64, False)])
 def test_steps_whose_siblings_share_pages(groups, live, shared, own, size, hq, hkv, d, taken):
     assert whole(groups, live, shared, own, size, hq, hkv, d) is taken
+
+
+@pytest.mark.parametrize("live,segments,pages,readers,total,hkv,d,taken", [
+    (32, 64, 128, 1, 64, 8, 128, False), (32, 64, 128, 1, 64, 8, 64, False), (3, 18, 63, 1, 18, 8, 128, False),  # one branch has most of the segments
+    (32, 64, 31, 1, 64, 8, 128, True), (3, 6, 39, 3, 12, 8, 128, True), (32, 41, 63, 32, 128, 8, 128, True), (16, 11, 80, 16, 48, 8, 128, True),
+    (1, 4, 64, 1, 4, 8, 128, True), (1, 5, 64, 1, 5, 8, 128, False), (1, 64, 6, 1, 64, 1, 64, True)])
+def test_frontiers_with_a_branch_of_many_segments(live, segments, pages, readers, total, hkv, d, taken):
+    assert q8_rules.segments_whole(B.dag_decode_seg_desc_t(live, segments, 16, pages, readers, total), hkv, d) is taken
