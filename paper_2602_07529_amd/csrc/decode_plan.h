@@ -276,7 +276,7 @@ inline bool q8_whole(const dag_decode_desc_t* d, int G, int hkv, int D, int rb_m
   const int64_t groups = (int64_t)d->n_live * hkv, shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages, pages = shared + own;
   const int few = D == 64 ? 52 : 41;
   if (groups > 2 * WHOLE_Q8_GROUPS || pages > WHOLE_Q8_FULL_PAGES) return false;
-  const bool many = d->n_live * pages <= 2 * ((int64_t)d->n_groups * rb_max * shared + d->n_live * own) || G >= 8 || (G >= 4 && hkv % 8 == 0);
+  const bool many = d->n_live * pages <= 2 * (shared > 0 ? (int64_t)d->n_groups * rb_max * shared : 0) + 2 * d->n_live * own || G >= 8 || (G >= 4 && hkv % 8 == 0);
   return (groups <= WHOLE_Q8_GROUPS && (pages <= few || (groups >= WHOLE_Q8_FULL && many))) || (D == 64 && pages <= (many ? 41 : 22));
 }
 // Whether the pages that a branch takes whole go through the caches.  Shared pages do where the workgroups of siblings are on several XCDs: cached : not
@@ -308,7 +308,10 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
   const int shared = d->n_groups > 0 ? d->max_shared_pages : 0, own = d->max_branch_pages;
   const int64_t most_rows = (int64_t)d->max_group_size * (hq / hkv);
   p->rb_max = (int)dag_ceil_div(most_rows, 32);
-  const int64_t base_a = (int64_t)d->n_groups * hkv * p->rb_max, base_b = (int64_t)d->n_live * hkv;
+  if ((int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;
+  const bool read = shared > 0 && p->rb_max > 0;  // (an item at least for every group, KV head and block of rows: none of what follows passes 64 bits)
+  if (read && ((int64_t)d->n_groups * hkv > INT32_MAX || (int64_t)d->n_groups * hkv * p->rb_max > INT32_MAX)) return DAG_ERR_UNSUPPORTED;
+  const int64_t base_a = read ? (int64_t)d->n_groups * hkv * p->rb_max : 0, base_b = (int64_t)d->n_live * hkv;
   auto cut = [](int pages, int64_t most, int* splits, int* chunk) {  // slices of one length, of whole pairs of pages
     *splits = (int)dag_ceil_div(pages, most);
     *chunk = *splits > 0 ? (int)dag_ceil_div(dag_ceil_div(pages, *splits), 2) * 2 : 2;
@@ -320,7 +323,7 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
   cut(own, most, &p->splits_b, &p->chunk_b);
   const int64_t ia = base_a * p->splits_a, ib = base_b * p->splits_b;
   const int64_t rows = (int64_t)d->n_live * ((int64_t)p->splits_a + p->splits_b) * hq;
-  if (ia + ib > INT32_MAX || rows > INT32_MAX || (int64_t)d->n_live * hq > INT32_MAX) return DAG_ERR_UNSUPPORTED;
+  if (ia + ib > INT32_MAX || rows > INT32_MAX) return DAG_ERR_UNSUPPORTED;
   p->items_a = (int)ia;
   p->items_b = (int)ib;
   p->whole = ia + ib > 0 && q8_whole(d, hq / hkv, hkv, D, p->rb_max);
