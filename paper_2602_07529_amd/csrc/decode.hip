@@ -1642,6 +1642,7 @@ extern "C" int dag_attn_decode_segments(const dag_decode_seg_desc_t* d, const vo
   a.total_readers = d->total_readers;
   a.fixed = decode_knobs().chunk_seg > 0;
   a.weight = (float)hkv * (float)head_dim / 128.f;
+  a.pages_128 = (float)SEG_PAGES_128;
   const int64_t most_pages = (int64_t)d->n_segments * p.rb_max * d->max_seg_pages * hkv * head_dim;
   a.few = !a.fixed && p.chunk == 8 && most_pages < (d->max_seg_pages <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) * 128;
   a.sc = softmax_scale * 1.4426950408889634f;

@@ -255,12 +255,16 @@ inline int make_seg_plan(const dag_decode_seg_desc_t* d, int hq, int hkv, int D,
 }
 
 // Decode over an 8-bit cache: slices of about one length, so that there are Q8_WAVES of them and all run at once (what was measured
-// stands at stream_slice; more of them where groups have more than 32 rows, 88 -> 86 us for two groups of 32 over 32768 | 640), no shorter than
-// Q8_LEAST_PAGES.  Dimension 64, with half the bytes on their way: 16 groups of 8 over 16384 | 1024 tokens 72.2 us, with 2048 waves 75.4, with 4096 83.2,
-// with four pages more on their way 72.6.
-constexpr int Q8_WAVES = 1536, Q8_WIDE_WAVES = 1920, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256;
-// Segments: slices by the rules of the bf16 cache, but for more than 32 rows, whose pages weigh less: shorter slices (nine new tokens of 48 nodes 95 -> 69 us).
-constexpr float Q8_SEG_WIDE = 0.5f;
+// stands at stream_slice), no shorter than Q8_LEAST_PAGES.  Dimension 64, with half the bytes on their way: 16 groups of 8 over 16384 | 1024
+// tokens 72.2 us, with 2048 waves 75.4, with 4096 83.2, with four pages more on their way 72.6.
+// Groups of more than 32 rows, whose long slices would be the last to end: Q8_LONG_WAVES of them where they are then longer than Q8_LONG_PAGES.  From 220 random steps
+// of 1 to 20 such groups, fewer waves : more by the length of a slice of the more: up to 50 pages 0.98 (0.85 to 1.04), 51 to 70 1.02, above 1.04
+// (0.92 to 1.24).
+constexpr int Q8_WAVES = 1536, Q8_LEAST_PAGES = 8, Q8_MOST_PAGES = 256, Q8_LONG_WAVES = 1920, Q8_LONG_PAGES = 62;
+// Segments: slices by the rules of the bf16 cache, but where readers have more than 32 rows a slice gets 128 pages only from twice as many pages on: 35
+// frontiers of 81,920 to 163,840 pages (of 128 dimensions, once for each block of rows), slices of 64 : 128 pages 0.96 (0.72 to 1.09); below
+// 9,216 pages half of all these lines 1.01 (61 frontiers).
+constexpr float Q8_SEG_WIDE_128 = 2.f * SEG_PAGES_128;
 // Short contexts: a workgroup to a (branch, KV head) takes them whole, one launch.  Its lines, from 112 steps of 1 to 64 branches on 8 KV heads
 // (4 query heads each) in graphs, items and merge : whole.  Pages that a branch reads: dimension 128, up to 28 of them 1.1 to 1.4, 41 0.96 to
 // 1.02, 63 0.9, 101 0.76; dimension 64 41 1.03 to 1.1, 63 0.94 to 1.  With 256 workgroups, which fill the device, 1.1 to 1.4 up to
@@ -317,7 +321,8 @@ inline int make_q8_plan(const dag_decode_desc_t* d, int hq, int hkv, int D, Q8Pl
     *chunk = *splits > 0 ? (int)dag_ceil_div(dag_ceil_div(pages, *splits), 2) * 2 : 2;
     *splits = (int)dag_ceil_div(pages, *chunk);
   };
-  const int64_t share = dag_ceil_div(base_a * shared + base_b * own, p->rb_max > 1 ? Q8_WIDE_WAVES : Q8_WAVES);
+  const int64_t work = base_a * shared + base_b * own, long_share = dag_ceil_div(work, Q8_LONG_WAVES);
+  const int64_t share = p->rb_max > 1 && dag_ceil_div(work, Q8_WAVES) > Q8_LONG_PAGES ? long_share : dag_ceil_div(work, Q8_WAVES);
   const int64_t most = share < Q8_LEAST_PAGES ? Q8_LEAST_PAGES : share > Q8_MOST_PAGES ? Q8_MOST_PAGES : share;
   cut(base_a > 0 ? shared : 0, most, &p->splits_a, &p->chunk_a);
   cut(own, most, &p->splits_b, &p->chunk_b);

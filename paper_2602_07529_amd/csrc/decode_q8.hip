@@ -742,7 +742,8 @@ extern "C" int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* d, const
   a.total_readers = d->total_readers;
   a.fixed = false;
   const bool wide = p.rb_max > 1;
-  a.weight = (float)hkv * (float)D / 128.f * (wide ? Q8_SEG_WIDE : 1.f);
+  a.weight = (float)hkv * (float)D / 128.f;
+  a.pages_128 = wide ? Q8_SEG_WIDE_128 : (float)SEG_PAGES_128;
   const int64_t most_pages = (int64_t)d->n_segments * p.rb_max * d->max_seg_pages * hkv * D;
   a.few = p.chunk == 8 && most_pages < (d->max_seg_pages <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) * 128;
   a.sc = q8_softmax_scale(softmax_scale);

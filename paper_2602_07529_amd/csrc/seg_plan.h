@@ -39,6 +39,7 @@ struct SegArgs {
   bool fixed;      // slices of `chunk` pages, whatever there is to read
   bool few;        // by the host's bounds the slices have eight pages
   float weight;    // of a page: hkv * D / 128
+  float pages_128; // from which a slice gets 128 of them
   float sc, th;
 };
 
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_seg_plan(SegArgs a) {
     sums = gather(sums);
     longest = sums.top;
     const float pages = sums.x * a.weight;
-    k = pages < (longest <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) ? 3 : pages < SEG_PAGES_32 ? 4 : pages < SEG_PAGES_64 ? 5 : pages < SEG_PAGES_128 ? 6 : 7;
+    k = pages < (longest <= SEG_SHORT ? SEG_PAGES_16_SHORT : SEG_PAGES_16) ? 3 : pages < SEG_PAGES_32 ? 4 : pages < SEG_PAGES_64 ? 5 : pages < a.pages_128 ? 6 : 7;
     for (; k < host; ++k) {
       const float one = 1.f / (float)longest_slice(k);
       if (!fits(sums.x * one, a.item_cap) || !fits(sums.y * one, room)) continue;

@@ -16,7 +16,8 @@ def up(a, b):
 def fits(groups, live, shared, own, size, hkv, g):
     rb = up(size * g, 32)
     a, b = groups * hkv * rb, live * hkv
-    most = min(max(up(a * shared + b * own, 1920 if rb > 1 else 1536), 8), 256)
+    work = a * shared + b * own
+    most = min(max(up(work, 1920 if rb > 1 and up(work, 1536) > 62 else 1536), 8), 256)
 
     def splits(pages):
         n = up(pages, most)
