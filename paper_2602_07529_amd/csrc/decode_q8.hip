@@ -353,8 +353,10 @@ __device__ __forceinline__ void run_item(const Q8Cache& c, const int32_t* pages,
 // A wave to a work item: a slice of a group's shared pages against 32 of its (branch, query head) rows of a KV head, or a slice of a branch's
 // own pages against its rows.  WIDE: groups have more rows; their waves read the same pages at about the same time, and what they wait for is
 // memory: each has two pages on their way, so five blocks of rows have ten, of which two are different.  Two groups of 32 over
-// 32768 | 640, 5 heads on one: 88 us; workgroups of a wave to a block that find the pages in the L1 98, the pages in a ring
-// in LDS (80 KB on their way) 95, because the waves of a SIMD then do the same at the same time, 64 rows to a wave 90 to 101.
+// 32768 | 640, 5 heads on one: 83 us (88 when these were built in its place: workgroups of a wave to a block that find the pages in the L1 98, the
+// pages in a ring in LDS, 80 KB on their way, 95, because the waves of a SIMD then do the same at the same time, 64 rows to a wave 90 to 101).
+// The KV head is the fast index, so the blocks of rows of a page meet in one L2 where the heads are a multiple of 8 (the XCDs are eight and take
+// workgroups in turn).  As many bytes in fewer heads come over for several XCDs: 8 heads 218 MiB read, 83 us; 4 350 and 89; 2 617 and 115; 1 733 and 143.
 template <int D, bool WIDE>
 __global__ void __launch_bounds__(64, 2) k_q8_decode(Q8DecodeArgs a) {
   const int lane = threadIdx.x;
