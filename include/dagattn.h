@@ -399,9 +399,8 @@ typedef struct {
  * A run that starts in slot 0 begins the page: what was there is dropped, the scale is that of the new tokens, the slots
  * behind them hold zeros.  Any other run adds to the page, whose slots in front hold tokens.
  * Scale of (page, head): the smallest power of two, 2^-100 at least, with which all new elements of the head are within
- * +-448, or the page's scale so far if that is larger; codes are rounded to nearest even (of a
- * value times the scale's reciprocal, which is exact for powers of two).  When the scale grows, the codes that are there are
- * divided by the same factor and rounded again (exact unless they fall under 2^-6 by it).  An Inf or NaN is stored as NaN and
+ * +-448, or the page's scale so far if that is larger; codes are rounded to nearest even (a value times the scale's reciprocal,
+ * which is exact for powers of two).  When the scale grows, the codes that are there are divided by the same factor and rounded again (exact unless they fall under 2^-6 by it).  An Inf or NaN is stored as NaN and
  * does not count for the scale.  No atomics: the same call gives the same bits.
  * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_HIP. */
 int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new,
@@ -411,8 +410,8 @@ int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int
  * tokens).  q / out [n_live][hq][head_dim] bf16 DEVICE, q already rotated; hq a multiple of kv->hkv, hq / hkv <= 32.
  * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), otherwise every branch is in a
  * group; a branch that sees no token gets zeros.  Slots behind a list's last token may hold any codes; page ids outside the pool are clamped,
- * never followed; a list that is longer than its host bound is read up to the bound.  softmax_scale may be of either sign, or zero; if it is
- * not finite the rows that see a token get NaN.  Sums, maxima and partial results are
+ * never followed; a list that is longer than its host bound is read up to the bound, the other bounds are trusted.  softmax_scale may be of
+ * either sign, or zero; if it is not finite the rows that see a token get NaN.  Sums, maxima and partial results are
  * fp32; probabilities are rounded to bf16 for the second product.  Enqueued on `stream` (two launches; one for short contexts); the call
  * allocates nothing and does not synchronise; calls that overlap need a workspace each. */
 size_t dag_decode_q8_workspace_bytes(const dag_decode_desc_t* desc, int32_t hq, int32_t hkv, int32_t head_dim);
