@@ -424,6 +424,20 @@ size_t dag_decode_segments_q8_workspace_bytes(const dag_decode_seg_desc_t* desc,
 int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* desc, const dag_kv_q8_t* kv, const void* q, void* out, int32_t hq,
                                 float softmax_scale, void* ws, size_t ws_bytes, void* stream);
 
+/* dag_attn_prefill_paged over an 8-bit cache, for any number of new tokens, one too: same description and meaning (new token i of a node sees
+ * the tokens in the pages in front of its own and its own node's tokens 0 .. own_len - n_i + i), q / out [n_rows][hq][head_dim] bf16 DEVICE, q
+ * already rotated, lse NULL or [n_rows][hq] fp32 DEVICE; hq a multiple of kv->hkv, hq / hkv <= 256.  n_rows: HOST, rows of q and out; rows outside
+ * q_off[0] .. q_off[n_nodes] - 1 are left as they are.  Any page of a context may be partly filled or empty (its scales are then not looked at);
+ * slots behind its last token may hold any codes, and what a row does not see does not reach it, whatever it holds; page ids outside the
+ * pool are clamped, never followed; a row that sees no token gets zeros and an lse of minus infinity.  softmax_scale may be of either sign, or zero;
+ * if it is not finite the rows that see a token get NaN.  Sums, maxima and partial results are fp32; probabilities are rounded to bf16 for the
+ * second product.  Enqueued on `stream` (one launch, two where contexts are cut among workgroups); the call allocates nothing and does
+ * not synchronise; calls that overlap need a workspace each (16-byte aligned; may be NULL where no bytes are needed).
+ * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE, DAG_ERR_HIP. */
+size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* desc, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim);
+int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* desc, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
+                              int32_t hq, float softmax_scale, void* ws, size_t ws_bytes, void* stream);
+
 /* Pages of rows that grow, kept on the GPU.  A row is what owns pages: a live branch, a node.  All pointers DEVICE int32.
  * Row r with n tokens holds the first ceil(n / 16) entries of its line of `table`; the first `*free_count` entries of `free_pages` are
  * the pages that nobody holds, taken from the end.  With dag_kv_release and dag_kv_tables a step needs no round trip to the host:

@@ -146,6 +146,10 @@ def lib():
             need, call = getattr(L, "dag_%s_workspace_bytes" % name), getattr(L, "dag_attn_" + name)
             need.argtypes, need.restype = [C.POINTER(desc), i32, i32, i32], C.c_size_t
             call.argtypes = [C.POINTER(desc), C.POINTER(dag_kv_q8_t), vp, vp, i32, f32, vp, C.c_size_t, vp]
+        L.dag_prefill_paged_q8_workspace_bytes.argtypes = [C.POINTER(dag_paged_prefill_desc_t), i64, i32, i32, i32]
+        L.dag_prefill_paged_q8_workspace_bytes.restype = C.c_size_t
+        L.dag_attn_prefill_paged_q8.argtypes = [C.POINTER(dag_paged_prefill_desc_t), C.POINTER(dag_kv_q8_t), vp, i64, vp, vp, i32, f32, vp,
+                                                C.c_size_t, vp]
         L.dag_kv_tables_workspace_bytes.argtypes = [i32]
         L.dag_kv_tables_workspace_bytes.restype = C.c_size_t
         L.dag_kv_release.argtypes = [C.POINTER(dag_kv_rows_t), vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
@@ -164,7 +168,7 @@ def lib():
                      "dag_kv_append_rope", "dag_attn_decode", "dag_attn_decode_static", "dag_attn_decode_segments",
                      "dag_sched_create", "dag_attn_prefill_paged", "dag_copy_calibration",
                      "dag_attn_prefill_bwd", "dag_kv_append_rope_q8", "dag_attn_decode_q8", "dag_attn_decode_segments_q8",
-                     "dag_kv_release", "dag_kv_tables",
+                     "dag_attn_prefill_paged_q8", "dag_kv_release", "dag_kv_tables",
                      "dag_sched_step"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -478,6 +482,18 @@ class PagedPrefillDesc:
                                           int(np.diff(p_off).max()) if n_nodes else 0,
                                           *[self.t[n].data_ptr() for n in _PAGED_ARRAYS])
 
+    @classmethod
+    def on_device(cls, n_nodes, max_new, max_ctx_pages, q_off, ctx_page_off, ctx_pages, ctx_page_len, own_page, own_len):
+        """A description whose arrays are on the device already (int32 tensors, kept alive here), with the host bounds."""
+        self = cls.__new__(cls)
+        self.t = _device_arrays(dict(zip(_PAGED_ARRAYS, (q_off, ctx_page_off, ctx_pages, ctx_page_len, own_page, own_len))), dict(
+            q_off=n_nodes + 1, ctx_page_off=n_nodes + 1, own_page=n_nodes, own_len=n_nodes))
+        if ctx_pages.numel() != ctx_page_len.numel():
+            raise ValueError("ctx_pages and ctx_page_len are of one length")
+        self.n_rows = None  # (known on the device only)
+        self.c = dag_paged_prefill_desc_t(n_nodes, PAGE, max_new, max_ctx_pages, *[x.data_ptr() for x in self.t.values()])
+        return self
+
 
 def dag_prefill_paged_workspace_bytes(pdesc):
     return int(lib().dag_prefill_paged_workspace_bytes(C.byref(pdesc.c)))
@@ -569,6 +585,27 @@ def dag_attn_decode_q8(ddesc, q, cache, out, workspace, softmax_scale=None):
 
 def dag_attn_decode_segments_q8(sdesc, q, cache, out, workspace, softmax_scale=None):
     _decode_q8(lib().dag_attn_decode_segments_q8, sdesc, q, cache, out, workspace, softmax_scale)
+
+
+def dag_prefill_paged_q8_workspace_bytes(pdesc, cache, n_rows, hq):
+    return lib().dag_prefill_paged_q8_workspace_bytes(C.byref(pdesc.c), n_rows, hq, cache.hkv, cache.head_dim)
+
+
+def dag_attn_prefill_paged_q8(pdesc, q, cache, out, workspace, lse=None, softmax_scale=None):
+    n, hq, d = q.shape
+    if d != cache.head_dim or out.shape != q.shape:
+        raise ValueError("q and out are [rows][heads][head_dim]")
+    if pdesc.n_rows is not None and pdesc.n_rows > n:
+        raise ValueError("q has %d rows, not the %d of the description" % (n, pdesc.n_rows))
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or not q.is_contiguous() or not out.is_contiguous():
+        raise TypeError("q and out are contiguous bfloat16")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        raise TypeError("lse is contiguous float32 [rows][heads]")
+    more = (workspace,) if lse is None else (workspace, lse)
+    _check(lib().dag_attn_prefill_paged_q8(
+        C.byref(pdesc.c), cache.ref, q.data_ptr(), n, out.data_ptr(), None if lse is None else lse.data_ptr(), hq,
+        d ** -0.5 if softmax_scale is None else softmax_scale, workspace.data_ptr(), workspace.numel(),
+        _here(q, out, cache.k_pool, pdesc.t["q_off"], *more)))
 
 
 class KvRows:

@@ -17,17 +17,10 @@
 
 #include "common.h"
 #include "decode_plan.h"
+#include "q8_ops.h"
 #include "seg_plan.h"
 
 namespace {
-
-struct Q8Cache {
-  const uint8_t* k_pool;
-  const uint8_t* v_pool;
-  const float* k_scale;
-  const float* v_scale;
-  int n_pages, hkv;
-};
 
 struct Q8DecodeArgs {
   Q8Cache kv;
@@ -55,33 +48,12 @@ struct Q8SegArgs {
   int most;  // tokens of a segment by the host's bound
 };
 
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
-// Eight codes as bf16 (exact: e4m3 has four significant bits).
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi) {
-  u32x4 x;
-  x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
-  x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
-  x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
-  x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
-  return __builtin_bit_cast(bf16x8, x);
-}
-
-__device__ __forceinline__ float other_half(float x) { return __uint_as_float(dag_other_group<32>(__float_as_uint(x))); }  // of lane ^ 32
-
 template <int D>
 struct Block {         // 32 keys (two pages)
   u32x4 k[D / 32];     // k[s]: dims 16 (2 s + H) .. of the key of MFMA row L
   u32x4 v[D / 32];     // v[db]: the slots of page H of dimension 32 db + L
 };
 
-template <bool ONCE>
-__device__ __forceinline__ u32x4 load16(const uint8_t* p) {  // ONCE: passes the caches by
-  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4*)p);
-  else return *(const u32x4*)p;
-}
 // pages: of 64 pages, a lane each; rel, rel + 1: the two of the block, last: the slice's last one
 template <int D, bool ONCE>
 __device__ __forceinline__ void load_block(Block<D>& b, const Q8Cache& c, int pages, int rel, int last, int hk, int L, int H) {
@@ -278,23 +250,6 @@ __device__ __forceinline__ void stream_slice(const Q8Cache& c, const int32_t* pa
   }
 }
 
-// Query operands of the lane's row: step 2 s + u has dims 16 (2 s + H) + 8 u .., with the sign of the softmax scale.
-template <int D>
-__device__ __forceinline__ void fetch_q(bf16x8 (&q)[D / 16], const uint16_t* row, int lane) {
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) q[s] = *(const bf16x8*)(row + 16 * (lane >> 5) + 32 * (s >> 1) + 8 * (s & 1));
-}
-template <int D>
-__device__ __forceinline__ void sign_q(bf16x8 (&q)[D / 16], float sc) {
-  const uint32_t sign = sc < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    u32x4 x = __builtin_bit_cast(u32x4, q[s]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] ^= sign;
-    q[s] = __builtin_bit_cast(bf16x8, x);
-  }
-}
 template <int D>
 __device__ __forceinline__ void load_q(bf16x8 (&q)[D / 16], const uint16_t* row, float sc, int lane) {
   fetch_q<D>(q, row, lane);

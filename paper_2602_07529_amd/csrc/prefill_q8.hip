@@ -1,0 +1,427 @@
+// dag_attn_prefill_paged_q8: the new tokens of nodes against the pages of their contexts in an 8-bit cache.
+//
+// out_i = sum_j p_ij v_j / sum_j p_ij with p_ij = exp(scale q_i . k_j), over the slots j of the node's list of pages that hold a token and do
+// not lie behind new token i.  A code c of a page stands for its scale times c; the key scale goes into the exponent,
+// t_j = (scale log2(e) s) q . c_j, and so does the value scale z, p'_j = 2^(t_j - m + log2 z), which the sum of the probabilities
+// takes out again.
+//
+// A work item is 32 NW (row, query head) pairs of a node and KV head, row after row, against a stretch of its pages, 32 pairs to a wave.  A tile is
+// four pages: the threads fetch the codes of the tile after next into registers, put those of the next one into LDS (keys as they are,
+// values as bf16) and work on the present one.
+#include <algorithm>
+
+#include "common.h"
+#include "q8_ops.h"
+
+namespace {
+
+constexpr int PAGE = DAG_PAGE_SIZE;
+constexpr int TILE = 4;          // pages
+constexpr int MAX_SPLITS = 64;   // (the lanes of the wave that puts them together)
+constexpr int WAVES = 4;
+
+struct ChunkArgs {
+  Q8Cache kv;
+  const int32_t* q_off;
+  const int32_t* ctx_page_off;
+  const int32_t* ctx_pages;
+  const int32_t* ctx_page_len;
+  const int32_t* own_page;
+  const int32_t* own_len;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  float* part_o;   // [slot][KV head][split][pair][D]
+  float* part_ml;  // the same [2]: reference in the exponent's units, sum
+  int n_nodes, n_rows, max_new, max_ctx_pages, hq, G;
+  int splits, slice;  // stretches of a context, tiles in each
+  float sc;           // softmax_scale * log2(e)
+};
+
+// What a slot of the launch is: slot x holds pairs 32 NW (x - first slot of the node) .. of the node with the largest first slot up to x,
+// the first slot of node i being floor(G q_off[i] / 32 NW) + i: as many as its pairs fill, and known without a scan.
+struct Place {
+  int row0, n, pair0, pages, np, nstart;
+};
+__device__ __forceinline__ int64_t first_row(const ChunkArgs& a, int i) { return min(max(a.q_off[i], 0), a.n_rows); }
+template <int PAIRS>
+__device__ __forceinline__ bool find_place(const ChunkArgs& a, int64_t slot, int lane, Place* p) {
+  int lo = 0, hi = a.n_nodes;
+  while (hi > lo) {  // 64 nodes of [lo, hi) a turn; the last one whose first slot is not behind
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool ok = i < hi && lane * (int64_t)step < hi - lo && first_row(a, i) * a.G / PAIRS + i <= slot;
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(ok));
+    if (n == 0) return false;
+    lo += (n - 1) * step;
+    hi = min(hi, lo + step);
+    if (step == 1) break;
+  }
+  const int64_t r0 = first_row(a, lo);
+  p->n = (int)min(first_row(a, lo + 1) - r0, (int64_t)a.max_new);
+  p->row0 = (int)r0;
+  const int64_t pair0 = (slot - (r0 * a.G / PAIRS + lo)) * PAIRS;
+  if (pair0 >= (int64_t)p->n * a.G) return false;
+  p->pair0 = (int)pair0;
+  p->pages = a.ctx_page_off[lo];
+  p->np = min(max(a.ctx_page_off[lo + 1] - p->pages, 0), a.max_ctx_pages);
+  p->nstart = a.own_page[lo] * PAGE + a.own_len[lo] - (int)(first_row(a, lo + 1) - r0);
+  return true;
+}
+
+__device__ __forceinline__ void lds_barrier() {  // (loads from memory stay on their way)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int D, int NW>
+struct Lds {
+  static constexpr int KPAGE = D * PAGE + 128;  // the two pages that 16 lanes read together start half the banks apart
+  uint8_t k[2][TILE * KPAGE];
+  uint8_t v[2][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
+  f32x4 page[2][TILE];                // key scale with the softmax's, log2 of the value scale and the inverse of that scale, tokens
+};
+
+template <int D, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
+  constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = 2 * TILE * D / THREADS;  // 16-byte pieces of a tile to a thread
+  static_assert(PIECES >= 1, "");
+  __shared__ __attribute__((aligned(16))) Lds<D, NW> lds;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, L = lane & 31, H = lane >> 5;
+  const int hkv = a.kv.hkv, hk = blockIdx.x % hkv, split = blockIdx.x / hkv % a.splits;
+  const int64_t slot = blockIdx.x / hkv / a.splits;
+  Place pl;
+  if (!find_place<PAIRS>(a, slot, lane, &pl)) return;
+  const int n_pairs = min(PAIRS, pl.n * a.G - pl.pair0);
+  const int pair = min(pl.pair0 + 32 * w + L, pl.n * a.G - 1), row = pair / a.G, head = hk * a.G + pair % a.G;
+  const int lim = pl.nstart + row;  // the last place that the row sees
+  const int lim_first = pl.nstart + min(pl.pair0 + 32 * w, pl.n * a.G - 1) / a.G;
+  const int lim_last = pl.nstart + (pl.pair0 + n_pairs - 1) / a.G;
+  const int nt = lim_last < 0 ? 0 : min((pl.np + TILE - 1) / TILE, lim_last / (TILE * PAGE) + 1);
+  const int t0 = min(split * a.slice, nt), t1 = min(t0 + a.slice, nt);
+
+  bf16x8 q[D / 16];
+  fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
+  f32x16 O[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+  float m = -1e30f, l = 0.f;
+
+  if (t0 < t1) {
+    sign_q<D>(q, a.sc);
+    // ids and tokens of 64 pages, a lane each, and of the 64 behind them
+    int win_pg, win_len, next_pg, next_len;
+    auto ask = [&](int rel) __attribute__((always_inline)) {
+      const int i = rel + lane;
+      next_pg = a.ctx_pages[(size_t)pl.pages + min(i, pl.np - 1)];
+      next_len = i < pl.np ? a.ctx_page_len[(size_t)pl.pages + min(i, pl.np - 1)] : 0;
+    };
+    auto have = [&]() __attribute__((always_inline)) {
+      win_pg = min(max(next_pg, 0), a.kv.n_pages - 1);
+      win_len = min(max(next_len, 0), PAGE);
+    };
+    u32x4 piece[PIECES];
+    int held[PIECES];
+    float ks = 0.f, vs = 0.f;
+    int len = 0;
+    auto piece_at = [&](int i) __attribute__((always_inline)) { return w * 64 + i * THREADS; };  // its first lane's
+    auto load = [&](int t) __attribute__((always_inline)) {  // tile t of the stretch
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int x = piece_at(i) % (TILE * D), j = x / D, at = (TILE * t + j) & 63;
+        const int pg = __builtin_amdgcn_readlane(win_pg, at);
+        held[i] = __builtin_amdgcn_readlane(win_len, at);
+        const uint8_t* const pool = piece_at(i) < TILE * D ? a.kv.k_pool : a.kv.v_pool;
+        piece[i] = *(const u32x4*)(pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (x % D + lane) * 16);
+      }
+      const int at = (TILE * t + min(w, TILE - 1)) & 63;
+      const size_t ph = (size_t)__builtin_amdgcn_readlane(win_pg, at) * hkv + hk;
+      len = __builtin_amdgcn_readlane(win_len, at);
+      ks = a.kv.k_scale[ph];
+      vs = a.kv.v_scale[ph];
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int x = piece_at(i) % (TILE * D), j = x / D;
+        if (piece_at(i) < TILE * D) {
+          *(u32x4*)(lds.k[buf] + j * lds.KPAGE + (x % D + lane) * 16) = piece[i];
+        } else {
+          u32x4 c = piece[i];
+          if (held[i] < PAGE) {  // slots without a token may hold any codes
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int n = held[i] - 4 * e;
+              c[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
+            }
+          }
+          uint8_t* const to = lds.v[buf] + j * (D * 32) + (x % D + lane) * 16;
+          *(bf16x8*)to = codes_to_bf16(c[0], c[1]);
+          *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
+        }
+      }
+      if (w < TILE && lane == 0) {
+        float k = ks * fabsf(a.sc), z = __builtin_amdgcn_logf(vs);
+        k = k < 1.2e-38f ? 1.2e-38f : k;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
+        if (len == 0) k = 1.f, z = 0.f;   // (scales of a page without tokens)
+        lds.page[buf][w] = f32x4{k, z, __builtin_amdgcn_exp2f(-z), __int_as_float(len)};
+      }
+    };
+    auto compute = [&](int t, int buf) __attribute__((always_inline)) {  // tile t of the context
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 page = lds.page[buf][2 * b + H];
+        float pks = page[0], plv = page[1], inv = page[2];
+        const int plen = __float_as_int(page[3]), pos = (TILE * t + 2 * b + H) * PAGE;
+        f32x16 S;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = 0.f;
+        const uint8_t* const kp = lds.k[buf] + (2 * b + (L >> 2 & 1)) * lds.KPAGE + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          const u32x4 c = *(const u32x4*)(kp + s * 512);
+          S = mfma32(codes_to_bf16(c[0], c[1]), q[2 * s], S);
+          S = mfma32(codes_to_bf16(c[2], c[3]), q[2 * s + 1], S);
+        }
+        const bool masked = __builtin_amdgcn_ballot_w64(plen < PAGE || pos + PAGE - 1 > lim_first) != 0;
+        if (masked) {
+          const int n = min(plen, lim - pos + 1);  // slots that the row sees
+#pragma unroll
+          for (int r = 0; r < 16; ++r) S[r] = r < n ? S[r] : -INFINITY;
+          if (n <= 0) pks = 1.f, plv = 0.f, inv = 1.f;
+        }
+        float bm = S[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
+        bm *= pks;
+        bm = fmaxf(bm, other_half(bm));
+        if (__builtin_amdgcn_ballot_w64(bm > m + 3.f) != 0) {
+          const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
+          l *= alpha;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
+          m = m_new;
+        }
+        const float ref = plv - m;
+        f32x8 x[2];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref));
+          sum[r >> 3] += x[r >> 3][r & 7];
+        }
+        l = fmaf(sum[0] + sum[1], inv, l);
+        // (rounded to bf16, as the probabilities over a bf16 cache are)
+        const bf16x8 p[2] = {__builtin_convertvector(x[0], bf16x8), __builtin_convertvector(x[1], bf16x8)};
+        const uint8_t* const vp = lds.v[buf] + (2 * b + H) * (D * 32) + L * 16;
+        if (masked) {
+          // A value that is no number may not reach the rows that do not see it, and a probability of zero does not keep it from them: such
+          // values are cleared, and the sums of the rows that see one become no number, found by a product of "is none" and "is seen".
+          f32x8 seen[2];
+          const int n = min(plen, lim - pos + 1);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) seen[r >> 3][r & 7] = r < n ? 1.f : 0.f;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) {
+            u32x4 v[2], none[2];
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              v[e] = *(const u32x4*)(vp + e * (D * 16) + db * 512);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = (v[e][i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (v[e][i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                none[e][i] = (lo | hi) & 0x3f803f80u;  // one
+                v[e][i] &= ~(lo | hi);
+                any |= lo | hi;
+              }
+            }
+            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+              f32x16 c;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) c[r] = 0.f;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) c = mfma32(__builtin_bit_cast(bf16x8, none[e]), __builtin_convertvector(seen[e], bf16x8), c);
+#pragma unroll
+              for (int r = 0; r < 16; ++r) O[db][r] = c[r] > 0.f ? NAN : O[db][r];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) O[db] = mfma32(__builtin_bit_cast(bf16x8, v[e]), p[e], O[db]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), p[e], O[db]);
+        }
+      }
+    };
+
+    const int n = t1 - t0, page0 = TILE * t0;
+    ask(page0);
+    have();
+    ask(page0 + 64);
+    load(0);
+    store(0);
+    // (what is loaded behind the stretch is never used: its pages are those of the list, or the last one again)
+    load(1);
+    lds_barrier();
+    for (int i = 0; i < n; ++i) {
+      store((i + 1) & 1);
+      if (((i + 2) * TILE & 63) == 0) {
+        have();
+        ask(page0 + (i + 2) * TILE + 64);
+      }
+      load(i + 2);
+      compute(t0 + i, i & 1);
+      lds_barrier();
+    }
+    l += other_half(l);
+  }
+
+  if (32 * w + L >= n_pairs) return;
+  if (a.splits > 1) {
+    const size_t at = (((size_t)slot * hkv + hk) * a.splits + split) * PAIRS + 32 * w + L;
+    float* const po = a.part_o + at * D;
+    if (t0 < t1)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *(f32x4*)(po + 32 * db + 8 * r + 4 * H) = f32x4{O[db][4 * r], O[db][4 * r + 1], O[db][4 * r + 2], O[db][4 * r + 3]};
+    if (H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(m, l);
+    return;
+  }
+  const size_t at = (size_t)(pl.row0 + row) * a.hq + head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      u32x2 y;
+      y[0] = dag_pack_bf2(O[db][4 * r] * inv, O[db][4 * r + 1] * inv);
+      y[1] = dag_pack_bf2(O[db][4 * r + 2] * inv, O[db][4 * r + 3] * inv);
+      *(u32x2*)(a.out + at * D + 32 * db + 8 * r + 4 * H) = y;
+    }
+  if (a.lse && H == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+// Puts the stretches of a context together, in their order: a wave to a pair, a lane to a stretch and then to D / 64 dims.
+template <int D, int NW>
+__global__ void __launch_bounds__(256) k_q8_chunk_merge(ChunkArgs a) {
+  constexpr int PAIRS = 32 * NW, EACH = D / 64;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hkv = a.kv.hkv;
+  const int part = blockIdx.x % (PAIRS / 4), hk = blockIdx.x / (PAIRS / 4) % hkv;
+  const int64_t slot = blockIdx.x / (PAIRS / 4) / hkv;
+  Place pl;
+  if (!find_place<PAIRS>(a, slot, lane, &pl)) return;
+  const int mine = part * 4 + w, pair = pl.pair0 + mine;
+  if (pair >= pl.n * a.G) return;
+  const size_t at = ((size_t)slot * hkv + hk) * a.splits * PAIRS + mine;
+  float2 ml = make_float2(-1e30f, 0.f);
+  if (lane < a.splits) ml = *(const float2*)(a.part_ml + (at + (size_t)lane * PAIRS) * 2);
+  const float top = dag_wave_max(ml.y != 0.f ? ml.x : -1e30f), weight = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+  const float total = dag_wave_sum(ml.y * weight);
+  float o[EACH] = {};
+  for (uint64_t rest = __builtin_amdgcn_ballot_w64(ml.y != 0.f); rest; rest &= rest - 1) {
+    const int s = __builtin_ctzll(rest);
+    const float f = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), s));
+    const float* const from = a.part_o + (at + (size_t)s * PAIRS) * D + EACH * lane;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] = fmaf(from[e], f, o[e]);
+  }
+  const int row = pair / a.G, head = hk * a.G + pair % a.G;
+  const size_t to = (size_t)(pl.row0 + row) * a.hq + head;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  if constexpr (EACH == 2) *(uint32_t*)(a.out + to * D + 2 * lane) = dag_pack_bf2(o[0] * inv, o[EACH - 1] * inv);
+  else a.out[to * D + lane] = (uint16_t)dag_pack_bf2(o[0] * inv, 0.f);
+  if (a.lse && lane == 0) a.lse[to] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
+struct Plan {
+  int64_t slots;
+  int splits, slice;
+};
+// By the host's bounds.  Compute units of the device with two workgroups each; contexts are cut while there are fewer items than that.
+bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, int pairs, Plan* p) {
+  const int64_t G = hq / hkv, tiles = dag_ceil_div(d->max_ctx_pages, TILE);
+  p->slots = d->max_new == 0 || d->n_nodes == 0 ? 0 : n_rows * G / pairs + d->n_nodes;  // (the last node's last one is below: find_place)
+  const int64_t items = p->slots * hkv, at_once = 512;
+  int64_t splits = 1;
+  if (items > 0 && items < at_once) splits = std::min<int64_t>({at_once / items, dag_ceil_div(tiles, 4), MAX_SPLITS});
+  splits = std::max<int64_t>(1, splits);
+  p->slice = (int)std::max<int64_t>(1, dag_ceil_div(tiles, splits));
+  p->splits = (int)std::max<int64_t>(1, dag_ceil_div(tiles, p->slice));
+  return p->slots * hkv * p->splits <= (int64_t)1 << 23 && p->slots * hkv * (p->splits > 1 ? pairs / 4 : 1) <= (int64_t)1 << 23;  // (threads are counted in 32 bits)
+}
+
+bool bounds_ok(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim) {
+  return d && d->n_nodes >= 0 && d->max_new >= 0 && d->max_ctx_pages >= 0 && d->max_ctx_pages <= (1 << 26) && n_rows >= 0 && n_rows <= INT32_MAX && hkv >= 1 &&
+         hq >= 1 && hq % hkv == 0 && hq / hkv <= 256 && (int64_t)d->max_new * (hq / hkv) <= INT32_MAX && (head_dim == 64 || head_dim == 128);
+}
+
+template <int D>
+int launch(const ChunkArgs& a, const Plan& p, hipStream_t stream) {
+  hipLaunchKernelGGL((k_q8_chunk<D, WAVES>), dim3((unsigned)(p.slots * a.kv.hkv * p.splits)), dim3(64 * WAVES), 0, stream, a);
+  DAG_LAUNCH_CHECK();
+  if (p.splits > 1) {
+    hipLaunchKernelGGL((k_q8_chunk_merge<D, WAVES>), dim3((unsigned)(p.slots * a.kv.hkv * (32 * WAVES / 4))), dim3(256), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+  }
+  return DAG_OK;
+}
+
+size_t part_count(const Plan& p, int hkv, int pairs) { return p.splits > 1 ? (size_t)p.slots * hkv * p.splits * pairs : 0; }
+
+}  // namespace
+
+extern "C" size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim) {
+  Plan p;
+  if (!bounds_ok(d, n_rows, hq, hkv, head_dim) || d->page_size != PAGE || !plan(d, n_rows, hq, hkv, 32 * WAVES, &p)) return 0;
+  return part_count(p, hkv, 32 * WAVES) * (head_dim + 2) * sizeof(float);
+}
+
+extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
+                                         int32_t hq, float softmax_scale, void* ws, size_t ws_bytes, void* stream_) {
+  if (!d || !kv) return DAG_ERR_NULL;
+  if (d->n_nodes < 0 || d->max_new < 0 || d->max_ctx_pages < 0 || kv->n_pages < 0 || n_rows < 0) return DAG_ERR_BAD_LEN;
+  Plan p;
+  if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, 32 * WAVES, &p)) return DAG_ERR_UNSUPPORTED;
+  if (p.slots == 0 || n_rows == 0) return DAG_OK;  // no new token anywhere
+  const bool pages = d->max_ctx_pages > 0;
+  if (pages && kv->n_pages == 0) return DAG_ERR_BAD_LEN;
+  if (!q || !out || !d->q_off || !d->ctx_page_off || !d->own_page || !d->own_len) return DAG_ERR_NULL;
+  if (pages && (!d->ctx_pages || !d->ctx_page_len || !kv->k_pool || !kv->v_pool || !kv->k_scale || !kv->v_scale)) return DAG_ERR_NULL;
+  if (!dag_aligned16(q) || !dag_aligned16(out) || !dag_aligned16(kv->k_pool) || !dag_aligned16(kv->v_pool) || ((uintptr_t)kv->k_scale & 3) ||
+      ((uintptr_t)kv->v_scale & 3) || ((uintptr_t)lse & 3))
+    return DAG_ERR_ALIGN;
+  const size_t parts = part_count(p, kv->hkv, 32 * WAVES);
+  if (parts > 0 && (!ws || ws_bytes < parts * (kv->head_dim + 2) * sizeof(float))) return DAG_ERR_WORKSPACE;
+  if (parts > 0 && !dag_aligned16(ws)) return DAG_ERR_ALIGN;
+  ChunkArgs a = {};
+  a.kv = Q8Cache{(const uint8_t*)kv->k_pool, (const uint8_t*)kv->v_pool, kv->k_scale, kv->v_scale, kv->n_pages, kv->hkv};
+  a.q_off = d->q_off;
+  a.ctx_page_off = d->ctx_page_off;
+  a.ctx_pages = d->ctx_pages;
+  a.ctx_page_len = d->ctx_page_len;
+  a.own_page = d->own_page;
+  a.own_len = d->own_len;
+  a.q = (const uint16_t*)q;
+  a.out = (uint16_t*)out;
+  a.lse = lse;
+  a.part_o = (float*)ws;
+  a.part_ml = a.part_o + parts * kv->head_dim;
+  a.n_nodes = d->n_nodes;
+  a.n_rows = (int)n_rows;
+  a.max_new = d->max_new;
+  a.max_ctx_pages = d->max_ctx_pages;
+  a.hq = hq;
+  a.G = hq / kv->hkv;
+  a.splits = p.splits;
+  a.slice = p.slice;
+  a.sc = softmax_scale * 1.4426950408889634f;
+  return kv->head_dim == 128 ? launch<128>(a, p, (hipStream_t)stream_) : launch<64>(a, p, (hipStream_t)stream_);
+}
