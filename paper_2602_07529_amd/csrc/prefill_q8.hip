@@ -9,12 +9,14 @@
 // four pages: the threads fetch the codes of the tile after next into registers, put those of the next one into LDS (keys as they are,
 // values as bf16) and work on the present one.
 #include <algorithm>
+#include <cmath>
 
 #include "common.h"
 #include "q8_ops.h"
 
 namespace {
 
+typedef __attribute__((ext_vector_type(8))) int i32x8;
 constexpr int PAGE = DAG_PAGE_SIZE;
 constexpr int TILE = 4;          // pages
 constexpr int MAX_SPLITS = 64;   // (the lanes of the wave that puts them together)
@@ -77,14 +79,65 @@ __device__ __forceinline__ void lds_barrier() {  // (loads from memory stay on t
 template <int D, int NW>
 struct Lds {
   static constexpr int KPAGE = D * PAGE + 128;  // the two pages that 16 lanes read together start half the banks apart
+  static constexpr int VWAVES = TILE * D / 64;  // wave-level pieces of the values of a tile
   uint8_t k[2][TILE * KPAGE];
   uint8_t v[2][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
-  f32x4 page[2][TILE];                // key scale with the softmax's, log2 of the value scale and the inverse of that scale, tokens
+  f32x4 page[4][TILE];                // key scale with the softmax's, log2 of the value scale and the inverse of that scale, tokens
+  int none[2][VWAVES];                // whether a piece of the values holds codes that are no number
+  int ids[4][TILE];
 };
+
+// Query operands in 8 bits: q = 2^e (a + 2^-5 b) with a and b in e4m3, e the row's: a has the first four significant bits of an element, b the
+// other four.  Exact for elements down to 2^-14 of the row's largest, below that off by at most 2^-22 of it.
+template <int D>
+struct QueryCodes {
+  i32x8 a[D / 64], b[D / 64];
+  int ea, eb;  // scale bytes
+};
+template <int D>
+__device__ __forceinline__ void split_q(QueryCodes<D>& y, const bf16x8 (&q)[D / 16]) {
+  float most = 0.f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const u32x4 x = __builtin_bit_cast(u32x4, q[s]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = fabsf(dag_bf_lo(x[i])), hi = fabsf(dag_bf_hi(x[i]));
+      most = fmaxf(most, fmaxf(lo < INFINITY ? lo : 0.f, hi < INFINITY ? hi : 0.f));
+    }
+  }
+  most = fmaxf(most, other_half(most));
+  const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 7, -100);  // largest element in [128, 256)
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const u32x4 x = __builtin_bit_cast(u32x4, q[s]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f[2 * j] = dag_bf_lo(x[2 * i + j]) * inv;
+        f[2 * j + 1] = dag_bf_hi(x[2 * i + j]) * inv;
+      }
+      int wa = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+      wa = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], wa, true);
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(wa, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(wa, true);
+      int wb = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - lo[0]) * 32.f, (f[1] - lo[1]) * 32.f, 0, false);
+      wb = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - hi[0]) * 32.f, (f[3] - hi[1]) * 32.f, wb, true);
+      y.a[s / 4][2 * (s % 4) + i] = wa;
+      y.b[s / 4][2 * (s % 4) + i] = wb;
+    }
+  }
+  y.ea = 127 + e;
+  y.eb = 127 + e - 5;
+}
+
+constexpr float TOP_SUM = 1073741824.f;  // of a block's probabilities relative to the reference: 2^30
 
 template <int D, int NW>
 __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
-  constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = 2 * TILE * D / THREADS;  // 16-byte pieces of a tile to a thread
+  constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = TILE * D / THREADS;  // 16-byte pieces of the keys of a tile to a thread
   static_assert(PIECES >= 1, "");
   __shared__ __attribute__((aligned(16))) Lds<D, NW> lds;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, L = lane & 31, H = lane >> 5;
@@ -100,8 +153,6 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
   const int nt = lim_last < 0 ? 0 : min((pl.np + TILE - 1) / TILE, lim_last / (TILE * PAGE) + 1);
   const int t0 = min(split * a.slice, nt), t1 = min(t0 + a.slice, nt);
 
-  bf16x8 q[D / 16];
-  fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
   f32x16 O[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -110,7 +161,13 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
   float m = -1e30f, l = 0.f;
 
   if (t0 < t1) {
-    sign_q<D>(q, a.sc);
+    QueryCodes<D> q;
+    {
+      bf16x8 x[D / 16];
+      fetch_q<D>(x, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
+      sign_q<D>(x, a.sc);
+      split_q<D>(q, x);
+    }
     // ids and tokens of 64 pages, a lane each, and of the 64 behind them
     int win_pg, win_len, next_pg, next_len;
     auto ask = [&](int rel) __attribute__((always_inline)) {
@@ -122,164 +179,207 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       win_pg = min(max(next_pg, 0), a.kv.n_pages - 1);
       win_len = min(max(next_len, 0), PAGE);
     };
-    u32x4 piece[PIECES];
+    u32x4 kpiece[PIECES], vpiece[PIECES];
     int held[PIECES];
     float ks = 0.f, vs = 0.f;
-    int len = 0;
-    auto piece_at = [&](int i) __attribute__((always_inline)) { return w * 64 + i * THREADS; };  // its first lane's
-    auto load = [&](int t) __attribute__((always_inline)) {  // tile t of the stretch
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int x = piece_at(i) % (TILE * D), j = x / D, at = (TILE * t + j) & 63;
-        const int pg = __builtin_amdgcn_readlane(win_pg, at);
-        held[i] = __builtin_amdgcn_readlane(win_len, at);
-        const uint8_t* const pool = piece_at(i) < TILE * D ? a.kv.k_pool : a.kv.v_pool;
-        piece[i] = *(const u32x4*)(pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (x % D + lane) * 16);
-      }
-      const int at = (TILE * t + min(w, TILE - 1)) & 63;
-      const size_t ph = (size_t)__builtin_amdgcn_readlane(win_pg, at) * hkv + hk;
-      len = __builtin_amdgcn_readlane(win_len, at);
-      ks = a.kv.k_scale[ph];
-      vs = a.kv.v_scale[ph];
+    int len = 0, id = 0;
+    auto fetch = [&](const uint8_t* pool, int t, int i, u32x4& to, int* n) __attribute__((always_inline)) {
+      const int x = w * 64 + i * THREADS, j = x / D, at = (TILE * t + j) & 63;
+      const int pg = __builtin_amdgcn_readlane(win_pg, at);
+      if (n) *n = __builtin_amdgcn_readlane(win_len, at);
+      to = *(const u32x4*)(pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (uint32_t)((x % D + lane) * 16));
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
+    auto load_k = [&](int t) __attribute__((always_inline)) {  // tile t of the context
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) fetch(a.kv.k_pool, t, i, kpiece[i], nullptr);
+      const int at = (TILE * t + (w & (TILE - 1))) & 63;
+      id = __builtin_amdgcn_readlane(win_pg, at);
+      len = __builtin_amdgcn_readlane(win_len, at);
+      ks = a.kv.k_scale[(size_t)id * hkv + hk];
+      vs = a.kv.v_scale[(size_t)id * hkv + hk];
+    };
+    auto load_v = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) fetch(a.kv.v_pool, t, i, vpiece[i], &held[i]);
+    };
+    auto store_k = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int x = piece_at(i) % (TILE * D), j = x / D;
-        if (piece_at(i) < TILE * D) {
-          *(u32x4*)(lds.k[buf] + j * lds.KPAGE + (x % D + lane) * 16) = piece[i];
-        } else {
-          u32x4 c = piece[i];
-          if (held[i] < PAGE) {  // slots without a token may hold any codes
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int n = held[i] - 4 * e;
-              c[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
-            }
-          }
-          uint8_t* const to = lds.v[buf] + j * (D * 32) + (x % D + lane) * 16;
-          *(bf16x8*)to = codes_to_bf16(c[0], c[1]);
-          *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
-        }
+        const int x = w * 64 + i * THREADS;
+        *(u32x4*)(lds.k[t & 1] + x / D * lds.KPAGE + (x % D + lane) * 16) = kpiece[i];
       }
       if (w < TILE && lane == 0) {
         float k = ks * fabsf(a.sc), z = __builtin_amdgcn_logf(vs);
         k = k < 1.2e-38f ? 1.2e-38f : k;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
         if (len == 0) k = 1.f, z = 0.f;   // (scales of a page without tokens)
-        lds.page[buf][w] = f32x4{k, z, __builtin_amdgcn_exp2f(-z), __int_as_float(len)};
+        lds.page[t & 3][w] = f32x4{k, z, __builtin_amdgcn_exp2f(-z), __int_as_float(len)};
+        lds.ids[t & 3][w] = id;
       }
     };
-    auto compute = [&](int t, int buf) __attribute__((always_inline)) {  // tile t of the context
+    auto store_v = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int x = w * 64 + i * THREADS;
+        u32x4 c = vpiece[i];
+        if (held[i] < PAGE) {  // slots without a token may hold any codes
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int n = held[i] - 4 * e;
+            c[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
+          }
+        }
+        // Codes that are no number enter as zeros; rows that see one get what they make of it from mark_none.
+        uint32_t any = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= (c[e] & 0x7f7f7f7fu) + 0x01010101u;
+        const bool none = __builtin_amdgcn_ballot_w64((any & 0x80808080u) != 0) != 0;
+        if (none) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[e] &= ~(((((c[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+        }
+        if (lane == 0) lds.none[t & 1][x / 64] = none;
+        uint8_t* const to = lds.v[t & 1] + x / D * (D * 32) + (x % D + lane) * 16;
+        *(bf16x8*)to = codes_to_bf16(c[0], c[1]);
+        *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
+      }
+    };
+    // The sums of the rows that see a value that is no number become no number: a product of "is none" and "is seen" finds them.
+    auto mark_none = [&](int t) __attribute__((always_inline)) {
+#pragma unroll 1
       for (int b = 0; b < 2; ++b) {
-        const f32x4 page = lds.page[buf][2 * b + H];
-        float pks = page[0], plv = page[1], inv = page[2];
-        const int plen = __float_as_int(page[3]), pos = (TILE * t + 2 * b + H) * PAGE;
-        f32x16 S;
+        const int pg = lds.ids[t & 3][2 * b + H], n = min(__float_as_int(lds.page[t & 3][2 * b + H][3]), lim - (TILE * t + 2 * b + H) * PAGE + 1);
+        f32x8 seen[2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[r] = 0.f;
-        const uint8_t* const kp = lds.k[buf] + (2 * b + (L >> 2 & 1)) * lds.KPAGE + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16;
+        for (int r = 0; r < 16; ++r) seen[r >> 3][r & 7] = r < n ? 1.f : 0.f;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-          const u32x4 c = *(const u32x4*)(kp + s * 512);
-          S = mfma32(codes_to_bf16(c[0], c[1]), q[2 * s], S);
-          S = mfma32(codes_to_bf16(c[2], c[3]), q[2 * s + 1], S);
+        for (int db = 0; db < D / 32; ++db) {
+          u32x4 c = *(const u32x4*)(a.kv.v_pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (32 * db + L) * 16);
+          f32x16 s;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[e] = ((((c[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0x38u;  // the code of one
+          s = mfma32(codes_to_bf16(c[0], c[1]), __builtin_convertvector(seen[0], bf16x8), s);
+          s = mfma32(codes_to_bf16(c[2], c[3]), __builtin_convertvector(seen[1], bf16x8), s);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[db][r] = s[r] > 0.f ? NAN : O[db][r];
         }
-        const bool masked = __builtin_amdgcn_ballot_w64(plen < PAGE || pos + PAGE - 1 > lim_first) != 0;
-        if (masked) {
-          const int n = min(plen, lim - pos + 1);  // slots that the row sees
+      }
+    };
+    const int koff = (L >> 2 & 1) * lds.KPAGE + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = H * (D * 32) + L * 16;
+    auto scores = [&](f32x16& S, int t, int b) __attribute__((always_inline)) {
+      const uint8_t* const kp = lds.k[t & 1] + 2 * b * lds.KPAGE + koff;
+      f32x16 z;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) S[r] = r < n ? S[r] : -INFINITY;
-          if (n <= 0) pks = 1.f, plv = 0.f, inv = 1.f;
-        }
+      for (int r = 0; r < 16; ++r) z[r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < D / 64; ++s) {
+        const u32x4 x = *(const u32x4*)(kp + s * 1024), y = *(const u32x4*)(kp + s * 1024 + 512);
+        const i32x8 k = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.a[s], z, 0, 0, 0, 127, 0, q.ea);
+        z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.b[s], z, 0, 0, 0, 127, 0, q.eb);
+      }
+      S = z;
+    };
+    bf16x8 P[2][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) P[i >> 1][i & 1][e] = (__bf16)0.f;
+    // One step: the scores of block g + 1, the probabilities of block g = (t, b) and the product of those of block g - 1 with their values.
+    auto step = [&](f32x16& S, f32x16& S_next, bf16x8(&p)[2], const bf16x8(&p_before)[2], int t, int b, int t_v) __attribute__((always_inline)) {
+      const f32x4 page = lds.page[t & 3][2 * b + H];
+      float pks = page[0], plv = page[1], inv = page[2];
+      const int plen = __float_as_int(page[3]), pos = (TILE * t + 2 * b + H) * PAGE;
+      if (__builtin_amdgcn_ballot_w64(plen < PAGE || pos + PAGE - 1 > lim_first) != 0) {
+        asm volatile("");  // (a branch: the compiler would compare and select in every block)
+        const int n = min(plen, lim - pos + 1);  // slots that the row sees
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = r < n ? S[r] : -INFINITY;
+        if (n <= 0) pks = 1.f, plv = 0.f, inv = 1.f;
+      }
+      float ref = plv - m, sum[2] = {0.f, 0.f};
+      f32x8 x[2];
+      scores(S_next, b ? t + 1 : t, 1 - b);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref));
+        sum[r >> 3] += x[r >> 3][r & 7];
+      }
+      // (rounded to bf16, as the probabilities over a bf16 cache are)
+      p[0] = __builtin_convertvector(x[0], bf16x8);
+      p[1] = __builtin_convertvector(x[1], bf16x8);
+      const uint8_t* const vp = lds.v[t_v & 1] + 2 * (1 - b) * (D * 32) + voff;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), p_before[e], O[db]);
+      float more = (sum[0] + sum[1]) * inv;
+      if (__builtin_amdgcn_ballot_w64(!(more < TOP_SUM)) != 0) {  // the reference follows, and the block once more
         float bm = S[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
         bm *= pks;
         bm = fmaxf(bm, other_half(bm));
-        if (__builtin_amdgcn_ballot_w64(bm > m + 3.f) != 0) {
-          const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
-          l *= alpha;
+        const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        l *= alpha;
 #pragma unroll
-          for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
-          m = m_new;
-        }
-        const float ref = plv - m;
-        f32x8 x[2];
-        float sum[2] = {0.f, 0.f};
+          for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
+        m = m_new;
+        ref = plv - m;
+        sum[0] = sum[1] = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref));
           sum[r >> 3] += x[r >> 3][r & 7];
         }
-        l = fmaf(sum[0] + sum[1], inv, l);
-        // (rounded to bf16, as the probabilities over a bf16 cache are)
-        const bf16x8 p[2] = {__builtin_convertvector(x[0], bf16x8), __builtin_convertvector(x[1], bf16x8)};
-        const uint8_t* const vp = lds.v[buf] + (2 * b + H) * (D * 32) + L * 16;
-        if (masked) {
-          // A value that is no number may not reach the rows that do not see it, and a probability of zero does not keep it from them: such
-          // values are cleared, and the sums of the rows that see one become no number, found by a product of "is none" and "is seen".
-          f32x8 seen[2];
-          const int n = min(plen, lim - pos + 1);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) seen[r >> 3][r & 7] = r < n ? 1.f : 0.f;
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) {
-            u32x4 v[2], none[2];
-            uint32_t any = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              v[e] = *(const u32x4*)(vp + e * (D * 16) + db * 512);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = (v[e][i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (v[e][i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                none[e][i] = (lo | hi) & 0x3f803f80u;  // one
-                v[e][i] &= ~(lo | hi);
-                any |= lo | hi;
-              }
-            }
-            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
-              f32x16 c;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) c[r] = 0.f;
-#pragma unroll
-              for (int e = 0; e < 2; ++e) c = mfma32(__builtin_bit_cast(bf16x8, none[e]), __builtin_convertvector(seen[e], bf16x8), c);
-#pragma unroll
-              for (int r = 0; r < 16; ++r) O[db][r] = c[r] > 0.f ? NAN : O[db][r];
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) O[db] = mfma32(__builtin_bit_cast(bf16x8, v[e]), p[e], O[db]);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), p[e], O[db]);
-        }
+        p[0] = __builtin_convertvector(x[0], bf16x8);
+        p[1] = __builtin_convertvector(x[1], bf16x8);
+        more = (sum[0] + sum[1]) * inv;
       }
+      l += more;
     };
 
-    const int n = t1 - t0, page0 = TILE * t0;
-    ask(page0);
-    have();
-    ask(page0 + 64);
-    load(0);
-    store(0);
-    // (what is loaded behind the stretch is never used: its pages are those of the list, or the last one again)
-    load(1);
-    lds_barrier();
-    for (int i = 0; i < n; ++i) {
-      store((i + 1) & 1);
-      if (((i + 2) * TILE & 63) == 0) {
+    // (what is fetched behind the stretch is never used: its pages are those of the list, or the last one again)
+    auto window = [&](int t) __attribute__((always_inline)) {  // before the pages of tile t are fetched
+      if ((TILE * t & 63) == 0) {
         have();
-        ask(page0 + (i + 2) * TILE + 64);
+        ask(TILE * t + 64);
       }
-      load(i + 2);
-      compute(t0 + i, i & 1);
+    };
+    ask(TILE * t0 & ~63);
+    have();
+    ask((TILE * t0 & ~63) + 64);
+    load_k(t0);
+    load_v(t0);
+    store_k(t0);
+    store_v(t0);
+    window(t0 + 1);
+    load_k(t0 + 1);
+    load_v(t0 + 1);
+    lds_barrier();
+    f32x16 S0, S1;
+    scores(S0, t0, 0);
+    int t_v = t0;  // (the first product is of zeros)
+    for (int t = t0; t < t1; ++t) {
+      store_k(t + 1);
+      window(t + 2);
+      load_k(t + 2);
+      step(S0, S1, P[0], P[1], t, 0, t_v);
       lds_barrier();
+      if (__builtin_amdgcn_ballot_w64(lds.none[t & 1][lane & (lds.VWAVES - 1)] != 0) != 0) mark_none(t);
+      store_v(t + 1);
+      load_v(t + 2);
+      step(S1, S0, P[1], P[0], t, 1, t);
+      t_v = t;
     }
+    const uint8_t* const vp = lds.v[t_v & 1] + 2 * (D * 32) + voff;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), P[1][e], O[db]);
     l += other_half(l);
   }
 
@@ -422,6 +522,6 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   a.G = hq / kv->hkv;
   a.splits = p.splits;
   a.slice = p.slice;
-  a.sc = softmax_scale * 1.4426950408889634f;
+  a.sc = std::isfinite(softmax_scale) ? softmax_scale * 1.4426950408889634f : NAN;
   return kv->head_dim == 128 ? launch<128>(a, p, (hipStream_t)stream_) : launch<64>(a, p, (hipStream_t)stream_);
 }
