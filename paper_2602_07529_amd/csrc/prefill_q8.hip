@@ -20,7 +20,7 @@ typedef __attribute__((ext_vector_type(8))) int i32x8;
 constexpr int PAGE = DAG_PAGE_SIZE;
 constexpr int TILE = 4;          // pages
 constexpr int MAX_SPLITS = 64;   // (the lanes of the wave that puts them together)
-constexpr int WAVES = 4;
+constexpr int waves_of(int D) { return 8; }
 
 struct ChunkArgs {
   Q8Cache kv;
@@ -76,15 +76,22 @@ __device__ __forceinline__ void lds_barrier() {  // (loads from memory stay on t
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+__device__ __forceinline__ uint32_t slots_mask(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u; }  // the first n of four
+
+// Of a page for its scores and probabilities: key scale with the softmax's, log2 of the value scale.
+__device__ __forceinline__ float2 page_scales(const ChunkArgs& a, float ks, float vs, int len) {
+  ks *= fabsf(a.sc);
+  ks = ks < 1.2e-38f ? 1.2e-38f : ks;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
+  return len == 0 ? make_float2(1.f, 0.f) : make_float2(ks, __builtin_amdgcn_logf(vs));  // (nobody looks at the scales of a page without tokens)
+}
+
 template <int D, int NW>
 struct Lds {
-  static constexpr int KPAGE = D * PAGE + 128;  // the two pages that 16 lanes read together start half the banks apart
-  static constexpr int VWAVES = TILE * D / 64;  // wave-level pieces of the values of a tile
+  static constexpr int KPAGE = D * PAGE;
   uint8_t k[2][TILE * KPAGE];
-  uint8_t v[2][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
-  f32x4 page[4][TILE];                // key scale with the softmax's, log2 of the value scale and the inverse of that scale, tokens
-  int none[2][VWAVES];                // whether a piece of the values holds codes that are no number
-  int ids[4][TILE];
+  uint8_t v[3][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
+  float2 page[4][TILE];               // key scale with the softmax's, log2 of the value scale
+  int len[4][TILE];                   // tokens
 };
 
 // Query operands in 8 bits: q = 2^e (a + 2^-5 b) with a and b in e4m3, e the row's: a has the first four significant bits of an element, b the
@@ -133,12 +140,94 @@ __device__ __forceinline__ void split_q(QueryCodes<D>& y, const bf16x8 (&q)[D / 
   y.eb = 127 + e - 5;
 }
 
+// A wave's pairs once more, page by page from memory, where a value that is no number was among those that it multiplied: it may not reach
+// the rows that do not see it, and a probability of zero does not keep it from them.  Such values are cleared here, and the sums of the rows
+// that see one become no number: a product of "is none" and "is seen" finds them.
+template <int D>
+__device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, int t0, int t1, int hk, int row, int head, int lim, int L, int H,
+                                        f32x16 (&O)[D / 32], float& m, float& l) {
+  bf16x8 q[D / 16];
+  fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, L + 32 * H);
+  sign_q<D>(q, a.sc);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+  m = -1e30f;
+  l = 0.f;
+  for (int pg0 = TILE * t0; pg0 < min(TILE * t1, pl.np); pg0 += 2) {
+    int64_t at[2];
+    int len[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t e = (size_t)pl.pages + min(pg0 + i, pl.np - 1);
+      at[i] = (int64_t)min(max(a.ctx_pages[e], 0), a.kv.n_pages - 1) * a.kv.hkv + hk;
+      len[i] = pg0 + i < pl.np ? min(max(a.ctx_page_len[e], 0), PAGE) : 0;
+    }
+    const size_t mine = H ? at[1] : at[0], key = L >> 2 & 1 ? at[1] : at[0];
+    const int plen = H ? len[1] : len[0], n = min(plen, lim - (pg0 + H) * PAGE + 1);
+    float2 page = page_scales(a, a.kv.k_scale[mine], a.kv.v_scale[mine], plen);
+    if (n <= 0) page = make_float2(1.f, 0.f);
+    f32x16 S;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      const u32x4 c = *(const u32x4*)(a.kv.k_pool + key * (D * PAGE) + s * 512 + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16);
+      S = mfma32(codes_to_bf16(c[0], c[1]), q[2 * s], S);
+      S = mfma32(codes_to_bf16(c[2], c[3]), q[2 * s + 1], S);
+    }
+    float bm = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      S[r] = r < n ? S[r] * page.x : -INFINITY;
+      bm = fmaxf(bm, S[r]);
+    }
+    bm = fmaxf(bm, other_half(bm));
+    const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    f32x8 x[2], seen[2];
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(S[r] + (page.y - m));
+      sum += x[r >> 3][r & 7];
+      seen[r >> 3][r & 7] = r < n ? 1.f : 0.f;
+    }
+    l = fmaf(l, alpha, sum * __builtin_amdgcn_exp2f(-page.y));
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      u32x4 c = *(const u32x4*)(a.kv.v_pool + mine * (D * PAGE) + (32 * db + L) * 16), one;
+      f32x16 none;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        O[db][r] *= alpha;
+        none[r] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t bad = (((c[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+        one[e] = bad * 0x38u & slots_mask(plen - 4 * e);  // the code of one
+        c[e] &= ~(bad * 0xffu) & slots_mask(plen - 4 * e);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        none = mfma32(codes_to_bf16(one[2 * e], one[2 * e + 1]), __builtin_convertvector(seen[e], bf16x8), none);
+        O[db] = mfma32(codes_to_bf16(c[2 * e], c[2 * e + 1]), __builtin_convertvector(x[e], bf16x8), O[db]);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[db][r] = none[r] > 0.f ? NAN : O[db][r];
+    }
+  }
+}
+
 constexpr float TOP_SUM = 1073741824.f;  // of a block's probabilities relative to the reference: 2^30
 
 template <int D, int NW>
 __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
-  constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = TILE * D / THREADS;  // 16-byte pieces of the keys of a tile to a thread
-  static_assert(PIECES >= 1, "");
+  constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = (TILE * D + THREADS - 1) / THREADS;  // 16-byte pieces of the keys of a tile to a thread
+  constexpr bool HALF = TILE * D < THREADS;  // the upper half of the waves fetches the values, the lower one the keys
+  static_assert(!HALF || 2 * TILE * D == THREADS, "");
   __shared__ __attribute__((aligned(16))) Lds<D, NW> lds;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, L = lane & 31, H = lane >> 5;
   const int hkv = a.kv.hkv, hk = blockIdx.x % hkv, split = blockIdx.x / hkv % a.splits;
@@ -182,139 +271,142 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
     u32x4 kpiece[PIECES], vpiece[PIECES];
     int held[PIECES];
     float ks = 0.f, vs = 0.f;
-    int len = 0, id = 0;
+    int len = 0;
+    const bool my_k = !HALF || w < NW / 2, my_v = !HALF || w >= NW / 2;
+    const int wv = HALF ? w & (NW / 2 - 1) : w;  // the wave's place among those that fetch
     auto fetch = [&](const uint8_t* pool, int t, int i, u32x4& to, int* n) __attribute__((always_inline)) {
-      const int x = w * 64 + i * THREADS, j = x / D, at = (TILE * t + j) & 63;
+      const int x = wv * 64 + i * THREADS, j = x / D, at = (TILE * t + j) & 63;
       const int pg = __builtin_amdgcn_readlane(win_pg, at);
       if (n) *n = __builtin_amdgcn_readlane(win_len, at);
       to = *(const u32x4*)(pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (uint32_t)((x % D + lane) * 16));
     };
     auto load_k = [&](int t) __attribute__((always_inline)) {  // tile t of the context
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) fetch(a.kv.k_pool, t, i, kpiece[i], nullptr);
+      for (int i = 0; i < PIECES; ++i)
+        if (my_k) fetch(a.kv.k_pool, t, i, kpiece[i], nullptr);
       const int at = (TILE * t + (w & (TILE - 1))) & 63;
-      id = __builtin_amdgcn_readlane(win_pg, at);
+      const size_t ph = (size_t)__builtin_amdgcn_readlane(win_pg, at) * hkv + hk;
       len = __builtin_amdgcn_readlane(win_len, at);
-      ks = a.kv.k_scale[(size_t)id * hkv + hk];
-      vs = a.kv.v_scale[(size_t)id * hkv + hk];
+      ks = a.kv.k_scale[ph];
+      vs = a.kv.v_scale[ph];
     };
     auto load_v = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) fetch(a.kv.v_pool, t, i, vpiece[i], &held[i]);
+      for (int i = 0; i < PIECES; ++i)
+        if (my_v) fetch(a.kv.v_pool, t, i, vpiece[i], &held[i]);
     };
     auto store_k = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int x = w * 64 + i * THREADS;
-        *(u32x4*)(lds.k[t & 1] + x / D * lds.KPAGE + (x % D + lane) * 16) = kpiece[i];
+        const int x = wv * 64 + i * THREADS;
+        if (my_k) *(u32x4*)(lds.k[t & 1] + x / D * lds.KPAGE + (x % D + lane) * 16) = kpiece[i];
       }
       if (w < TILE && lane == 0) {
-        float k = ks * fabsf(a.sc), z = __builtin_amdgcn_logf(vs);
-        k = k < 1.2e-38f ? 1.2e-38f : k;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
-        if (len == 0) k = 1.f, z = 0.f;   // (scales of a page without tokens)
-        lds.page[t & 3][w] = f32x4{k, z, __builtin_amdgcn_exp2f(-z), __int_as_float(len)};
-        lds.ids[t & 3][w] = id;
+        lds.page[t & 3][w] = page_scales(a, ks, vs, len);
+        lds.len[t & 3][w] = len;
       }
     };
-    auto store_v = [&](int t) __attribute__((always_inline)) {
+    auto store_v = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        const int x = w * 64 + i * THREADS;
+        if (!my_v) break;
+        const int x = wv * 64 + i * THREADS;
         u32x4 c = vpiece[i];
         if (held[i] < PAGE) {  // slots without a token may hold any codes
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int n = held[i] - 4 * e;
-            c[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << 8 * n) - 1u;
-          }
+          for (int e = 0; e < 4; ++e) c[e] &= slots_mask(held[i] - 4 * e);
         }
-        // Codes that are no number enter as zeros; rows that see one get what they make of it from mark_none.
-        uint32_t any = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) any |= (c[e] & 0x7f7f7f7fu) + 0x01010101u;
-        const bool none = __builtin_amdgcn_ballot_w64((any & 0x80808080u) != 0) != 0;
-        if (none) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[e] &= ~(((((c[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
-        }
-        if (lane == 0) lds.none[t & 1][x / 64] = none;
-        uint8_t* const to = lds.v[t & 1] + x / D * (D * 32) + (x % D + lane) * 16;
+        uint8_t* const to = lds.v[buf] + x / D * (D * 32) + (x % D + lane) * 16;
         *(bf16x8*)to = codes_to_bf16(c[0], c[1]);
         *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
       }
     };
-    // The sums of the rows that see a value that is no number become no number: a product of "is none" and "is seen" finds them.
-    auto mark_none = [&](int t) __attribute__((always_inline)) {
-#pragma unroll 1
-      for (int b = 0; b < 2; ++b) {
-        const int pg = lds.ids[t & 3][2 * b + H], n = min(__float_as_int(lds.page[t & 3][2 * b + H][3]), lim - (TILE * t + 2 * b + H) * PAGE + 1);
-        f32x8 seen[2];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) seen[r >> 3][r & 7] = r < n ? 1.f : 0.f;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          u32x4 c = *(const u32x4*)(a.kv.v_pool + ((size_t)pg * hkv + hk) * (D * PAGE) + (32 * db + L) * 16);
-          f32x16 s;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[e] = ((((c[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0x38u;  // the code of one
-          s = mfma32(codes_to_bf16(c[0], c[1]), __builtin_convertvector(seen[0], bf16x8), s);
-          s = mfma32(codes_to_bf16(c[2], c[3]), __builtin_convertvector(seen[1], bf16x8), s);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) O[db][r] = s[r] > 0.f ? NAN : O[db][r];
-        }
-      }
-    };
     const int koff = (L >> 2 & 1) * lds.KPAGE + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = H * (D * 32) + L * 16;
-    auto scores = [&](f32x16& S, int t, int b) __attribute__((always_inline)) {
-      const uint8_t* const kp = lds.k[t & 1] + 2 * b * lds.KPAGE + koff;
-      f32x16 z;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = 0.f;
-#pragma unroll
-      for (int s = 0; s < D / 64; ++s) {
-        const u32x4 x = *(const u32x4*)(kp + s * 1024), y = *(const u32x4*)(kp + s * 1024 + 512);
-        const i32x8 k = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-        z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.a[s], z, 0, 0, 0, 127, 0, q.ea);
-        z = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.b[s], z, 0, 0, 0, 127, 0, q.eb);
-      }
-      S = z;
+    constexpr int NK = D / 32, NV = D / 16, SLOTS = 3 * D / 32;  // operands of a block's keys and values, matrix products of a step
+    int v_old = 0, v_now = 0, v_next = 1;  // buffers of the values of tiles t - 1, t, t + 1
+    constexpr int AHEAD = 4;  // operands of values on their way
+    u32x4 kop[NK], vop[AHEAD];
+    auto read_k = [&](int i, int t, int b) __attribute__((always_inline)) { kop[i] = *(const u32x4*)(lds.k[t & 1] + 2 * b * lds.KPAGE + koff + i * 512); };
+    auto read_v = [&](int i, int buf, int b) __attribute__((always_inline)) {
+      vop[i % AHEAD] = *(const u32x4*)(lds.v[buf] + 2 * b * (D * 32) + voff + i / (D / 32) * (D * 16) + i % (D / 32) * 512);
     };
-    bf16x8 P[2][2];
+    auto score = [&](f32x16& S, int j) __attribute__((always_inline)) {  // product j of a block's scores
+      const u32x4 x = kop[j & ~1], y = kop[j | 1];
+      const i32x8 k = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+      if (j == 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int r = 0; r < 16; ++r) S[r] = 0.f;
+      }
+      S = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, j & 1 ? q.b[j >> 1] : q.a[j >> 1], S, 0, 0, 0, 127, 0, j & 1 ? q.eb : q.ea);
+    };
+    auto product = [&](int i, const u32x4(&p)[2]) __attribute__((always_inline)) {
+      O[i % (D / 32)] = mfma32(__builtin_bit_cast(bf16x8, vop[i % AHEAD]), __builtin_bit_cast(bf16x8, p[i / (D / 32)]), O[i % (D / 32)]);
+    };
+    u32x4 P[2][2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) P[i >> 1][i & 1][e] = (__bf16)0.f;
-    // One step: the scores of block g + 1, the probabilities of block g = (t, b) and the product of those of block g - 1 with their values.
-    auto step = [&](f32x16& S, f32x16& S_next, bf16x8(&p)[2], const bf16x8(&p_before)[2], int t, int b, int t_v) __attribute__((always_inline)) {
-      const f32x4 page = lds.page[t & 3][2 * b + H];
-      float pks = page[0], plv = page[1], inv = page[2];
-      const int plen = __float_as_int(page[3]), pos = (TILE * t + 2 * b + H) * PAGE;
-      if (__builtin_amdgcn_ballot_w64(plen < PAGE || pos + PAGE - 1 > lim_first) != 0) {
-        asm volatile("");  // (a branch: the compiler would compare and select in every block)
-        const int n = min(plen, lim - pos + 1);  // slots that the row sees
+    for (int i = 0; i < 4; ++i) P[i >> 1][i & 1] = u32x4{0, 0, 0, 0};
+    // One step: the scores of block g + 1 from the operands that are there, the probabilities of block g = (t, b) and the product of those of
+    // block g - 1 with their values, slot by slot: a matrix product, the read of an operand of the next step into the place of the one just
+    // used, some of the exponentials.  stage: called behind the second slot.
+    auto step = [&](f32x16& S, f32x16& S_next, u32x4(&p)[2], const u32x4(&p_before)[2], float2 page, int t, int b, bool masked, auto&& stage) __attribute__((always_inline)) {
+      float pks = page.x, plv = page.y;
+      if (masked) {
+        const int n = min(lds.len[t & 3][2 * b + H], lim - (TILE * t + 2 * b + H) * PAGE + 1);  // slots that the row sees
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = r < n ? S[r] : -INFINITY;
-        if (n <= 0) pks = 1.f, plv = 0.f, inv = 1.f;
+        if (n <= 0) pks = 1.f, plv = 0.f;
       }
+      const float inv = __builtin_amdgcn_exp2f(-plv);
       float ref = plv - m, sum[2] = {0.f, 0.f};
-      f32x8 x[2];
-      scores(S_next, b ? t + 1 : t, 1 - b);
+      float x[16];
+      // (elements of slot i)
+      auto of_slot = [&](int i, auto&& f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref));
-        sum[r >> 3] += x[r >> 3][r & 7];
+        for (int r = 0; r < 16; ++r)
+          if (r >= i * 16 / SLOTS && r < (i + 1) * 16 / SLOTS) f(r);
+      };
+      auto soft_a = [&](int i) __attribute__((always_inline)) { of_slot(i, [&](int r) __attribute__((always_inline)) { x[r] = fmaf(S[r], pks, ref); }); };
+      auto soft_b = [&](int i) __attribute__((always_inline)) { of_slot(i, [&](int r) __attribute__((always_inline)) { x[r] = __builtin_amdgcn_exp2f(x[r]); }); };
+      auto soft_c = [&](int i) __attribute__((always_inline)) {
+        of_slot(i, [&](int r) __attribute__((always_inline)) {
+          sum[r & 1] += x[r];
+          // (rounded to bf16, as the probabilities over a bf16 cache are)
+          if (r & 1) p[r >> 3][(r & 7) >> 1] = dag_pack_bf2(x[r - 1], x[r]);
+        });
+      };
+      constexpr int LAG = 2;
+#pragma unroll
+      for (int i = 0; i < LAG; ++i) soft_a(i);
+#pragma unroll
+      for (int i = 0; i < LAG - 1; ++i) soft_b(i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < SLOTS; ++i) {
+        if (i % 3 == 0) {
+          const int j = i / 3;
+          score(S_next, j);
+          if (j & 1) {
+            read_k(j - 1, t + 1, b);
+            read_k(j, t + 1, b);
+          }
+        } else {
+          const int j = i / 3 * 2 + i % 3 - 1;
+          product(j, p_before);
+          if (j + AHEAD < NV) read_v(j + AHEAD, b ? v_now : v_old, 1 - b);  // of this block g - 1, then of the next one
+          else read_v(j + AHEAD - NV, v_now, b);
+        }
+        // (an element's multiply-add, exponential, sum and rounding in slots behind one another: none waits for the one in front)
+        soft_a(i + LAG);
+        soft_b(i + LAG - 1);
+        soft_c(i);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i == 1) {
+          stage();
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      // (rounded to bf16, as the probabilities over a bf16 cache are)
-      p[0] = __builtin_convertvector(x[0], bf16x8);
-      p[1] = __builtin_convertvector(x[1], bf16x8);
-      const uint8_t* const vp = lds.v[t_v & 1] + 2 * (1 - b) * (D * 32) + voff;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), p_before[e], O[db]);
       float more = (sum[0] + sum[1]) * inv;
+      asm volatile("" : "+v"(S_next));  // (here, not where they are used: the compiler would put all their products in one place)
       if (__builtin_amdgcn_ballot_w64(!(more < TOP_SUM)) != 0) {  // the reference follows, and the block once more
         float bm = S[0];
 #pragma unroll
@@ -331,55 +423,93 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         ref = plv - m;
         sum[0] = sum[1] = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          x[r >> 3][r & 7] = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref));
-          sum[r >> 3] += x[r >> 3][r & 7];
+        for (int r = 0; r < 16; r += 2) {
+          const float y = __builtin_amdgcn_exp2f(fmaf(S[r], pks, ref)), z = __builtin_amdgcn_exp2f(fmaf(S[r + 1], pks, ref));
+          sum[0] += y;
+          sum[1] += z;
+          p[r >> 3][(r & 7) >> 1] = dag_pack_bf2(y, z);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        p[0] = __builtin_convertvector(x[0], bf16x8);
-        p[1] = __builtin_convertvector(x[1], bf16x8);
         more = (sum[0] + sum[1]) * inv;
       }
       l += more;
     };
 
-    // (what is fetched behind the stretch is never used: its pages are those of the list, or the last one again)
+    // Tile t reads the keys of tile t + 1 and its own values; the keys of tile t + 2 and the values of t + 1 come into LDS, those of t + 3 and
+    // t + 2 are fetched.  (What is fetched behind the stretch is never used: its pages are those of the list, or the last one again.)
+    uint64_t full = 0;  // pages of the window that are full
     auto window = [&](int t) __attribute__((always_inline)) {  // before the pages of tile t are fetched
       if ((TILE * t & 63) == 0) {
         have();
         ask(TILE * t + 64);
       }
     };
+    auto is_full = [&](int t) __attribute__((always_inline)) {
+      full = __builtin_amdgcn_ballot_w64(win_len == PAGE);
+      return (full >> (TILE * t & 63) & ((1 << TILE) - 1)) == (1 << TILE) - 1 && (t + 1) * (TILE * PAGE) - 1 <= lim_first;
+    };
     ask(TILE * t0 & ~63);
     have();
     ask((TILE * t0 & ~63) + 64);
+    bool f0, f1, f2, f3;  // whether nothing of tiles t .. t + 3 is hidden
     load_k(t0);
     load_v(t0);
+    f0 = is_full(t0);
     store_k(t0);
-    store_v(t0);
+    store_v(0);
     window(t0 + 1);
     load_k(t0 + 1);
     load_v(t0 + 1);
+    f1 = is_full(t0 + 1);
+    store_k(t0 + 1);
+    window(t0 + 2);
+    load_k(t0 + 2);
+    f2 = is_full(t0 + 2);
     lds_barrier();
     f32x16 S0, S1;
-    scores(S0, t0, 0);
-    int t_v = t0;  // (the first product is of zeros)
+#pragma unroll
+    for (int i = 0; i < NK; ++i) read_k(i, t0, 0);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) score(S0, j);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) read_k(i, t0, 1);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read_v(i, 0, 1);  // (the first product is of zeros)
+    float2 page0 = lds.page[t0 & 3][H], page1 = lds.page[t0 & 3][2 + H];
     for (int t = t0; t < t1; ++t) {
-      store_k(t + 1);
-      window(t + 2);
-      load_k(t + 2);
-      step(S0, S1, P[0], P[1], t, 0, t_v);
       lds_barrier();
-      if (__builtin_amdgcn_ballot_w64(lds.none[t & 1][lane & (lds.VWAVES - 1)] != 0) != 0) mark_none(t);
-      store_v(t + 1);
-      load_v(t + 2);
-      step(S1, S0, P[1], P[0], t, 1, t);
-      t_v = t;
+      step(S0, S1, P[0], P[1], page0, t, 0, !f0, [&]() __attribute__((always_inline)) {
+        store_v(v_next);
+        load_v(t + 2);
+        page0 = lds.page[(t + 1) & 3][H];
+      });
+      step(S1, S0, P[1], P[0], page1, t, 1, !f0, [&]() __attribute__((always_inline)) {
+        store_k(t + 2);
+        window(t + 3);
+        load_k(t + 3);
+        f3 = is_full(t + 3);
+        page1 = lds.page[(t + 1) & 3][2 + H];
+      });
+      v_old = v_now;
+      v_now = v_next;
+      v_next = v_next == 2 ? 0 : v_next + 1;
+      f0 = f1;
+      f1 = f2;
+      f2 = f3;
     }
-    const uint8_t* const vp = lds.v[t_v & 1] + 2 * (D * 32) + voff;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int i = 0; i < NV; ++i) {
+      product(i, P[1]);
+      if (i + AHEAD < NV) read_v(i + AHEAD, v_old, 1);
+    }
+    float any = 0.f;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) O[db] = mfma32(*(const bf16x8*)(vp + e * (D * 16) + db * 512), P[1][e], O[db]);
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) any = fmaf(O[db][r], 0.f, any);
+    if (__builtin_amdgcn_ballot_w64(any != any) != 0) {  // a value that is no number has been among them
+      sums_again<D>(a, pl, t0, t1, hk, row, head, lim, L, H, O, m, l);
+    }
     l += other_half(l);
   }
 
@@ -465,10 +595,10 @@ bool bounds_ok(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, in
 
 template <int D>
 int launch(const ChunkArgs& a, const Plan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((k_q8_chunk<D, WAVES>), dim3((unsigned)(p.slots * a.kv.hkv * p.splits)), dim3(64 * WAVES), 0, stream, a);
+  hipLaunchKernelGGL((k_q8_chunk<D, waves_of(D)>), dim3((unsigned)(p.slots * a.kv.hkv * p.splits)), dim3(64 * waves_of(D)), 0, stream, a);
   DAG_LAUNCH_CHECK();
   if (p.splits > 1) {
-    hipLaunchKernelGGL((k_q8_chunk_merge<D, WAVES>), dim3((unsigned)(p.slots * a.kv.hkv * (32 * WAVES / 4))), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_q8_chunk_merge<D, waves_of(D)>), dim3((unsigned)(p.slots * a.kv.hkv * (32 * waves_of(D) / 4))), dim3(256), 0, stream, a);
     DAG_LAUNCH_CHECK();
   }
   return DAG_OK;
@@ -480,8 +610,8 @@ size_t part_count(const Plan& p, int hkv, int pairs) { return p.splits > 1 ? (si
 
 extern "C" size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim) {
   Plan p;
-  if (!bounds_ok(d, n_rows, hq, hkv, head_dim) || d->page_size != PAGE || !plan(d, n_rows, hq, hkv, 32 * WAVES, &p)) return 0;
-  return part_count(p, hkv, 32 * WAVES) * (head_dim + 2) * sizeof(float);
+  if (!bounds_ok(d, n_rows, hq, hkv, head_dim) || d->page_size != PAGE || !plan(d, n_rows, hq, hkv, 32 * waves_of(head_dim), &p)) return 0;
+  return part_count(p, hkv, 32 * waves_of(head_dim)) * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
@@ -489,7 +619,7 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   if (!d || !kv) return DAG_ERR_NULL;
   if (d->n_nodes < 0 || d->max_new < 0 || d->max_ctx_pages < 0 || kv->n_pages < 0 || n_rows < 0) return DAG_ERR_BAD_LEN;
   Plan p;
-  if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, 32 * WAVES, &p)) return DAG_ERR_UNSUPPORTED;
+  if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, 32 * waves_of(kv->head_dim), &p)) return DAG_ERR_UNSUPPORTED;
   if (p.slots == 0 || n_rows == 0) return DAG_OK;  // no new token anywhere
   const bool pages = d->max_ctx_pages > 0;
   if (pages && kv->n_pages == 0) return DAG_ERR_BAD_LEN;
@@ -498,7 +628,7 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   if (!dag_aligned16(q) || !dag_aligned16(out) || !dag_aligned16(kv->k_pool) || !dag_aligned16(kv->v_pool) || ((uintptr_t)kv->k_scale & 3) ||
       ((uintptr_t)kv->v_scale & 3) || ((uintptr_t)lse & 3))
     return DAG_ERR_ALIGN;
-  const size_t parts = part_count(p, kv->hkv, 32 * WAVES);
+  const size_t parts = part_count(p, kv->hkv, 32 * waves_of(kv->head_dim));
   if (parts > 0 && (!ws || ws_bytes < parts * (kv->head_dim + 2) * sizeof(float))) return DAG_ERR_WORKSPACE;
   if (parts > 0 && !dag_aligned16(ws)) return DAG_ERR_ALIGN;
   ChunkArgs a = {};
