@@ -143,6 +143,33 @@ int dag_build_meta(const dag_desc_t* desc, const dag_meta_t* meta, void* ws, siz
 int dag_rope_qk(const int32_t* pos_ids, int64_t n_tokens, void* q, void* k, int32_t hq,
                 int32_t hkv, int32_t head_dim, float theta, dag_dtype_t dtype, void* stream);
 
+/* Rotary positions by a table of frequencies: pair m of the leading rotary_dim elements of a head turns by pos * freq[m] and is multiplied by
+ * `factor` (1, or what a stretched embedding asks for); the elements behind stay as they are.  DAG_ROPE_HALVES pairs elements (m, m + rotary_dim / 2),
+ * DAG_ROPE_PAIRS (2 m, 2 m + 1).  The struct lives on the HOST. */
+typedef enum { DAG_ROPE_HALVES = 0, DAG_ROPE_PAIRS = 1 } dag_rope_layout_t;
+typedef struct {
+  const double* freq; /* DEVICE [rotary_dim / 2]                                                 */
+  float factor;
+  int32_t rotary_dim;
+  int32_t layout;     /* dag_rope_layout_t                                                       */
+} dag_rope_t;
+
+/* A table of frequencies: f = theta^(-2 m / rotary_dim), for contexts `stretch` times as long as those of the training.  original = 0: all are
+ * divided by it (positions are interpolated).  original > 0, a length in tokens: by parts, a pair that turns `high` times or more over it keeps
+ * f, one that turns `low` times or less has f / stretch, in between the two are mixed in proportion.  `freq` HOST [rotary_dim / 2];
+ * rotary_dim even and <= 256.  Errors: DAG_ERR_NULL, DAG_ERR_UNSUPPORTED. */
+int dag_rope_frequencies(double* freq, int32_t rotary_dim, double theta, double stretch, double original, double low, double high);
+
+/* Rotates q [n_tokens][hq][head_dim] and k [n_tokens][hkv][head_dim] (either may be NULL) at pos [n_tokens] into q_out and k_out; a token's heads
+ * lie next to each other, tokens `stride` elements apart (the parts of a fused projection, say).  q_out may be q and k_out k, with the same
+ * stride; no other output may overlap an input.  transposed != 0: the transposed rotation, with which gradients of the outputs become those of
+ * the inputs (the inverse where factor is 1).  All DEVICE, 16-byte aligned, strides a multiple of 16 bytes.  head_dim and rotary_dim multiples of
+ * 16, head_dim <= 256; DAG_F32 or DAG_BF16; angles in 64 bits, the rotation in 32.
+ * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_HIP. */
+int dag_rope_apply(const dag_rope_t* rope, const int32_t* pos, int64_t n_tokens, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                   const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t hq, int32_t hkv, int32_t head_dim, int32_t transposed,
+                   dag_dtype_t dtype, void* stream);
+
 /* Eq. 2 + Eq. 3: out[i] = sum_j softmax_j(q_i . k_j * softmax_scale + M_ij) v_j, where M is the
  * DAG mask described by `meta`.  q/out [T][hq][head_dim], k/v [T][hkv][head_dim] DEVICE, already
  * rotated; lse (nullable) [T][hq] fp32 receives log sum exp of the scaled scores.
@@ -406,6 +433,11 @@ typedef struct {
 int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new,
                           const void* v_new, float theta, dag_dtype_t dtype, void* stream);
 
+/* dag_kv_append_rope_q8 with the key rotated as dag_rope_apply rotates (rotary_dim a multiple of 32), from tokens that lie k_stride and v_stride elements
+ * apart (multiples of 16 bytes). */
+int dag_kv_append_rotary_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const dag_rope_t* rope, dag_dtype_t dtype, void* stream);
+
 /* dag_attn_decode over an 8-bit cache: same description, same attention of every live branch's query over (shared context, own
  * tokens).  q / out [n_live][hq][head_dim] bf16 DEVICE, q already rotated; hq a multiple of kv->hkv, hq / hkv <= 32.
  * n_groups may be 0 (no shared context anywhere; the group_* and shared_* arrays are then not read), otherwise every branch is in a
@@ -479,6 +511,44 @@ int dag_kv_tables(const dag_kv_rows_t* rows, const int32_t* new_len, const int32
                   const int32_t* free_count, int32_t* free_count_out, int32_t* new_off, int32_t* slots, int64_t max_new,
                   const int32_t* pos0, int32_t* pos, int32_t* page_off, int32_t* pages, int64_t max_pages, int32_t* refused,
                   void* ws, size_t ws_bytes, void* stream);
+
+/* Rows that share pages.  extra [n_pages] DEVICE int32 says how many rows hold a page besides its first holder (0 for a page of one row and for a
+ * free one).  dag_kv_tables goes on as before (a row's new tokens only go into a last page of its own: dag_kv_fork sees to that); rows give
+ * their pages back through dag_kv_release_shared in the place of dag_kv_release.  Bytes of the DEVICE workspace (8-byte aligned, any contents) of the
+ * three calls below, n_forks for dag_kv_fork; calls that overlap need one each. */
+size_t dag_kv_pages_workspace_bytes(int32_t n_rows, int32_t n_pages, int32_t n_forks);
+
+/* Section 4.3 (Fork: the children inherit the same context): row child[f] becomes a copy of the first fork_len[f] tokens (all of them without
+ * fork_len, never more than there are) of row parent[f]: the full pages by reference, and for the tokens of a partly filled last one a page of its own,
+ * taken as dag_kv_tables takes them.  copy_src[f] / copy_dst[f] [n_forks] are the pages to copy for it with dag_kv_copy_pages(_q8), -1 where there is none.
+ * A fork is refused (counted in refused [1], nullable; the row stays as it is) if a row is outside the table, if child[f] holds tokens or is the
+ * child of a fork in front, or if its page and those of the forks in front are more than are free.  A parent may have any number of children; lengths are
+ * those before the call.  row_len_out may be row_len, extra_out extra and free_count_out free_count; no other output may overlap an input.
+ * Errors as dag_kv_tables. */
+int dag_kv_fork(const dag_kv_rows_t* rows, int32_t n_forks, const int32_t* parent, const int32_t* child, const int32_t* fork_len, const int32_t* row_len,
+                int32_t* row_len_out, const int32_t* extra, int32_t* extra_out, const int32_t* free_count, int32_t* free_count_out, int32_t* copy_src,
+                int32_t* copy_dst, int32_t* refused, void* ws, size_t ws_bytes, void* stream);
+
+/* dag_kv_release for rows that share pages: rows with ended[r] != 0 hold theirs no more; a page that nobody holds any longer is given back once, at the
+ * place of the last of the ended rows that held it (in the order of rows and tokens).  Page ids outside the pool are left out.  row_len_out may be
+ * row_len, extra_out extra and free_count_out free_count. */
+int dag_kv_release_shared(const dag_kv_rows_t* rows, const int32_t* ended, const int32_t* row_len, int32_t* row_len_out, const int32_t* extra,
+                          int32_t* extra_out, const int32_t* free_count, int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Moves the pages in use to the front of the pool: with U = n_pages - *free_count the k-th used page (ascending) from U on goes to the k-th free page in
+ * front of U.  copy_src / copy_dst [n_pages / 2] get the *n_copies pairs, for dag_kv_copy_pages(_q8) (entries behind them are left as they were);
+ * page_map [n_pages] every page's new id, -1 for free ones, for lists other than the table's; extra_out the holders by new id; rows_out (of the
+ * same sizes; its arrays may be those of rows) the table's lines with new ids as far as they are held, and the free pages so that the lowest is taken first
+ * (entries behind *free_count are left).  The free list has to name every free page once. */
+int dag_kv_compact(const dag_kv_rows_t* rows, const dag_kv_rows_t* rows_out, const int32_t* row_len, const int32_t* extra, int32_t* extra_out,
+                   const int32_t* free_count, int32_t* page_map, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies, void* ws, size_t ws_bytes,
+                   void* stream);
+
+/* Copies pages src[i] of both pools (and their scales) to dst[i], i < n, or < min(n, *count) with count (DEVICE [1], nullable).  Pairs with a
+ * page outside the pool, -1 say, are left out; no page may be written twice, nor be read where another pair writes it.  dag_kv_copy_pages: bf16 pools. */
+int dag_kv_copy_pages_q8(const dag_kv_q8_t* kv, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* count, void* stream);
+int dag_kv_copy_pages(void* k_pool, void* v_pool, int32_t n_pages, int32_t hkv, int32_t head_dim, const int32_t* src, const int32_t* dst, int32_t n,
+                      const int32_t* count, void* stream);
 
 /* Host-side scheduler of the execution phase (section 3.2: the plan as a Petri net whose places
  * are the DAG nodes, one transition per node with its parents as input places; section 3.3, Eq. 1:

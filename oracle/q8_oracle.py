@@ -133,3 +133,89 @@ def extend(table, free, count, row_len, new_len, pos0):
 
 def rope(x, pos, theta):
     return orc.rope(x, pos, theta)
+
+
+def fork(table, free, count, row_len, extra, parent, child, fork_len):
+    """In place, fork by fork.  Returns (free pages left, copy_src, copy_dst, refused)."""
+    before = np.maximum(np.asarray(row_len), 0).copy()
+    taken, asked, refused, src, dst = set(), 0, 0, [], []
+    for f, (p, c) in enumerate(zip(parent, child)):
+        src.append(-1)
+        dst.append(-1)
+        if not (0 <= p < len(before) and 0 <= c < len(before)) or before[c] > 0 or c in taken:
+            refused += 1
+            continue
+        taken.add(c)
+        n = min(before[p], table.shape[1] * PAGE)
+        n = n if fork_len is None else min(n, max(fork_len[f], 0))
+        if n % PAGE:
+            asked += 1
+            if asked > count:
+                refused += 1
+                continue
+            src[f], dst[f] = table[p, n // PAGE], free[count - asked]
+        for i in range(n // PAGE):
+            table[c, i] = table[p, i]
+            if 0 <= table[p, i] < len(extra):
+                extra[table[p, i]] += 1
+        if n % PAGE:
+            table[c, n // PAGE] = dst[f]
+        row_len[c] = n
+    return count - min(asked, count), src, dst, refused
+
+
+def release_shared(table, free, count, row_len, extra, ended):
+    """In place; returns the new number of free pages."""
+    given = [int(p) for r in range(len(row_len)) if ended[r] for p in table[r, :min(-(-max(int(row_len[r]), 0) // PAGE), table.shape[1])]]
+    given = [p for p in given if 0 <= p < len(extra)]
+    for i, p in enumerate(given):
+        if p not in given[i + 1:] and given.count(p) > max(extra[p], 0):
+            free[count] = p
+            count += 1
+    for p in set(given):
+        extra[p] = max(max(extra[p], 0) - given.count(p), 0)
+    for r in range(len(row_len)):
+        if ended[r]:
+            row_len[r] = 0
+    return count
+
+
+def compact(table, free, count, row_len, extra):
+    """Returns (table, free, extra, page_map, pairs)."""
+    n = len(extra)
+    none = set(int(p) for p in free[:count])
+    used = n - count
+    to = [p for p in range(used) if p in none]
+    moved = [p for p in range(used, n) if p not in none]
+    new = {p: p for p in range(used) if p not in none}
+    new.update(zip(moved, to))
+    table, free, holders = table.copy(), free.copy(), np.zeros(n, dtype=np.int64)
+    for r in range(len(row_len)):
+        for i in range(min(-(-max(int(row_len[r]), 0) // PAGE), table.shape[1])):
+            table[r, i] = new.get(int(table[r, i]), table[r, i])
+    for i in range(count):
+        free[i] = n - 1 - i
+    for p, q in new.items():
+        holders[q] = extra[p]
+    return table, free, holders, [new.get(p, -1) for p in range(n)], list(zip(moved, to))
+
+
+def frequencies(rotary, theta, stretch=1.0, original=0.0, low=1.0, high=32.0):
+    out = []
+    for m in range(rotary // 2):
+        f = theta ** (-2.0 * m / rotary)
+        keep = 0.0 if original == 0 else min(max((original * f / (2 * math.pi) - low) / (high - low), 0.0), 1.0)
+        out.append(keep * f + (1 - keep) * f / stretch)
+    return np.asarray(out)
+
+
+def rotary(x, pos, freq, pairs, factor=1.0, transposed=False):
+    """x [token][head][dim] in 64 bits: pair m turned by pos * freq[m], times factor."""
+    y = np.array(x, dtype=np.float64)
+    half = len(freq)
+    i = 2 * np.arange(half) if pairs else np.arange(half)
+    j = i + 1 if pairs else i + half
+    angle = np.asarray(pos, dtype=np.float64)[:, None, None] * freq * (-1 if transposed else 1)
+    c, s = np.cos(angle) * factor, np.sin(angle) * factor
+    y[..., i], y[..., j] = x[..., i] * c - x[..., j] * s, x[..., j] * c + x[..., i] * s
+    return y

@@ -17,6 +17,7 @@ DAG_F32, DAG_BF16 = 0, 1
 DAG_STRICT_CLOSURE = 1
 TILE_SKIP, TILE_PARTIAL, TILE_FULL = 0, 1, 2
 PAGE = 16
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 
 
 class DagError(RuntimeError):
@@ -96,6 +97,10 @@ class dag_kv_q8_t(C.Structure):
                 ("n_pages", C.c_int32), ("hkv", C.c_int32), ("head_dim", C.c_int32)]
 
 
+class dag_rope_t(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("factor", C.c_float), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
+
+
 class dag_kv_rows_t(C.Structure):
     _fields_ = [("n_rows", C.c_int32), ("page_size", C.c_int32), ("max_row_pages", C.c_int32), ("n_pages", C.c_int32),
                 ("table", C.c_void_p), ("free_pages", C.c_void_p)]
@@ -150,6 +155,18 @@ def lib():
         L.dag_prefill_paged_q8_workspace_bytes.restype = C.c_size_t
         L.dag_attn_prefill_paged_q8.argtypes = [C.POINTER(dag_paged_prefill_desc_t), C.POINTER(dag_kv_q8_t), vp, i64, vp, vp, i32, f32, vp,
                                                 C.c_size_t, vp]
+        f64 = C.c_double
+        L.dag_rope_frequencies.argtypes = [vp, i32, f64, f64, f64, f64, f64]
+        L.dag_rope_apply.argtypes = [C.POINTER(dag_rope_t), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, C.c_int, vp]
+        L.dag_kv_append_rotary_q8.argtypes = [C.POINTER(dag_kv_q8_t), vp, vp, i64, vp, i64, vp, i64, C.POINTER(dag_rope_t), C.c_int, vp]
+        rows = C.POINTER(dag_kv_rows_t)
+        L.dag_kv_pages_workspace_bytes.argtypes = [i32, i32, i32]
+        L.dag_kv_pages_workspace_bytes.restype = C.c_size_t
+        L.dag_kv_fork.argtypes = [rows, i32] + [vp] * 13 + [C.c_size_t, vp]
+        L.dag_kv_release_shared.argtypes = [rows] + [vp] * 8 + [C.c_size_t, vp]
+        L.dag_kv_compact.argtypes = [rows, rows] + [vp] * 9 + [C.c_size_t, vp]
+        L.dag_kv_copy_pages_q8.argtypes = [C.POINTER(dag_kv_q8_t), vp, vp, i32, vp, vp]
+        L.dag_kv_copy_pages.argtypes = [vp, vp, i32, i32, i32, vp, vp, i32, vp, vp]
         L.dag_kv_tables_workspace_bytes.argtypes = [i32]
         L.dag_kv_tables_workspace_bytes.restype = C.c_size_t
         L.dag_kv_release.argtypes = [C.POINTER(dag_kv_rows_t), vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
@@ -168,7 +185,8 @@ def lib():
                      "dag_kv_append_rope", "dag_attn_decode", "dag_attn_decode_static", "dag_attn_decode_segments",
                      "dag_sched_create", "dag_attn_prefill_paged", "dag_copy_calibration",
                      "dag_attn_prefill_bwd", "dag_kv_append_rope_q8", "dag_attn_decode_q8", "dag_attn_decode_segments_q8",
-                     "dag_attn_prefill_paged_q8", "dag_kv_release", "dag_kv_tables",
+                     "dag_attn_prefill_paged_q8", "dag_rope_frequencies", "dag_rope_apply", "dag_kv_append_rotary_q8", "dag_kv_fork",
+                     "dag_kv_release_shared", "dag_kv_compact", "dag_kv_copy_pages_q8", "dag_kv_copy_pages", "dag_kv_release", "dag_kv_tables",
                      "dag_sched_step"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -560,6 +578,67 @@ def dag_kv_append_rope_q8(cache, slots, pos, k_new, v_new, theta):
                                        theta, _dtype_code(k_new), _here(slots, pos, k_new, v_new, cache.k_pool)))
 
 
+class Rope:
+    """Rotary positions: the table of frequencies on the device (dag_rope_frequencies, or `freq`, a sequence of rotary_dim / 2 of them)
+    and the ctypes struct."""
+
+    def __init__(self, rotary_dim, theta, device, layout=ROPE_HALVES, stretch=1.0, original=0.0, low=1.0, high=32.0, factor=1.0, freq=None):
+        if freq is None:
+            table = np.empty(max(rotary_dim // 2, 1), dtype=np.float64)
+            _check(lib().dag_rope_frequencies(table.ctypes.data, rotary_dim, theta, stretch, original, low, high))
+        else:
+            table = np.ascontiguousarray(freq, dtype=np.float64)
+            if table.shape != (rotary_dim // 2,):
+                raise ValueError("%d frequencies, not %d" % (table.size, rotary_dim // 2))
+        self.freq = torch.from_numpy(table).to(device)
+        self.rotary_dim, self.layout, self.factor = rotary_dim, layout, factor
+        self.c = dag_rope_t(self.freq.data_ptr(), factor, rotary_dim, layout)
+        self.ref = C.byref(self.c)
+
+
+def _token_stride(x, name):
+    """Elements from a token of x [tokens][heads][dim] to the next; its heads lie next to each other."""
+    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError("%s is [tokens][heads][dim] with the heads of a token next to each other" % name)
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2])
+
+
+def dag_rope_apply(rope, pos, q, k, q_out=None, k_out=None, transposed=False):
+    """q and k (either may be None) into q_out and k_out, in place without them."""
+    ref = q if q is not None else k
+    if ref is None:
+        return
+    n, d, args, there = pos.numel(), ref.shape[-1], [], []
+    _int32(pos, "pos")
+    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            if y is not None:
+                raise ValueError("%s_out without %s" % (name, name))
+            args += [None, 0, None, 0]
+            continue
+        y = x if y is None else y
+        if x.shape[0] != n or x.shape[-1] != d or y.shape != x.shape:
+            raise ValueError("%s is [%d][heads][%d], %s_out has its shape" % (name, n, d, name))
+        if x.dtype != ref.dtype or y.dtype != ref.dtype:
+            raise TypeError("tensors of one type")
+        args += [x.data_ptr(), _token_stride(x, name), y.data_ptr(), _token_stride(y, name + "_out")]
+        there += [x, y]
+    _check(lib().dag_rope_apply(rope.ref, pos.data_ptr(), n, *args, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d, int(transposed),
+                                _dtype_code(ref), _here(pos, rope.freq, *there)))
+
+
+def dag_kv_append_rotary_q8(cache, slots, pos, k_new, v_new, rope):
+    n = slots.numel()
+    shape = (n, cache.hkv, cache.head_dim)
+    if k_new.shape != shape or v_new.shape != shape or pos.numel() != n or k_new.dtype != v_new.dtype:
+        raise ValueError("k_new and v_new are [tokens][%d][%d] of one type, slots and pos as long" % shape[1:])
+    _int32(slots, "slots")
+    _int32(pos, "pos")
+    _check(lib().dag_kv_append_rotary_q8(
+        cache.ref, slots.data_ptr(), pos.data_ptr(), n, k_new.data_ptr(), _token_stride(k_new, "k_new"), v_new.data_ptr(),
+        _token_stride(v_new, "v_new"), rope.ref, _dtype_code(k_new), _here(slots, pos, k_new, v_new, cache.k_pool, rope.freq)))
+
+
 def dag_decode_q8_workspace_bytes(ddesc, cache, hq):
     return lib().dag_decode_q8_workspace_bytes(C.byref(ddesc.c), hq, cache.hkv, cache.head_dim)
 
@@ -618,6 +697,14 @@ class KvRows:
         n_rows, width = table.shape
         self.c = dag_kv_rows_t(n_rows, PAGE, width, free_pages.numel(), table.data_ptr(), free_pages.data_ptr())
         self.workspace = torch.zeros(int(lib().dag_kv_tables_workspace_bytes(n_rows)), dtype=torch.uint8, device=table.device)
+        self.shared_workspace = None  # of the calls on shared pages
+
+    def for_shared(self, n_forks=0):
+        """The workspace of dag_kv_fork, dag_kv_release_shared and dag_kv_compact, made at the first of them (outside a capture)."""
+        need = int(lib().dag_kv_pages_workspace_bytes(self.c.n_rows, self.c.n_pages, max(n_forks, self.c.n_rows)))
+        if self.shared_workspace is None or self.shared_workspace.numel() < need:
+            self.shared_workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
+        return self.shared_workspace
 
 
 def _at(x):
@@ -666,6 +753,75 @@ def dag_kv_tables(rows, new_len, row_len, row_len_out, free_count, free_count_ou
                                rows.workspace.numel(),
                                _here(rows.table, new_len, row_len, row_len_out, free_count, free_count_out, new_off, slots,
                                      *optional)))
+
+
+def dag_kv_fork(rows, parent, child, row_len, row_len_out, extra, extra_out, free_count, free_count_out, copy_src, copy_dst, fork_len=None,
+                refused=None):
+    n = parent.numel()
+    _ints(n, parent=parent, child=child, copy_src=copy_src, copy_dst=copy_dst)
+    _ints(rows.c.n_rows, row_len=row_len, row_len_out=row_len_out)
+    _ints(rows.c.n_pages, extra=extra, extra_out=extra_out)
+    _ints(1, free_count=free_count, free_count_out=free_count_out)
+    optional = [x for x in (fork_len, refused) if x is not None]
+    if fork_len is not None:
+        _ints(n, fork_len=fork_len)
+    if refused is not None:
+        _ints(1, refused=refused)
+    ws = rows.for_shared(n)
+    _check(lib().dag_kv_fork(rows.c, n, parent.data_ptr(), child.data_ptr(), _at(fork_len), row_len.data_ptr(), row_len_out.data_ptr(),
+                             extra.data_ptr(), extra_out.data_ptr(), free_count.data_ptr(), free_count_out.data_ptr(), copy_src.data_ptr(),
+                             copy_dst.data_ptr(), _at(refused), ws.data_ptr(), ws.numel(),
+                             _here(rows.table, parent, child, row_len, row_len_out, extra, extra_out, free_count, free_count_out, copy_src,
+                                   copy_dst, *optional)))
+
+
+def dag_kv_release_shared(rows, ended, row_len, row_len_out, extra, extra_out, free_count, free_count_out):
+    _ints(rows.c.n_rows, ended=ended, row_len=row_len, row_len_out=row_len_out)
+    _ints(rows.c.n_pages, extra=extra, extra_out=extra_out)
+    _ints(1, free_count=free_count, free_count_out=free_count_out)
+    ws = rows.for_shared()
+    _check(lib().dag_kv_release_shared(rows.c, ended.data_ptr(), row_len.data_ptr(), row_len_out.data_ptr(), extra.data_ptr(),
+                                       extra_out.data_ptr(), free_count.data_ptr(), free_count_out.data_ptr(), ws.data_ptr(), ws.numel(),
+                                       _here(rows.table, ended, row_len, row_len_out, extra, extra_out, free_count, free_count_out)))
+
+
+def dag_kv_compact(rows, rows_out, row_len, extra, extra_out, free_count, page_map, copy_src, copy_dst, n_copies):
+    """rows_out may be rows."""
+    n_pages = rows.c.n_pages
+    _ints(rows.c.n_rows, row_len=row_len)
+    _ints(n_pages, extra=extra, extra_out=extra_out, page_map=page_map)
+    _ints(n_pages // 2, copy_src=copy_src, copy_dst=copy_dst)
+    _ints(1, free_count=free_count, n_copies=n_copies)
+    ws = rows.for_shared()
+    _check(lib().dag_kv_compact(rows.c, rows_out.c, row_len.data_ptr(), extra.data_ptr(), extra_out.data_ptr(), free_count.data_ptr(),
+                                page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), n_copies.data_ptr(), ws.data_ptr(), ws.numel(),
+                                _here(rows.table, rows_out.table, row_len, extra, extra_out, free_count, page_map, copy_src, copy_dst,
+                                      n_copies)))
+
+
+def _copies(src, dst, count):
+    _ints(src.numel(), src=src, dst=dst)
+    if count is not None:
+        _ints(1, count=count)
+    return [src, dst] if count is None else [src, dst, count]
+
+
+def dag_kv_copy_pages_q8(cache, src, dst, count=None):
+    """Pages src[i] to dst[i] for all entries, or the first count[0] of them."""
+    there = _copies(src, dst, count)
+    _check(lib().dag_kv_copy_pages_q8(cache.ref, src.data_ptr(), dst.data_ptr(), src.numel(), _at(count), _here(cache.k_pool, *there)))
+
+
+def dag_kv_copy_pages(k_pool, v_pool, src, dst, count=None):
+    """The same for bf16 pools, [pages][heads][d / 8][16][8] and [pages][heads][d][16]."""
+    there = _copies(src, dst, count)
+    n_pages, hkv, d = v_pool.shape[:3]
+    if tuple(v_pool.shape[3:]) != (PAGE,) or tuple(k_pool.shape) != (n_pages, hkv, d // 8, PAGE, 8):
+        raise ValueError("pools are [pages][heads][dim / 8][16][8] and [pages][heads][dim][16]")
+    if any(x.dtype != torch.bfloat16 or not x.is_contiguous() for x in (k_pool, v_pool)):
+        raise TypeError("pools are contiguous bfloat16")
+    _check(lib().dag_kv_copy_pages(k_pool.data_ptr(), v_pool.data_ptr(), n_pages, hkv, d, src.data_ptr(), dst.data_ptr(), src.numel(), _at(count),
+                                   _here(k_pool, v_pool, *there)))
 
 
 class Scheduler:

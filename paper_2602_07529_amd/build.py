@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdagattn.so")
 SOURCES = ["api.hip", "meta.hip", "rope.hip", "prefill_f32.hip", "prefill_bf16.hip", "prefill_bwd.hip", "decode.hip", "sched.hip",
-           "decode_q8.hip", "kv_q8.hip", "kv_tables.hip", "prefill_q8.hip"]
+           "decode_q8.hip", "kv_q8.hip", "kv_tables.hip", "prefill_q8.hip", "rotary.hip", "kv_pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

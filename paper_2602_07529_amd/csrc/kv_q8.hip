@@ -12,6 +12,7 @@
 // 2 x 16 codes are two pieces of the pool as they are; values by lane (two dims), all 16 slots, 32 bytes of the pool.
 // Single tokens (a decode step): a lane has a pair of the key's dims and two of the value's.
 #include "common.h"
+#include "turns.h"
 
 namespace {
 
@@ -30,7 +31,29 @@ struct AppendArgs {
   int64_t n_slots;
   int hkv;
   RopeTheta theta;
+  // rotary positions as a description has them
+  const double* freq;
+  float factor;
+  int rotary;
+  bool pairs;
+  int64_t k_stride, v_stride;  // elements from a token to the next
 };
+
+// Where the element (or the piece of 16) m of the lower half of a head's pairs lies, and its partner: (m, m + half) of the rotated part in the layout
+// of halves, else next to each other; those behind the rotated part, which stay as they are, next to each other too.
+struct Partners {
+  int lo, hi;
+  bool turned, apart;
+};
+__device__ __forceinline__ Partners partners(const AppendArgs& a, int m, int each) {
+  const int half = a.rotary / (2 * each);
+  Partners p;
+  p.turned = m < half;
+  p.apart = p.turned && !a.pairs;
+  p.lo = p.apart ? m : 2 * m;
+  p.hi = p.apart ? m + half : 2 * m + 1;
+  return p;
+}
 
 // 2^k with the smallest k of at least -100 that brings `most` (finite, not negative) within 448 = 0.875 * 2^9.
 __device__ __forceinline__ float q8_scale(float most) {
@@ -89,30 +112,6 @@ struct Raw2 {
   }
 };
 
-// Cosine and sine of x turns: the nearest quarter is taken off exactly, and what is left, an angle y of at most pi / 4, goes through the
-// Taylor series (the terms left out are below 2e-14 there).  A library call for any angle takes three times as long.
-__device__ __forceinline__ void cos_sin_of_turns(double x, float* c, float* s) {
-  const double quarter = rint(4. * x), y = fma(-0.25, quarter, x) * 6.283185307179586477, z = y * y;
-  double sn = 1. / 6227020800., cs = -1. / 87178291200.;
-  sn = fma(sn, z, -1. / 39916800.);
-  sn = fma(sn, z, 1. / 362880.);
-  sn = fma(sn, z, -1. / 5040.);
-  sn = fma(sn, z, 1. / 120.);
-  sn = fma(sn, z, -1. / 6.);
-  sn = fma(sn * z, y, y);
-  cs = fma(cs, z, 1. / 479001600.);
-  cs = fma(cs, z, -1. / 3628800.);
-  cs = fma(cs, z, 1. / 40320.);
-  cs = fma(cs, z, -1. / 720.);
-  cs = fma(cs, z, 1. / 24.);
-  cs = fma(cs, z, -0.5);
-  cs = fma(cs, z, 1.);
-  const int k = (int)((int64_t)quarter & 3);
-  const float u = (float)(k & 1 ? sn : cs), v = (float)(k & 1 ? cs : sn);
-  *c = k == 1 || k == 2 ? -u : u;
-  *s = k >= 2 ? -v : v;
-}
-
 constexpr int SPAN = 16, THREADS = 256;
 template <int D>
 struct Angles {  // of the tokens from a workgroup's first one on; lines four longer: 16 slots read 16 bytes each from all banks
@@ -120,7 +119,7 @@ struct Angles {  // of the tokens from a workgroup's first one on; lines four lo
 };
 
 // A run of n tokens from token t0 on, which go to the slots i0 .. of a page; ang: row of the first one's angles.
-template <int D, bool BF16>
+template <int D, bool BF16, bool ROTARY>
 __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>& angles, int ang, int64_t t0, int n, int64_t page, int i0, int h,
                                            int lane) {
   const bool begins = i0 == 0;
@@ -129,35 +128,54 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>&
   // keys
   const int slot = lane & 15, g = lane >> 4, j = slot - i0;
   const bool active = g < HALF / 16, mine = active && j >= 0 && j < n;
+  const Partners pt = ROTARY ? partners(a, g, 16) : Partners{g, g + HALF / 16, true, true};
   Raw16<BF16> k_lo, k_hi;
   if (mine) {
-    const size_t at = ((size_t)(t0 + j) * a.hkv + h) * D + 16 * g;
-    k_lo.load(a.k_new, at);
-    k_hi.load(a.k_new, at + HALF);
+    const size_t at = ROTARY ? (size_t)(t0 + j) * a.k_stride + h * D : ((size_t)(t0 + j) * a.hkv + h) * D;
+    k_lo.load(a.k_new, at + 16 * pt.lo);
+    k_hi.load(a.k_new, at + 16 * pt.hi);
   }
   // values
   const bool active_v = lane < D / 2;
   Raw2<BF16> v[PAGE] = {};
 #pragma unroll
   for (int i = 0; i < PAGE; ++i)
-    if (active_v && i >= i0 && i < i0 + n) v[i].load(a.v_new, ((size_t)(t0 + i - i0) * a.hkv + h) * D + 2 * lane);
+    if (active_v && i >= i0 && i < i0 + n) v[i].load(a.v_new, (ROTARY ? (size_t)(t0 + i - i0) * a.v_stride + h * D : ((size_t)(t0 + i - i0) * a.hkv + h) * D) + 2 * lane);
   const float before = begins ? 0.f : a.k_scale[ph], before_v = begins ? 0.f : a.v_scale[ph];
   float lo[16], hi[16], most = 0.f;
   if (mine) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float c = angles.cs[ang + j][16 * g + e], s = angles.sn[ang + j][16 * g + e], x = k_lo[e], y = k_hi[e];
-      lo[e] = fmaf(x, c, -(y * s));  // (as dag_kv_append_rope rotates)
-      hi[e] = fmaf(x, s, y * c);
-      most = fmaxf(most, fmaxf(finite_abs(lo[e]), finite_abs(hi[e])));
+      lo[e] = k_lo[e];
+      hi[e] = k_hi[e];
     }
+    if (pt.apart) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float c = angles.cs[ang + j][16 * g + e], s = angles.sn[ang + j][16 * g + e], x = lo[e], y = hi[e];
+        lo[e] = fmaf(x, c, -(y * s));  // (as dag_kv_append_rope rotates)
+        hi[e] = fmaf(x, s, y * c);
+      }
+    } else if (pt.turned) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float c = angles.cs[ang + j][16 * g + e], s = angles.sn[ang + j][16 * g + e];
+        float& u = e < 8 ? lo[2 * (e & 7)] : hi[2 * (e & 7)];
+        float& v2 = e < 8 ? lo[2 * (e & 7) + 1] : hi[2 * (e & 7) + 1];
+        const float x = u, y = v2;
+        u = fmaf(x, c, -(y * s));
+        v2 = fmaf(x, s, y * c);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = fmaxf(most, fmaxf(finite_abs(lo[e]), finite_abs(hi[e])));
   }
   {
     most = dag_wave_max(most);
     const float scale = fmaxf(before, q8_scale(most)), inv = 1.f / scale;
     if (active) {
-      u32x4* const p = (u32x4*)(a.k_pool + ph * (D * PAGE) + g * 256 + slot * 16);
-      u32x4* const q = p + HALF;  // 16 dims = 16 16-byte pieces
+      u32x4* const p = (u32x4*)(a.k_pool + ph * (D * PAGE) + pt.lo * 256 + slot * 16);
+      u32x4* const q = (u32x4*)(a.k_pool + ph * (D * PAGE) + pt.hi * 256 + slot * 16);
       if (mine) {
         u32x4 x, y;
 #pragma unroll
@@ -210,26 +228,28 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>&
 }
 
 // A single token.  Where its page begins or its scale grows the whole page is written, else the token's bytes.
-template <int D, bool BF16>
+template <int D, bool BF16, bool ROTARY>
 __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>& angles, int ang, uint8_t* lds, int64_t t, int64_t page, int i0, int h,
                                            int lane) {
   constexpr int HALF = D / 2;
   const bool begins = i0 == 0, active = lane < HALF;
   const int m = active ? lane : 0;
-  const size_t ph = (size_t)page * a.hkv + h, at = ((size_t)t * a.hkv + h) * D;
+  const size_t ph = (size_t)page * a.hkv + h, at = ROTARY ? (size_t)t * a.k_stride + h * D : ((size_t)t * a.hkv + h) * D;
+  const size_t at_v = ROTARY ? (size_t)t * a.v_stride + h * D : at;
+  const Partners pt = ROTARY ? partners(a, m, 1) : Partners{m, m + HALF, true, true};
   float x, y;
   if constexpr (BF16) {
-    x = __uint_as_float((uint32_t)((const uint16_t*)a.k_new)[at + m] << 16);
-    y = __uint_as_float((uint32_t)((const uint16_t*)a.k_new)[at + m + HALF] << 16);
+    x = __uint_as_float((uint32_t)((const uint16_t*)a.k_new)[at + pt.lo] << 16);
+    y = __uint_as_float((uint32_t)((const uint16_t*)a.k_new)[at + pt.hi] << 16);
   } else {
-    x = ((const float*)a.k_new)[at + m];
-    y = ((const float*)a.k_new)[at + m + HALF];
+    x = ((const float*)a.k_new)[at + pt.lo];
+    y = ((const float*)a.k_new)[at + pt.hi];
   }
   Raw2<BF16> v;
-  v.load(a.v_new, at + 2 * m);
+  v.load(a.v_new, at_v + 2 * m);
   const float before = begins ? 0.f : a.k_scale[ph], before_v = begins ? 0.f : a.v_scale[ph];
-  const float c = angles.cs[ang][m], s = angles.sn[ang][m];
-  const float lo = fmaf(x, c, -(y * s)), hi = fmaf(x, s, y * c);
+  const float c = pt.turned ? angles.cs[ang][m] : 1.f, s = pt.turned ? angles.sn[ang][m] : 0.f;
+  const float lo = pt.turned ? fmaf(x, c, -(y * s)) : x, hi = pt.turned ? fmaf(x, s, y * c) : y;
   const float scale = fmaxf(before, q8_scale(dag_wave_max(fmaxf(finite_abs(lo), finite_abs(hi))))), inv = 1.f / scale;
   const float scale_v = fmaxf(before_v, q8_scale(dag_wave_max(fmaxf(finite_abs(v[0]), finite_abs(v[1]))))), inv_v = 1.f / scale_v;
   const uint32_t ck = codes4(lo * inv, hi * inv, 0.f, 0.f), cv = codes4(v[0] * inv_v, v[1] * inv_v, 0.f, 0.f);
@@ -237,8 +257,8 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>&
   uint8_t* const vp = a.v_pool + ph * (D * PAGE);
   if (begins || scale != before) {
     if (active) {
-      lds[m] = (uint8_t)ck;
-      lds[m + HALF] = (uint8_t)(ck >> 8);
+      lds[pt.lo] = (uint8_t)ck;
+      lds[pt.hi] = (uint8_t)(ck >> 8);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -251,8 +271,8 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>&
       else *p = begins ? u32x4{0, 0, 0, 0} : rescaled(*p, f);
     }
   } else if (active) {
-    kp[m / 16 * 256 + i0 * 16 + m % 16] = (uint8_t)ck;
-    kp[(m + HALF) / 16 * 256 + i0 * 16 + m % 16] = (uint8_t)(ck >> 8);
+    kp[pt.lo / 16 * 256 + i0 * 16 + pt.lo % 16] = (uint8_t)ck;
+    kp[pt.hi / 16 * 256 + i0 * 16 + pt.hi % 16] = (uint8_t)(ck >> 8);
   }
   if (active) {
     if (begins || scale_v != before_v) {
@@ -280,7 +300,7 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>&
   __builtin_amdgcn_wave_barrier();  // (the next head writes the same bytes of LDS, in the order of the instructions)
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool ROTARY>
 __global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendArgs a, int span) {
   __shared__ Angles<D> angles;
   __shared__ __attribute__((aligned(16))) uint8_t one[THREADS / 64][D];
@@ -300,19 +320,65 @@ __global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendAr
   const int begin = __builtin_ctzll(lead), last = 63 - __builtin_clzll(lead), n_ang = last + length(last) - begin;
   {
     const int m = tid % HALF;
-    const double f = dag_rope_freq(a.theta, m, D) * 0.15915494309189533577;  // turns
-    for (int i = tid / HALF; i < n_ang; i += THREADS / HALF) cos_sin_of_turns((double)a.pos[first - 1 + begin + i] * f, &angles.cs[i][m], &angles.sn[i][m]);
+    const bool turned = !ROTARY || m < a.rotary / 2;
+    const double f = (ROTARY ? (turned ? a.freq[m] : 0.) : dag_rope_freq(a.theta, m, D)) * 0.15915494309189533577;  // turns
+    for (int i = tid / HALF; turned && i < n_ang; i += THREADS / HALF) {
+      cos_sin_of_turns((double)a.pos[first - 1 + begin + i] * f, &angles.cs[i][m], &angles.sn[i][m]);
+      if constexpr (ROTARY) {
+        angles.cs[i][m] *= a.factor;
+        angles.sn[i][m] *= a.factor;
+      }
+    }
   }
   __syncthreads();
   for (int x = w; lead; lead &= lead - 1) {
     const int i = __builtin_ctzll(lead), n = length(i);
     const int64_t s0 = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s, i);
     for (; x < a.hkv; x += THREADS / 64) {
-      if (n > 1) append_run<D, BF16>(a, angles, i - begin, first - 1 + i, n, s0 / PAGE, (int)(s0 % PAGE), x, lane);
-      else append_one<D, BF16>(a, angles, i - begin, one[w], first - 1 + i, s0 / PAGE, (int)(s0 % PAGE), x, lane);
+      if (n > 1) append_run<D, BF16, ROTARY>(a, angles, i - begin, first - 1 + i, n, s0 / PAGE, (int)(s0 % PAGE), x, lane);
+      else append_one<D, BF16, ROTARY>(a, angles, i - begin, one[w], first - 1 + i, s0 / PAGE, (int)(s0 % PAGE), x, lane);
     }
     x -= a.hkv;
   }
+}
+
+template <bool ROTARY>
+int launch_append(const AppendArgs& a, int D, dag_dtype_t dtype, hipStream_t stream) {
+  auto* const kernel = dtype == DAG_BF16 ? (D == 128 ? k_kv_append_q8<128, true, ROTARY> : k_kv_append_q8<64, true, ROTARY>)
+                                         : (D == 128 ? k_kv_append_q8<128, false, ROTARY> : k_kv_append_q8<64, false, ROTARY>);
+  const int span = a.n_tokens >= 512 * SPAN ? SPAN : a.n_tokens >= 2048 ? 4 : 1;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)dag_ceil_div(a.n_tokens, span)), dim3(THREADS), 0, stream, a, span);
+  DAG_LAUNCH_CHECK();
+  return DAG_OK;
+}
+
+// What both appends ask of the cache and the tokens (theta and rope apart).
+int check_append(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new, const void* v_new, dag_dtype_t dtype) {
+  const int D = kv->head_dim;
+  if (dtype != DAG_F32 && dtype != DAG_BF16) return DAG_ERR_UNSUPPORTED;
+  if (kv->hkv < 1 || (D != 64 && D != 128)) return DAG_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return DAG_OK;
+  if (!slots || !pos || !k_new || !v_new || !kv->k_pool || !kv->v_pool || !kv->k_scale || !kv->v_scale) return DAG_ERR_NULL;
+  if (!dag_aligned16(k_new) || !dag_aligned16(v_new) || !dag_aligned16(kv->k_pool) || !dag_aligned16(kv->v_pool) ||
+      ((uintptr_t)kv->k_scale & 3) || ((uintptr_t)kv->v_scale & 3))
+    return DAG_ERR_ALIGN;
+  return DAG_OK;
+}
+
+AppendArgs append_args(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new, const void* v_new) {
+  AppendArgs a = {};
+  a.slots = slots;
+  a.pos = pos;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.k_pool = (uint8_t*)kv->k_pool;
+  a.v_pool = (uint8_t*)kv->v_pool;
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.n_tokens = n_tokens;
+  a.n_slots = (int64_t)kv->n_pages * PAGE;
+  a.hkv = kv->hkv;
+  return a;
 }
 
 }  // namespace
@@ -321,20 +387,34 @@ extern "C" int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots
                                      const void* v_new, float theta, dag_dtype_t dtype, void* stream_) {
   if (!kv) return DAG_ERR_NULL;
   if (n_tokens < 0 || n_tokens > INT32_MAX || kv->n_pages < 0) return DAG_ERR_BAD_LEN;
-  const int D = kv->head_dim;
-  if (dtype != DAG_F32 && dtype != DAG_BF16) return DAG_ERR_UNSUPPORTED;
-  if (kv->hkv < 1 || (D != 64 && D != 128) || !(theta > 0.f)) return DAG_ERR_UNSUPPORTED;
+  if (!(theta > 0.f)) return DAG_ERR_UNSUPPORTED;
+  const int rc = check_append(kv, slots, pos, n_tokens, k_new, v_new, dtype);
+  if (rc != DAG_OK || n_tokens == 0) return rc;
+  AppendArgs a = append_args(kv, slots, pos, n_tokens, k_new, v_new);
+  a.theta = dag_rope_theta(theta);
+  return launch_append<false>(a, kv->head_dim, dtype, (hipStream_t)stream_);
+}
+
+extern "C" int dag_kv_append_rotary_q8(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new,
+                                       int64_t k_stride, const void* v_new, int64_t v_stride, const dag_rope_t* rope, dag_dtype_t dtype, void* stream_) {
+  if (!kv || !rope) return DAG_ERR_NULL;
+  if (n_tokens < 0 || n_tokens > INT32_MAX || kv->n_pages < 0) return DAG_ERR_BAD_LEN;
+  const int rc = check_append(kv, slots, pos, n_tokens, k_new, v_new, dtype);
+  if (rc != DAG_OK) return rc;
+  if ((rope->layout != DAG_ROPE_HALVES && rope->layout != DAG_ROPE_PAIRS) || rope->rotary_dim < 32 || rope->rotary_dim % 32 != 0 ||
+      rope->rotary_dim > kv->head_dim)
+    return DAG_ERR_UNSUPPORTED;
   if (n_tokens == 0) return DAG_OK;
-  if (!slots || !pos || !k_new || !v_new || !kv->k_pool || !kv->v_pool || !kv->k_scale || !kv->v_scale) return DAG_ERR_NULL;
-  if (!dag_aligned16(k_new) || !dag_aligned16(v_new) || !dag_aligned16(kv->k_pool) || !dag_aligned16(kv->v_pool) ||
-      ((uintptr_t)kv->k_scale & 3) || ((uintptr_t)kv->v_scale & 3))
-    return DAG_ERR_ALIGN;
-  const AppendArgs a = {slots, pos, k_new, v_new, (uint8_t*)kv->k_pool, (uint8_t*)kv->v_pool, kv->k_scale, kv->v_scale, n_tokens,
-                        (int64_t)kv->n_pages * PAGE, kv->hkv, dag_rope_theta(theta)};
-  auto* const kernel = dtype == DAG_BF16 ? (D == 128 ? k_kv_append_q8<128, true> : k_kv_append_q8<64, true>)
-                                         : (D == 128 ? k_kv_append_q8<128, false> : k_kv_append_q8<64, false>);
-  const int span = n_tokens >= 512 * SPAN ? SPAN : n_tokens >= 2048 ? 4 : 1;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)dag_ceil_div(n_tokens, span)), dim3(THREADS), 0, (hipStream_t)stream_, a, span);
-  DAG_LAUNCH_CHECK();
-  return DAG_OK;
+  const int64_t row = (int64_t)kv->hkv * kv->head_dim, each = dtype == DAG_BF16 ? 8 : 4;
+  if (k_stride < row || v_stride < row) return DAG_ERR_BAD_LEN;
+  if (!rope->freq) return DAG_ERR_NULL;
+  if (k_stride % each != 0 || v_stride % each != 0 || ((uintptr_t)rope->freq & 7)) return DAG_ERR_ALIGN;
+  AppendArgs a = append_args(kv, slots, pos, n_tokens, k_new, v_new);
+  a.freq = rope->freq;
+  a.factor = rope->factor;
+  a.rotary = rope->rotary_dim;
+  a.pairs = rope->layout == DAG_ROPE_PAIRS;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  return launch_append<true>(a, kv->head_dim, dtype, (hipStream_t)stream_);
 }

@@ -7,12 +7,11 @@
 // few of them.  Lengths and the number of free pages may be written where they were read, so the workgroup that comes last writes
 // them, when all have read.  More rows: a scan by one workgroup, then a launch that writes the lists.  What bounds it is launches and the
 // chain of loads behind one another (length, free page or line, lists), not bytes.
-#include "common.h"
+#include "kv_rows.h"
 
 namespace {
 
-constexpr int PAGE = DAG_PAGE_SIZE;
-constexpr int ROW_THREADS = 1024, LIST_THREADS = 256;
+constexpr int LIST_THREADS = 256;
 constexpr int ONE_ROWS = ROW_THREADS, ONE_WAVES = ROW_THREADS / 64;
 
 struct TableArgs {
@@ -35,29 +34,6 @@ struct TableArgs {
   int32_t* held;   // [n_rows] workspace: tokens before
   uint32_t* ticket;  // workspace: zero between calls
 };
-
-__device__ __forceinline__ int64_t pages_of(int64_t n) { return (n + PAGE - 1) / PAGE; }
-
-// Sums over the threads in front of this one of N values each, and over all threads.
-template <int N>
-__device__ __forceinline__ void block_scan(int64_t (&x)[N], int64_t (&all)[N]) {
-  __shared__ int64_t s_wave[N][ROW_THREADS / 64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t incl[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    incl[i] = dag_wave_scan(x[i]);
-    if (lane == 63) s_wave[i][w] = incl[i];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int64_t v = lane < (int)(blockDim.x >> 6) ? s_wave[i][lane] : 0, s = dag_wave_scan(v);
-    all[i] = dag_readlane(s, 63);
-    x[i] = incl[i] - x[i] + (w > 0 ? dag_readlane(s, w - 1) : 0);
-  }
-  __syncthreads();
-}
 
 // Sums of many rows by one workgroup, PER_THREAD of them to a thread, as a turn is loads and scans behind one another (release and tables of 4096
 // rows, replayed: 29.6 us with one to a thread, 25.1 with four).
