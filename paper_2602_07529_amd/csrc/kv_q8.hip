@@ -11,6 +11,8 @@
 // sines once for all heads (in LDS) and its waves share out (run, head).  Long runs: keys by lane (slot, 16 dims and their partners), whose
 // 2 x 16 codes are two pieces of the pool as they are; values by lane (two dims), all 16 slots, 32 bytes of the pool.
 // Single tokens (a decode step): a lane has a pair of the key's dims and two of the value's.
+#include <type_traits>
+
 #include "common.h"
 #include "turns.h"
 
@@ -113,14 +115,28 @@ struct Raw2 {
 };
 
 constexpr int SPAN = 16, THREADS = 256;
-template <int D>
+template <bool ROTARY>
+using Angle = std::conditional_t<ROTARY, double, float>;
+// x cos - y sin and x sin + y cos (as dag_kv_append_rope rotates, in 32 bits).
+__device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
+  const float a = fmaf(x, c, -(y * s)), b = fmaf(x, s, y * c);
+  x = a;
+  y = b;
+}
+__device__ __forceinline__ void turn(float& x, float& y, double c, double s) {
+  const double u = x, v = y;
+  x = (float)fma(u, c, -(v * s));
+  y = (float)fma(u, s, v * c);
+}
+// (ROTARY: in 64 bits, and the rotation too: of 20000 x 8 keys of 128 a code in 25000 is another one otherwise, for the same time)
+template <int D, typename T>
 struct Angles {  // of the tokens from a workgroup's first one on; lines four longer: 16 slots read 16 bytes each from all banks
-  float cs[SPAN + PAGE - 1][D / 2 + 4], sn[SPAN + PAGE - 1][D / 2 + 4];
+  T cs[SPAN + PAGE - 1][D / 2 + 4], sn[SPAN + PAGE - 1][D / 2 + 4];
 };
 
 // A run of n tokens from token t0 on, which go to the slots i0 .. of a page; ang: row of the first one's angles.
 template <int D, bool BF16, bool ROTARY>
-__device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>& angles, int ang, int64_t t0, int n, int64_t page, int i0, int h,
+__device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D, Angle<ROTARY>>& angles, int ang, int64_t t0, int n, int64_t page, int i0, int h,
                                            int lane) {
   const bool begins = i0 == 0;
   const size_t ph = (size_t)page * a.hkv + h;
@@ -152,19 +168,14 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>&
     if (pt.apart) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float c = angles.cs[ang + j][16 * g + e], s = angles.sn[ang + j][16 * g + e], x = lo[e], y = hi[e];
-        lo[e] = fmaf(x, c, -(y * s));  // (as dag_kv_append_rope rotates)
-        hi[e] = fmaf(x, s, y * c);
+        turn(lo[e], hi[e], angles.cs[ang + j][16 * g + e], angles.sn[ang + j][16 * g + e]);
       }
     } else if (pt.turned) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float c = angles.cs[ang + j][16 * g + e], s = angles.sn[ang + j][16 * g + e];
-        float& u = e < 8 ? lo[2 * (e & 7)] : hi[2 * (e & 7)];
-        float& v2 = e < 8 ? lo[2 * (e & 7) + 1] : hi[2 * (e & 7) + 1];
-        const float x = u, y = v2;
-        u = fmaf(x, c, -(y * s));
-        v2 = fmaf(x, s, y * c);
+        float& x = e < 8 ? lo[2 * (e & 7)] : hi[2 * (e & 7)];
+        float& y = e < 8 ? lo[2 * (e & 7) + 1] : hi[2 * (e & 7) + 1];
+        turn(x, y, angles.cs[ang + j][16 * g + e], angles.sn[ang + j][16 * g + e]);
       }
     }
 #pragma unroll
@@ -229,7 +240,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D>&
 
 // A single token.  Where its page begins or its scale grows the whole page is written, else the token's bytes.
 template <int D, bool BF16, bool ROTARY>
-__device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>& angles, int ang, uint8_t* lds, int64_t t, int64_t page, int i0, int h,
+__device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D, Angle<ROTARY>>& angles, int ang, uint8_t* lds, int64_t t, int64_t page, int i0, int h,
                                            int lane) {
   constexpr int HALF = D / 2;
   const bool begins = i0 == 0, active = lane < HALF;
@@ -248,8 +259,8 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>&
   Raw2<BF16> v;
   v.load(a.v_new, at_v + 2 * m);
   const float before = begins ? 0.f : a.k_scale[ph], before_v = begins ? 0.f : a.v_scale[ph];
-  const float c = pt.turned ? angles.cs[ang][m] : 1.f, s = pt.turned ? angles.sn[ang][m] : 0.f;
-  const float lo = pt.turned ? fmaf(x, c, -(y * s)) : x, hi = pt.turned ? fmaf(x, s, y * c) : y;
+  float lo = x, hi = y;
+  if (pt.turned) turn(lo, hi, angles.cs[ang][m], angles.sn[ang][m]);
   const float scale = fmaxf(before, q8_scale(dag_wave_max(fmaxf(finite_abs(lo), finite_abs(hi))))), inv = 1.f / scale;
   const float scale_v = fmaxf(before_v, q8_scale(dag_wave_max(fmaxf(finite_abs(v[0]), finite_abs(v[1]))))), inv_v = 1.f / scale_v;
   const uint32_t ck = codes4(lo * inv, hi * inv, 0.f, 0.f), cv = codes4(v[0] * inv_v, v[1] * inv_v, 0.f, 0.f);
@@ -302,7 +313,7 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D>&
 
 template <int D, bool BF16, bool ROTARY>
 __global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendArgs a, int span) {
-  __shared__ Angles<D> angles;
+  __shared__ Angles<D, Angle<ROTARY>> angles;
   __shared__ __attribute__((aligned(16))) uint8_t one[THREADS / 64][D];
   constexpr int HALF = D / 2;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;

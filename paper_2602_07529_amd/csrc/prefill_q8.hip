@@ -20,7 +20,6 @@ typedef __attribute__((ext_vector_type(8))) int i32x8;
 constexpr int PAGE = DAG_PAGE_SIZE;
 constexpr int TILE = 4;          // pages
 constexpr int MAX_SPLITS = 64;   // (the lanes of the wave that puts them together)
-constexpr int waves_of(int D) { return 8; }
 
 struct ChunkArgs {
   Q8Cache kv;
@@ -37,37 +36,53 @@ struct ChunkArgs {
   float* part_ml;  // the same [2]: reference in the exponent's units, sum
   int n_nodes, n_rows, max_new, max_ctx_pages, hq, G;
   int splits, slice;  // stretches of a context, tiles in each
+  int blocks;         // of 32 pairs to a node (nodes with few pairs)
+  int few_rows;       // pairs that a block of them may have
   float sc;           // softmax_scale * log2(e)
 };
 
-// What a slot of the launch is: slot x holds pairs 32 NW (x - first slot of the node) .. of the node with the largest first slot up to x,
-// the first slot of node i being floor(G q_off[i] / 32 NW) + i: as many as its pairs fill, and known without a scan.
+// New tokens of a node times query heads of a KV head, up to which they are k_q8_chunk_few's.
+constexpr int FEW_PAIRS = 64;
+
+// The pairs pair0 .. of a node, n new tokens from row0 on; pages / np: its list, nstart: place of its first new token in it.
 struct Place {
   int row0, n, pair0, pages, np, nstart;
 };
 __device__ __forceinline__ int64_t first_row(const ChunkArgs& a, int i) { return min(max(a.q_off[i], 0), a.n_rows); }
+__device__ __forceinline__ void node_place(const ChunkArgs& a, int i, Place* p) {
+  const int64_t r0 = first_row(a, i), r1 = first_row(a, i + 1);
+  p->row0 = (int)r0;
+  p->n = (int)max(min(r1 - r0, (int64_t)a.max_new), (int64_t)0);
+  p->pages = a.ctx_page_off[i];
+  p->np = min(max(a.ctx_page_off[i + 1] - p->pages, 0), a.max_ctx_pages);
+  p->nstart = a.own_page[i] * PAGE + a.own_len[i] - (int)(r1 - r0);
+}
+// Slot x holds pairs PAIRS (x - first slot of the node) .. of the node with the largest first slot up to x, the first slot of node i being
+// floor(G q_off[i] / PAIRS) + i: at least as many as its pairs fill, and known without a scan.
 template <int PAIRS>
 __device__ __forceinline__ bool find_place(const ChunkArgs& a, int64_t slot, int lane, Place* p) {
   int lo = 0, hi = a.n_nodes;
   while (hi > lo) {  // 64 nodes of [lo, hi) a turn; the last one whose first slot is not behind
-    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-    const bool ok = i < hi && lane * (int64_t)step < hi - lo && first_row(a, i) * a.G / PAIRS + i <= slot;
+    const int step = (hi - lo + 63) / 64;
+    const int64_t i = lo + lane * (int64_t)step;
+    const bool ok = i < hi && first_row(a, (int)i) * a.G / PAIRS + i <= slot;
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(ok));
     if (n == 0) return false;
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
     if (step == 1) break;
   }
-  const int64_t r0 = first_row(a, lo);
-  p->n = (int)min(first_row(a, lo + 1) - r0, (int64_t)a.max_new);
-  p->row0 = (int)r0;
-  const int64_t pair0 = (slot - (r0 * a.G / PAIRS + lo)) * PAIRS;
-  if (pair0 >= (int64_t)p->n * a.G) return false;
+  node_place(a, lo, p);
+  const int64_t pair0 = (slot - ((int64_t)p->row0 * a.G / PAIRS + lo)) * PAIRS;
+  if (pair0 >= (int64_t)p->n * a.G || p->n * a.G <= FEW_PAIRS) return false;
   p->pair0 = (int)pair0;
-  p->pages = a.ctx_page_off[lo];
-  p->np = min(max(a.ctx_page_off[lo + 1] - p->pages, 0), a.max_ctx_pages);
-  p->nstart = a.own_page[lo] * PAGE + a.own_len[lo] - (int)(first_row(a, lo + 1) - r0);
   return true;
+}
+// Slot x of the nodes with few pairs: block x % blocks of 32 pairs of node x / blocks.
+__device__ __forceinline__ bool few_place(const ChunkArgs& a, int64_t slot, Place* p) {
+  node_place(a, (int)(slot / a.blocks), p);
+  p->pair0 = (int)(slot % a.blocks) * 32;
+  return p->n * a.G <= FEW_PAIRS && p->pair0 < p->n * a.G;
 }
 
 __device__ __forceinline__ void lds_barrier() {  // (loads from memory stay on their way)
@@ -144,7 +159,16 @@ __device__ __forceinline__ void split_q(QueryCodes<D>& y, const bf16x8 (&q)[D / 
 // the rows that do not see it, and a probability of zero does not keep it from them.  Such values are cleared here, and the sums of the rows
 // that see one become no number: a product of "is none" and "is seen" finds them.
 template <int D>
-__device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, int t0, int t1, int hk, int row, int head, int lim, int L, int H,
+__device__ __forceinline__ bool no_number(const f32x16 (&O)[D / 32]) {  // has been among the values
+  float any = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) any = fmaf(O[db][r], 0.f, any);
+  return __builtin_amdgcn_ballot_w64(any != any) != 0;
+}
+template <int D>
+__device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, int p0, int p1, int hk, int row, int head, int lim, int L, int H,
                                         f32x16 (&O)[D / 32], float& m, float& l) {
   bf16x8 q[D / 16];
   fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, L + 32 * H);
@@ -155,14 +179,14 @@ __device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, 
     for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
   m = -1e30f;
   l = 0.f;
-  for (int pg0 = TILE * t0; pg0 < min(TILE * t1, pl.np); pg0 += 2) {
+  for (int pg0 = p0; pg0 < p1; pg0 += 2) {
     int64_t at[2];
     int len[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const size_t e = (size_t)pl.pages + min(pg0 + i, pl.np - 1);
+      const size_t e = (size_t)pl.pages + min(pg0 + i, p1 - 1);
       at[i] = (int64_t)min(max(a.ctx_pages[e], 0), a.kv.n_pages - 1) * a.kv.hkv + hk;
-      len[i] = pg0 + i < pl.np ? min(max(a.ctx_page_len[e], 0), PAGE) : 0;
+      len[i] = pg0 + i < p1 ? min(max(a.ctx_page_len[e], 0), PAGE) : 0;
     }
     const size_t mine = H ? at[1] : at[0], key = L >> 2 & 1 ? at[1] : at[0];
     const int plen = H ? len[1] : len[0], n = min(plen, lim - (pg0 + H) * PAGE + 1);
@@ -221,6 +245,31 @@ __device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, 
   }
 }
 
+template <int D>
+__device__ __forceinline__ void store_part(const ChunkArgs& a, size_t at, const f32x16 (&O)[D / 32], float m, float l, int H) {
+  float* const po = a.part_o + at * D;
+  if (l != 0.f)  // (nobody reads it otherwise)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) *(f32x4*)(po + 32 * db + 8 * r + 4 * H) = f32x4{O[db][4 * r], O[db][4 * r + 1], O[db][4 * r + 2], O[db][4 * r + 3]};
+  if (H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(m, l);
+}
+template <int D>
+__device__ __forceinline__ void store_out(const ChunkArgs& a, size_t at, const f32x16 (&O)[D / 32], float m, float l, int H) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      u32x2 y;
+      y[0] = dag_pack_bf2(O[db][4 * r] * inv, O[db][4 * r + 1] * inv);
+      y[1] = dag_pack_bf2(O[db][4 * r + 2] * inv, O[db][4 * r + 3] * inv);
+      *(u32x2*)(a.out + at * D + 32 * db + 8 * r + 4 * H) = y;
+    }
+  if (a.lse && H == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
 constexpr float TOP_SUM = 1073741824.f;  // of a block's probabilities relative to the reference: 2^30
 
 template <int D, int NW>
@@ -241,6 +290,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
   const int lim_last = pl.nstart + (pl.pair0 + n_pairs - 1) / a.G;
   const int nt = lim_last < 0 ? 0 : min((pl.np + TILE - 1) / TILE, lim_last / (TILE * PAGE) + 1);
   const int t0 = min(split * a.slice, nt), t1 = min(t0 + a.slice, nt);
+  const bool idle = 32 * w >= n_pairs;
 
   f32x16 O[D / 32];
 #pragma unroll
@@ -478,6 +528,13 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
     float2 page0 = lds.page[t0 & 3][H], page1 = lds.page[t0 & 3][2 + H];
     for (int t = t0; t < t1; ++t) {
       lds_barrier();
+      if (idle) {  // no row is this wave's: it fetches its share and leaves the matrix pipe to the others
+        store_v(v_next);
+        load_v(t + 2);
+        store_k(t + 2);
+        window(t + 3);
+        load_k(t + 3);
+      } else {
       step(S0, S1, P[0], P[1], page0, t, 0, !f0, [&]() __attribute__((always_inline)) {
         store_v(v_next);
         load_v(t + 2);
@@ -490,6 +547,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         f3 = is_full(t + 3);
         page1 = lds.page[(t + 1) & 3][2 + H];
       });
+      }
       v_old = v_now;
       v_now = v_next;
       v_next = v_next == 2 ? 0 : v_next + 1;
@@ -502,52 +560,206 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       product(i, P[1]);
       if (i + AHEAD < NV) read_v(i + AHEAD, v_old, 1);
     }
-    float any = 0.f;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) any = fmaf(O[db][r], 0.f, any);
-    if (__builtin_amdgcn_ballot_w64(any != any) != 0) {  // a value that is no number has been among them
-      sums_again<D>(a, pl, t0, t1, hk, row, head, lim, L, H, O, m, l);
+    if (no_number<D>(O)) {
+      sums_again<D>(a, pl, TILE * t0, min(TILE * t1, pl.np), hk, row, head, lim, L, H, O, m, l);
     }
     l += other_half(l);
   }
 
   if (32 * w + L >= n_pairs) return;
-  if (a.splits > 1) {
-    const size_t at = (((size_t)slot * hkv + hk) * a.splits + split) * PAIRS + 32 * w + L;
-    float* const po = a.part_o + at * D;
-    if (t0 < t1)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) *(f32x4*)(po + 32 * db + 8 * r + 4 * H) = f32x4{O[db][4 * r], O[db][4 * r + 1], O[db][4 * r + 2], O[db][4 * r + 3]};
-    if (H == 0) *(float2*)(a.part_ml + at * 2) = make_float2(m, l);
-    return;
-  }
-  const size_t at = (size_t)(pl.row0 + row) * a.hq + head;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (a.splits > 1) store_part<D>(a, (((size_t)slot * hkv + hk) * a.splits + split) * PAIRS + 32 * w + L, O, m, l, H);
+  else store_out<D>(a, (size_t)(pl.row0 + row) * a.hq + head, O, m, l, H);
+}
+
+// Few pairs: 32 of them to a workgroup, whose waves share a stretch of the pages, each a run of its own, straight from memory, and put their sums
+// together in LDS.  What bounds it is how the pages come: two blocks of two pages of a wave are on their way.
+constexpr int FEW_WAVES = 8;
+template <int D>
+__global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float s_o[];  // [wave][pair][D + 4], of as many pairs as a block may have
+  __shared__ float2 s_ml[FEW_WAVES][32];
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, L = lane & 31, H = lane >> 5;
+  const int hkv = a.kv.hkv, hk = blockIdx.x % hkv, split = blockIdx.x / hkv % a.splits;
+  const int64_t slot = blockIdx.x / hkv / a.splits;
+  Place pl;
+  if (!few_place(a, slot, &pl)) return;
+  const int n_pairs = min(32, pl.n * a.G - pl.pair0);
+  const int pair = min(pl.pair0 + L, pl.n * a.G - 1), row = pair / a.G, head = hk * a.G + pair % a.G;
+  const int lim = pl.nstart + row, lim_first = pl.nstart + pl.pair0 / a.G, lim_last = pl.nstart + (pl.pair0 + n_pairs - 1) / a.G;
+  const int np = lim_last < 0 ? 0 : min(pl.np, lim_last / PAGE + 1), slice = a.slice * TILE;
+  const int s0 = min(split * slice, np), s1 = min(s0 + slice, np), each = ((s1 - s0 + FEW_WAVES - 1) / FEW_WAVES + 1) & ~1;
+  const int p0 = min(s0 + w * each, s1), p1 = min(p0 + each, s1);
+
+  f32x16 O[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      u32x2 y;
-      y[0] = dag_pack_bf2(O[db][4 * r] * inv, O[db][4 * r + 1] * inv);
-      y[1] = dag_pack_bf2(O[db][4 * r + 2] * inv, O[db][4 * r + 3] * inv);
-      *(u32x2*)(a.out + at * D + 32 * db + 8 * r + 4 * H) = y;
+    for (int r = 0; r < 16; ++r) O[db][r] = 0.f;
+  float m = -1e30f, l = 0.f;
+  if (p0 < p1) {
+    struct Ahead {
+      u32x4 k[D / 32], v[D / 32];
+      float ks, lv;
+      int len[2];
+    } x[2];
+    // 64 pages, a lane each
+    int pg, len;
+    float2 scales;
+    auto load = [&](Ahead& y, int rel) __attribute__((always_inline)) {  // pages p0 + rel, + 1
+      const bool first = (rel & 63) == 0 && p0 + rel < p1;
+      if (first) {
+        const int i = p0 + rel + lane;
+        const size_t e = (size_t)pl.pages + min(i, p1 - 1);
+        pg = min(max(a.ctx_pages[e], 0), a.kv.n_pages - 1);
+        len = i < p1 ? min(max(a.ctx_page_len[e], 0), PAGE) : 0;
+        const size_t ph = (size_t)pg * hkv + hk;
+        scales = make_float2(a.kv.k_scale[ph], a.kv.v_scale[ph]);
+      }
+      size_t base[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) base[i] = ((size_t)__builtin_amdgcn_readlane(pg, (rel + i) & 63) * hkv + hk) * (D * PAGE);
+      const uint8_t* const kp = a.kv.k_pool + (L >> 2 & 1 ? base[1] : base[0]) + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16;
+      const uint8_t* const vp = a.kv.v_pool + (H ? base[1] : base[0]) + L * 16;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) y.k[s] = *(const u32x4*)(kp + s * 512);
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) y.v[s] = *(const u32x4*)(vp + s * 512);
+      if (first) {
+        scales = page_scales(a, scales.x, scales.y, len);
+        asm volatile("" ::"v"(scales.x), "v"(scales.y));  // (arrived: a wait for them later would also wait for the blocks in flight)
+      }
+      auto of = [&](float z, int i) __attribute__((always_inline)) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(z), (rel + i) & 63)); };
+      y.ks = H ? of(scales.x, 1) : of(scales.x, 0);
+      y.lv = H ? of(scales.y, 1) : of(scales.y, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) y.len[i] = p0 + rel + i < p1 ? __builtin_amdgcn_readlane(len, (rel + i) & 63) : 0;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    load(x[0], 0);
+    bf16x8 q[D / 16];
+    fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
+    sign_q<D>(q, a.sc);
+    auto compute = [&](Ahead& y, int rel) __attribute__((always_inline)) {
+      f32x16 S;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[r] = 0.f;
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) S = mfma32(codes_to_bf16(y.k[s >> 1][2 * (s & 1)], y.k[s >> 1][2 * (s & 1) + 1]), q[s], S);
+      float pks = y.ks, plv = y.lv;
+      const int pos = (p0 + rel) * PAGE;
+      if (y.len[0] < PAGE || y.len[1] < PAGE || pos + 2 * PAGE - 1 > lim_first) {
+        asm volatile("");  // (a branch: the compiler would compare and select in every block)
+        const int plen = H ? y.len[1] : y.len[0], n = min(plen, lim - (pos + H * PAGE) + 1);  // slots that the row sees
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = r < n ? S[r] : -INFINITY;
+        if (n <= 0) pks = 1.f, plv = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // slots without a token may hold any codes
+          const uint32_t mask = slots_mask(plen - 4 * e);
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) y.v[db][e] &= mask;
+        }
+      }
+      float bm = S[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) bm = fmaxf(bm, S[r]);
+      bm *= pks;
+      bm = fmaxf(bm, other_half(bm));
+      if (__builtin_amdgcn_ballot_w64(bm > m + 3.f) != 0) {
+        const float m_new = fmaxf(m, bm), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[db][r] *= alpha;
+        m = m_new;
+      }
+      const float ref = plv - m;
+      float sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // (one half behind the other: registers)
+        f32x8 e;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          e[r] = __builtin_amdgcn_exp2f(fmaf(S[8 * h + r], pks, ref));
+          sum += e[r];
+        }
+        const bf16x8 p = __builtin_convertvector(e, bf16x8);  // (rounded to bf16, as the probabilities over a bf16 cache are)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(y.v[db][2 * h], y.v[db][2 * h + 1]), p, O[db]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l = fmaf(sum, __builtin_amdgcn_exp2f(-plv), l);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // (no load and no block behind a condition: what is fetched behind the run is of pages of the window, and counts as pages without tokens)
+    for (int rel = 0; rel < p1 - p0; rel += 4) {
+      load(x[1], rel + 2);
+      compute(x[0], rel);
+      load(x[0], rel + 4);
+      compute(x[1], rel + 2);
     }
-  if (a.lse && H == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    if (no_number<D>(O)) sums_again<D>(a, pl, p0, p1, hk, row, head, lim, L, H, O, m, l);
+    l += other_half(l);
+  }
+
+  // The sums of all waves, added up in their order: 16 threads to a pair, eight (or four) dims each.
+  constexpr int LINE = D + 4, EACH = D / 16;
+  if (H == 0) s_ml[w][L] = make_float2(m, l);
+  if (L < a.few_rows && l != 0.f) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(f32x4*)&s_o[(w * a.few_rows + L) * LINE + 32 * db + 8 * r + 4 * H] = f32x4{O[db][4 * r], O[db][4 * r + 1], O[db][4 * r + 2], O[db][4 * r + 3]};
+  }
+  __syncthreads();
+  const int mine = tid / 16, d0 = tid % 16 * EACH;
+  if (mine >= n_pairs) return;
+  float top = -1e30f, total = 0.f, weight[FEW_WAVES], o[EACH] = {};
+#pragma unroll
+  for (int i = 0; i < FEW_WAVES; ++i) top = fmaxf(top, s_ml[i][mine].y != 0.f ? s_ml[i][mine].x : -1e30f);
+#pragma unroll
+  for (int i = 0; i < FEW_WAVES; ++i) {
+    const float2 ml = s_ml[i][mine];
+    weight[i] = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    total = fmaf(ml.y, weight[i], total);
+    if (ml.y != 0.f) {
+#pragma unroll
+      for (int e = 0; e < EACH; e += 4) {
+        const f32x4 y = *(const f32x4*)&s_o[(i * a.few_rows + mine) * LINE + d0 + e];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[e + j] = fmaf(y[j], weight[i], o[e + j]);
+      }
+    }
+  }
+  if (a.splits > 1) {
+    const size_t at = (((size_t)slot * hkv + hk) * a.splits + split) * 32 + mine;
+#pragma unroll
+    for (int e = 0; e < EACH; e += 4) *(f32x4*)(a.part_o + at * D + d0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+    if (d0 == 0) *(float2*)(a.part_ml + at * 2) = make_float2(top, total);
+    return;
+  }
+  const int p = pl.pair0 + mine;
+  const size_t at = (size_t)(pl.row0 + p / a.G) * a.hq + hk * a.G + p % a.G;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  uint32_t y[EACH / 2];
+#pragma unroll
+  for (int e = 0; e < EACH / 2; ++e) y[e] = dag_pack_bf2(o[2 * e] * inv, o[2 * e + 1] * inv);
+  if constexpr (EACH == 8) *(u32x4*)(a.out + at * D + d0) = u32x4{y[0], y[1], y[EACH / 2 - 2], y[EACH / 2 - 1]};
+  else *(u32x2*)(a.out + at * D + d0) = u32x2{y[0], y[1]};
+  if (a.lse && d0 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
 // Puts the stretches of a context together, in their order: a wave to a pair, a lane to a stretch and then to D / 64 dims.
-template <int D, int NW>
+template <int D, int PAIRS, bool FEW>
 __global__ void __launch_bounds__(256) k_q8_chunk_merge(ChunkArgs a) {
-  constexpr int PAIRS = 32 * NW, EACH = D / 64;
+  constexpr int EACH = D / 64;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hkv = a.kv.hkv;
   const int part = blockIdx.x % (PAIRS / 4), hk = blockIdx.x / (PAIRS / 4) % hkv;
   const int64_t slot = blockIdx.x / (PAIRS / 4) / hkv;
   Place pl;
-  if (!find_place<PAIRS>(a, slot, lane, &pl)) return;
+  if (!(FEW ? few_place(a, slot, &pl) : find_place<PAIRS>(a, slot, lane, &pl))) return;
   const int mine = part * 4 + w, pair = pl.pair0 + mine;
   if (pair >= pl.n * a.G) return;
   const size_t at = ((size_t)slot * hkv + hk) * a.splits * PAIRS + mine;
@@ -571,21 +783,62 @@ __global__ void __launch_bounds__(256) k_q8_chunk_merge(ChunkArgs a) {
   if (a.lse && lane == 0) a.lse[to] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
-struct Plan {
+// How the contexts are cut: `splits` stretches of `slice` tiles, for `slots` blocks of `pairs` pairs.
+struct Cut {
   int64_t slots;
-  int splits, slice;
+  int splits, slice, pairs;
+  size_t parts(int hkv) const { return splits > 1 ? (size_t)slots * hkv * splits * pairs : 0; }
 };
-// By the host's bounds.  Compute units of the device with two workgroups each; contexts are cut while there are fewer items than that.
-bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, int pairs, Plan* p) {
-  const int64_t G = hq / hkv, tiles = dag_ceil_div(d->max_ctx_pages, TILE);
-  p->slots = d->max_new == 0 || d->n_nodes == 0 ? 0 : n_rows * G / pairs + d->n_nodes;  // (the last node's last one is below: find_place)
-  const int64_t items = p->slots * hkv, at_once = 512;
-  int64_t splits = 1;
-  if (items > 0 && items < at_once) splits = std::min<int64_t>({at_once / items, dag_ceil_div(tiles, 4), MAX_SPLITS});
-  splits = std::max<int64_t>(1, splits);
-  p->slice = (int)std::max<int64_t>(1, dag_ceil_div(tiles, splits));
-  p->splits = (int)std::max<int64_t>(1, dag_ceil_div(tiles, p->slice));
-  return p->slots * hkv * p->splits <= (int64_t)1 << 23 && p->slots * hkv * (p->splits > 1 ? pairs / 4 : 1) <= (int64_t)1 << 23;  // (threads are counted in 32 bits)
+struct Plan {
+  Cut few, many;  // slots 0: not launched
+  int blocks, few_rows, waves;
+  size_t floats(int hkv, int D) const { return (few.parts(hkv) + many.parts(hkv)) * (D + 2); }
+};
+// As many stretches as take the least time: rounds of the workgroups that the device holds at once, each as long as its steps through a stretch
+// and what a workgroup costs apart from them, then the second launch and the partial results, which are written and read.  In microseconds.
+struct Cost {
+  double tile, each, merge;
+  int at_once;
+};
+void cut(Cut* c, double items, int64_t tiles, int D, const Cost& cost) {
+  double best = 1e300;
+  c->splits = 1;
+  c->slice = (int)std::max<int64_t>(tiles, 1);
+  for (int s = 1; s <= MAX_SPLITS && s <= std::max<int64_t>(tiles, 1); ++s) {
+    const int64_t slice = dag_ceil_div(std::max<int64_t>(tiles, 1), s);
+    if (dag_ceil_div(std::max<int64_t>(tiles, 1), slice) != s) continue;
+    double time = std::ceil(items * s / cost.at_once) * (slice * cost.tile + cost.each);
+    if (s > 1) time += cost.merge + items * s * c->pairs * (D + 2) * 8. / 4e6;
+    if (time < best * 0.97) {
+      best = time;
+      c->splits = s;
+      c->slice = (int)slice;
+    }
+  }
+}
+// By the host's bounds.  The device has 256 compute units.
+bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, int D, Plan* p) {
+  const int64_t G = hq / hkv, tiles = dag_ceil_div(d->max_ctx_pages, TILE), most = d->max_new * G;
+  const bool none = d->max_new == 0 || d->n_nodes == 0 || n_rows == 0;
+  p->few = p->many = Cut{0, 1, 1, 32};
+  p->blocks = (int)std::max<int64_t>(1, dag_ceil_div(std::min<int64_t>(most, FEW_PAIRS), 32));
+  p->few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, 32));
+  // (few new tokens in all: a node with more is a tile kernel's, which has a slot for it wherever there is one)
+  if (!none) {
+    p->few.slots = (int64_t)d->n_nodes * p->blocks;
+    // (a tile is a quarter of a step of the eight waves)
+    cut(&p->few, (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv, tiles, D, Cost{0.25, 5., 4., 256});
+  }
+  p->waves = most <= 128 ? 4 : 8;
+  if (!none && most > FEW_PAIRS) {
+    p->many.pairs = 32 * p->waves;
+    p->many.slots = n_rows * G / p->many.pairs + d->n_nodes;  // (the last node's last one is below: find_place)
+    const double items = d->n_nodes == 1 ? (double)dag_ceil_div(n_rows * G, p->many.pairs) : (double)n_rows * G / p->many.pairs + 0.5 * d->n_nodes;
+    cut(&p->many, items * hkv, tiles, D, p->waves == 4 ? Cost{D / 64., 6., 5., 512} : Cost{D / 64., 6., 5., 256});
+  }
+  for (const Cut* c : {&p->few, &p->many})  // (threads of a launch are counted in 32 bits)
+    if (c->slots * hkv * c->splits > (int64_t)1 << 22 || (c->splits > 1 && c->slots * hkv * (c->pairs / 4) > (int64_t)1 << 23)) return false;
+  return true;
 }
 
 bool bounds_ok(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim) {
@@ -593,25 +846,50 @@ bool bounds_ok(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, in
          hq >= 1 && hq % hkv == 0 && hq / hkv <= 256 && (int64_t)d->max_new * (hq / hkv) <= INT32_MAX && (head_dim == 64 || head_dim == 128);
 }
 
-template <int D>
-int launch(const ChunkArgs& a, const Plan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((k_q8_chunk<D, waves_of(D)>), dim3((unsigned)(p.slots * a.kv.hkv * p.splits)), dim3(64 * waves_of(D)), 0, stream, a);
+template <int D, int NW>
+int launch_many(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
+  hipLaunchKernelGGL((k_q8_chunk<D, NW>), dim3((unsigned)(c.slots * a.kv.hkv * c.splits)), dim3(64 * NW), 0, stream, a);
   DAG_LAUNCH_CHECK();
-  if (p.splits > 1) {
-    hipLaunchKernelGGL((k_q8_chunk_merge<D, waves_of(D)>), dim3((unsigned)(p.slots * a.kv.hkv * (32 * waves_of(D) / 4))), dim3(256), 0, stream, a);
+  if (c.splits > 1) {
+    hipLaunchKernelGGL((k_q8_chunk_merge<D, 32 * NW, false>), dim3((unsigned)(c.slots * a.kv.hkv * (32 * NW / 4))), dim3(256), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+  }
+  return DAG_OK;
+}
+template <int D>
+int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
+  a.blocks = p.blocks;
+  a.few_rows = p.few_rows;
+  auto use = [&](const Cut& c, float* part) {
+    a.splits = c.splits;
+    a.slice = c.slice;
+    a.part_o = part;
+    a.part_ml = part + c.parts(a.kv.hkv) * D;
+  };
+  float* const ws = a.part_o;
+  if (p.many.slots > 0) {
+    use(p.many, ws);
+    const int rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
+    if (rc != DAG_OK) return rc;
+  }
+  const size_t lds = (size_t)FEW_WAVES * p.few_rows * (D + 4) * sizeof(float);
+  if (lds > 65536 && hipFuncSetAttribute((const void*)k_q8_chunk_few<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return DAG_ERR_HIP;
+  use(p.few, ws + p.many.parts(a.kv.hkv) * (D + 2));
+  hipLaunchKernelGGL((k_q8_chunk_few<D>), dim3((unsigned)(p.few.slots * a.kv.hkv * p.few.splits)), dim3(64 * FEW_WAVES), lds, stream, a);
+  DAG_LAUNCH_CHECK();
+  if (p.few.splits > 1) {
+    hipLaunchKernelGGL((k_q8_chunk_merge<D, 32, true>), dim3((unsigned)(p.few.slots * a.kv.hkv * 8)), dim3(256), 0, stream, a);
     DAG_LAUNCH_CHECK();
   }
   return DAG_OK;
 }
 
-size_t part_count(const Plan& p, int hkv, int pairs) { return p.splits > 1 ? (size_t)p.slots * hkv * p.splits * pairs : 0; }
-
 }  // namespace
 
 extern "C" size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim) {
   Plan p;
-  if (!bounds_ok(d, n_rows, hq, hkv, head_dim) || d->page_size != PAGE || !plan(d, n_rows, hq, hkv, 32 * waves_of(head_dim), &p)) return 0;
-  return part_count(p, hkv, 32 * waves_of(head_dim)) * (head_dim + 2) * sizeof(float);
+  if (!bounds_ok(d, n_rows, hq, hkv, head_dim) || d->page_size != PAGE || !plan(d, n_rows, hq, hkv, head_dim, &p)) return 0;
+  return p.floats(hkv, head_dim) * sizeof(float);
 }
 
 extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
@@ -619,8 +897,8 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   if (!d || !kv) return DAG_ERR_NULL;
   if (d->n_nodes < 0 || d->max_new < 0 || d->max_ctx_pages < 0 || kv->n_pages < 0 || n_rows < 0) return DAG_ERR_BAD_LEN;
   Plan p;
-  if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, 32 * waves_of(kv->head_dim), &p)) return DAG_ERR_UNSUPPORTED;
-  if (p.slots == 0 || n_rows == 0) return DAG_OK;  // no new token anywhere
+  if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, kv->head_dim, &p)) return DAG_ERR_UNSUPPORTED;
+  if (p.few.slots == 0) return DAG_OK;  // no new token anywhere
   const bool pages = d->max_ctx_pages > 0;
   if (pages && kv->n_pages == 0) return DAG_ERR_BAD_LEN;
   if (!q || !out || !d->q_off || !d->ctx_page_off || !d->own_page || !d->own_len) return DAG_ERR_NULL;
@@ -628,9 +906,9 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   if (!dag_aligned16(q) || !dag_aligned16(out) || !dag_aligned16(kv->k_pool) || !dag_aligned16(kv->v_pool) || ((uintptr_t)kv->k_scale & 3) ||
       ((uintptr_t)kv->v_scale & 3) || ((uintptr_t)lse & 3))
     return DAG_ERR_ALIGN;
-  const size_t parts = part_count(p, kv->hkv, 32 * waves_of(kv->head_dim));
-  if (parts > 0 && (!ws || ws_bytes < parts * (kv->head_dim + 2) * sizeof(float))) return DAG_ERR_WORKSPACE;
-  if (parts > 0 && !dag_aligned16(ws)) return DAG_ERR_ALIGN;
+  const size_t need = p.floats(kv->hkv, kv->head_dim) * sizeof(float);
+  if (need > 0 && (!ws || ws_bytes < need)) return DAG_ERR_WORKSPACE;
+  if (need > 0 && !dag_aligned16(ws)) return DAG_ERR_ALIGN;
   ChunkArgs a = {};
   a.kv = Q8Cache{(const uint8_t*)kv->k_pool, (const uint8_t*)kv->v_pool, kv->k_scale, kv->v_scale, kv->n_pages, kv->hkv};
   a.q_off = d->q_off;
@@ -643,15 +921,12 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   a.out = (uint16_t*)out;
   a.lse = lse;
   a.part_o = (float*)ws;
-  a.part_ml = a.part_o + parts * kv->head_dim;
   a.n_nodes = d->n_nodes;
   a.n_rows = (int)n_rows;
   a.max_new = d->max_new;
   a.max_ctx_pages = d->max_ctx_pages;
   a.hq = hq;
   a.G = hq / kv->hkv;
-  a.splits = p.splits;
-  a.slice = p.slice;
   a.sc = std::isfinite(softmax_scale) ? softmax_scale * 1.4426950408889634f : NAN;
   return kv->head_dim == 128 ? launch<128>(a, p, (hipStream_t)stream_) : launch<64>(a, p, (hipStream_t)stream_);
 }
