@@ -573,8 +573,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
 
 // Few pairs: 32 of them to a workgroup, whose waves share a stretch of the pages, each a run of its own, straight from memory, and put their sums
 // together in LDS.  What bounds it is how the pages come: two blocks of two pages of a wave are on their way.
-constexpr int FEW_WAVES = 8;
-template <int D>
+template <int D, int FEW_WAVES>
 __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_o[];  // [wave][pair][D + 4], of as many pairs as a block may have
   __shared__ float2 s_ml[FEW_WAVES][32];
@@ -703,8 +702,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
     l += other_half(l);
   }
 
-  // The sums of all waves, added up in their order: 16 threads to a pair, eight (or four) dims each.
-  constexpr int LINE = D + 4, EACH = D / 16;
+  // The sums of all waves, added up in their order: 2 FEW_WAVES threads to a pair.
+  constexpr int LINE = D + 4, EACH = D / (2 * FEW_WAVES);
   if (H == 0) s_ml[w][L] = make_float2(m, l);
   if (L < a.few_rows && l != 0.f) {
 #pragma unroll
@@ -714,7 +713,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
         *(f32x4*)&s_o[(w * a.few_rows + L) * LINE + 32 * db + 8 * r + 4 * H] = f32x4{O[db][4 * r], O[db][4 * r + 1], O[db][4 * r + 2], O[db][4 * r + 3]};
   }
   __syncthreads();
-  const int mine = tid / 16, d0 = tid % 16 * EACH;
+  const int mine = tid / (2 * FEW_WAVES), d0 = tid % (2 * FEW_WAVES) * EACH;
   if (mine >= n_pairs) return;
   float top = -1e30f, total = 0.f, weight[FEW_WAVES], o[EACH] = {};
 #pragma unroll
@@ -746,8 +745,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
   uint32_t y[EACH / 2];
 #pragma unroll
   for (int e = 0; e < EACH / 2; ++e) y[e] = dag_pack_bf2(o[2 * e] * inv, o[2 * e + 1] * inv);
-  if constexpr (EACH == 8) *(u32x4*)(a.out + at * D + d0) = u32x4{y[0], y[1], y[EACH / 2 - 2], y[EACH / 2 - 1]};
-  else *(u32x2*)(a.out + at * D + d0) = u32x2{y[0], y[1]};
+#pragma unroll
+  for (int e = 0; e < EACH / 2; e += 2) *(u32x2*)(a.out + at * D + d0 + 2 * e) = u32x2{y[e], y[e + 1]};
   if (a.lse && d0 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
@@ -768,12 +767,24 @@ __global__ void __launch_bounds__(256) k_q8_chunk_merge(ChunkArgs a) {
   const float top = dag_wave_max(ml.y != 0.f ? ml.x : -1e30f), weight = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
   const float total = dag_wave_sum(ml.y * weight);
   float o[EACH] = {};
-  for (uint64_t rest = __builtin_amdgcn_ballot_w64(ml.y != 0.f); rest; rest &= rest - 1) {
-    const int s = __builtin_ctzll(rest);
-    const float f = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), s));
-    const float* const from = a.part_o + (at + (size_t)s * PAIRS) * D + EACH * lane;
+  const uint64_t there = __builtin_amdgcn_ballot_w64(ml.y != 0.f);  // (the others have not been written)
+  constexpr int AHEAD = 8;
+  for (int s0 = 0; s0 < a.splits; s0 += AHEAD) {
+    float x[AHEAD][EACH];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) o[e] = fmaf(from[e], f, o[e]);
+    for (int i = 0; i < AHEAD; ++i) {
+      const float* const from = a.part_o + (at + (size_t)min(s0 + i, a.splits - 1) * PAIRS) * D + EACH * lane;
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) x[i][e] = from[e];
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int s = s0 + i;
+      if (s >= a.splits || !(there >> s & 1)) continue;
+      const float f = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), s));
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) o[e] = fmaf(x[i][e], f, o[e]);
+    }
   }
   const int row = pair / a.G, head = hk * a.G + pair % a.G;
   const size_t to = (size_t)(pl.row0 + row) * a.hq + head;
@@ -791,7 +802,7 @@ struct Cut {
 };
 struct Plan {
   Cut few, many;  // slots 0: not launched
-  int blocks, few_rows, waves;
+  int blocks, few_rows, few_waves, waves;
   size_t floats(int hkv, int D) const { return (few.parts(hkv) + many.parts(hkv)) * (D + 2); }
 };
 // As many stretches as take the least time: rounds of the workgroups that the device holds at once, each as long as its steps through a stretch
@@ -800,7 +811,7 @@ struct Cost {
   double tile, each, merge;
   int at_once;
 };
-void cut(Cut* c, double items, int64_t tiles, int D, const Cost& cost) {
+double cut(Cut* c, double items, int64_t tiles, int D, const Cost& cost) {
   double best = 1e300;
   c->splits = 1;
   c->slice = (int)std::max<int64_t>(tiles, 1);
@@ -815,19 +826,28 @@ void cut(Cut* c, double items, int64_t tiles, int D, const Cost& cost) {
       c->slice = (int)slice;
     }
   }
+  return best;
 }
 // By the host's bounds.  The device has 256 compute units.
 bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, int D, Plan* p) {
   const int64_t G = hq / hkv, tiles = dag_ceil_div(d->max_ctx_pages, TILE), most = d->max_new * G;
   const bool none = d->max_new == 0 || d->n_nodes == 0 || n_rows == 0;
   p->few = p->many = Cut{0, 1, 1, 32};
+  p->few_waves = 4;
   p->blocks = (int)std::max<int64_t>(1, dag_ceil_div(std::min<int64_t>(most, FEW_PAIRS), 32));
   p->few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, 32));
   // (few new tokens in all: a node with more is a tile kernel's, which has a slot for it wherever there is one)
   if (!none) {
     p->few.slots = (int64_t)d->n_nodes * p->blocks;
-    // (a tile is a quarter of a step of the eight waves)
-    cut(&p->few, (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv, tiles, D, Cost{0.25, 5., 4., 256});
+    // four waves to a workgroup, or eight where that leaves compute units free
+    const double items = (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv;
+    Cut wide = p->few;
+    const double time = cut(&p->few, items, tiles, D, Cost{0.4, 5., 4., 512});
+    p->few_waves = 4;
+    if (cut(&wide, items, tiles, D, Cost{0.28, 5., 4., 256}) < time) {
+      p->few = wide;
+      p->few_waves = 8;
+    }
   }
   p->waves = most <= 128 ? 4 : 8;
   if (!none && most > FEW_PAIRS) {
@@ -856,6 +876,15 @@ int launch_many(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
   }
   return DAG_OK;
 }
+template <int D, int FEW_WAVES>
+int launch_few(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
+  const size_t lds = (size_t)FEW_WAVES * a.few_rows * (D + 4) * sizeof(float);
+  auto* const kernel = k_q8_chunk_few<D, FEW_WAVES>;
+  if (lds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return DAG_ERR_HIP;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(c.slots * a.kv.hkv * c.splits)), dim3(64 * FEW_WAVES), lds, stream, a);
+  DAG_LAUNCH_CHECK();
+  return DAG_OK;
+}
 template <int D>
 int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   a.blocks = p.blocks;
@@ -872,11 +901,9 @@ int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
     const int rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
     if (rc != DAG_OK) return rc;
   }
-  const size_t lds = (size_t)FEW_WAVES * p.few_rows * (D + 4) * sizeof(float);
-  if (lds > 65536 && hipFuncSetAttribute((const void*)k_q8_chunk_few<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return DAG_ERR_HIP;
   use(p.few, ws + p.many.parts(a.kv.hkv) * (D + 2));
-  hipLaunchKernelGGL((k_q8_chunk_few<D>), dim3((unsigned)(p.few.slots * a.kv.hkv * p.few.splits)), dim3(64 * FEW_WAVES), lds, stream, a);
-  DAG_LAUNCH_CHECK();
+  const int rc = p.few_waves == 4 ? launch_few<D, 4>(a, p.few, stream) : launch_few<D, 8>(a, p.few, stream);
+  if (rc != DAG_OK) return rc;
   if (p.few.splits > 1) {
     hipLaunchKernelGGL((k_q8_chunk_merge<D, 32, true>), dim3((unsigned)(p.few.slots * a.kv.hkv * 8)), dim3(256), 0, stream, a);
     DAG_LAUNCH_CHECK();
