@@ -38,6 +38,7 @@ struct ChunkArgs {
   int splits, slice;  // stretches of a context, tiles in each
   int blocks;         // of 32 pairs to a node (nodes with few pairs)
   int few_rows;       // pairs that a block of them may have
+  int few_most;       // pairs of a node up to which they are
   float sc;           // softmax_scale * log2(e)
 };
 
@@ -74,7 +75,7 @@ __device__ __forceinline__ bool find_place(const ChunkArgs& a, int64_t slot, int
   }
   node_place(a, lo, p);
   const int64_t pair0 = (slot - ((int64_t)p->row0 * a.G / PAIRS + lo)) * PAIRS;
-  if (pair0 >= (int64_t)p->n * a.G || p->n * a.G <= FEW_PAIRS) return false;
+  if (pair0 >= (int64_t)p->n * a.G || p->n * a.G <= a.few_most) return false;
   p->pair0 = (int)pair0;
   return true;
 }
@@ -82,7 +83,7 @@ __device__ __forceinline__ bool find_place(const ChunkArgs& a, int64_t slot, int
 __device__ __forceinline__ bool few_place(const ChunkArgs& a, int64_t slot, Place* p) {
   node_place(a, (int)(slot / a.blocks), p);
   p->pair0 = (int)(slot % a.blocks) * 32;
-  return p->n * a.G <= FEW_PAIRS && p->pair0 < p->n * a.G;
+  return p->n * a.G <= a.few_most && p->pair0 < p->n * a.G;
 }
 
 __device__ __forceinline__ void lds_barrier() {  // (loads from memory stay on their way)
@@ -837,7 +838,8 @@ bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, in
   p->blocks = (int)std::max<int64_t>(1, dag_ceil_div(std::min<int64_t>(most, FEW_PAIRS), 32));
   p->few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, 32));
   // (few new tokens in all: a node with more is a tile kernel's, which has a slot for it wherever there is one)
-  if (!none) {
+  // (a single node whose bound is past them is one of many pairs, whatever it has: a launch less)
+  if (!none && (most <= FEW_PAIRS || d->n_nodes > 1)) {
     p->few.slots = (int64_t)d->n_nodes * p->blocks;
     // four waves to a workgroup, or eight where that leaves compute units free
     const double items = (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv;
@@ -889,6 +891,7 @@ template <int D>
 int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   a.blocks = p.blocks;
   a.few_rows = p.few_rows;
+  a.few_most = p.few.slots > 0 ? FEW_PAIRS : 0;
   auto use = [&](const Cut& c, float* part) {
     a.splits = c.splits;
     a.slice = c.slice;
@@ -901,6 +904,7 @@ int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
     const int rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
     if (rc != DAG_OK) return rc;
   }
+  if (p.few.slots == 0) return DAG_OK;
   use(p.few, ws + p.many.parts(a.kv.hkv) * (D + 2));
   const int rc = p.few_waves == 4 ? launch_few<D, 4>(a, p.few, stream) : launch_few<D, 8>(a, p.few, stream);
   if (rc != DAG_OK) return rc;
@@ -925,7 +929,7 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   if (d->n_nodes < 0 || d->max_new < 0 || d->max_ctx_pages < 0 || kv->n_pages < 0 || n_rows < 0) return DAG_ERR_BAD_LEN;
   Plan p;
   if (d->page_size != PAGE || !bounds_ok(d, n_rows, hq, kv->hkv, kv->head_dim) || !plan(d, n_rows, hq, kv->hkv, kv->head_dim, &p)) return DAG_ERR_UNSUPPORTED;
-  if (p.few.slots == 0) return DAG_OK;  // no new token anywhere
+  if (p.few.slots == 0 && p.many.slots == 0) return DAG_OK;  // no new token anywhere
   const bool pages = d->max_ctx_pages > 0;
   if (pages && kv->n_pages == 0) return DAG_ERR_BAD_LEN;
   if (!q || !out || !d->q_off || !d->ctx_page_off || !d->own_page || !d->own_len) return DAG_ERR_NULL;
