@@ -130,7 +130,7 @@ __device__ __forceinline__ void split_q(QueryCodes<D>& y, const bf16x8 (&q)[D / 
     }
   }
   most = fmaxf(most, other_half(most));
-  const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 7, -100);  // largest element in [128, 256)
+  const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 7, -121);  // largest element in [128, 256) (2^-114 and more)
   const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
