@@ -53,13 +53,9 @@ __device__ __forceinline__ void settle() {
   __syncthreads();
 }
 
-// Workgroup 0: which forks there are, their tokens and pages; the others take the holders over.
-__global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_rows(PagesArgs a) {
+// Which forks there are, their tokens and pages; by one workgroup.
+__device__ __forceinline__ void fork_rows(const PagesArgs& a) {
   const int me = threadIdx.x, n_rows = a.rows.n_rows;
-  if (blockIdx.x > 0) {
-    for (int64_t p = (int64_t)(blockIdx.x - 1) * ROW_THREADS + me; p < a.rows.n_pages; p += (int64_t)(gridDim.x - 1) * ROW_THREADS) a.extra_out[p] = a.extra[p];
-    return;
-  }
   for (int r = me; r < n_rows; r += ROW_THREADS) {
     a.claim[r] = INT32_MAX;
     if (a.row_len_out != a.row_len) a.row_len_out[r] = max(a.row_len[r], 0);
@@ -108,17 +104,35 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_rows(PagesArgs a) {
   }
 }
 
-__global__ void __launch_bounds__(LIST_THREADS) k_kv_fork_lines(PagesArgs a) {
-  const int f = blockIdx.x, n = a.tokens[f];
+__device__ __forceinline__ void fork_extra(const PagesArgs& a, int64_t at, int64_t step) {
+  if (a.extra_out == a.extra) return;
+  for (int64_t p = at; p < a.rows.n_pages; p += step) a.extra_out[p] = a.extra[p];
+}
+// The child's line of fork f, by `step` threads.
+__device__ __forceinline__ void fork_line(const PagesArgs& a, int f, int at, int step) {
+  const int n = a.tokens[f];
   if (n <= 0) return;
   const int32_t* const from = a.rows.table + (size_t)a.parent[f] * a.rows.max_row_pages;
   int32_t* const to = a.rows.table + (size_t)a.child[f] * a.rows.max_row_pages;
-  for (int i = threadIdx.x; i < n / PAGE; i += LIST_THREADS) {
+  for (int i = at; i < n / PAGE; i += step) {
     const int p = from[i];
     to[i] = p;
     if (in_pool(a, p)) atomicAdd(a.extra_out + p, 1);
   }
-  if (threadIdx.x == 0 && n % PAGE != 0) to[n / PAGE] = a.copy_dst[f];
+  if (at == 0 && n % PAGE != 0) to[n / PAGE] = a.copy_dst[f];
+}
+
+// In two launches (workgroup 0: the forks; the others take the holders over), or small tables in one, by one workgroup.
+__global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_rows(PagesArgs a) {
+  if (blockIdx.x == 0) fork_rows(a);
+  else fork_extra(a, (int64_t)(blockIdx.x - 1) * ROW_THREADS + threadIdx.x, (int64_t)(gridDim.x - 1) * ROW_THREADS);
+}
+__global__ void __launch_bounds__(LIST_THREADS) k_kv_fork_lines(PagesArgs a) { fork_line(a, blockIdx.x, threadIdx.x, LIST_THREADS); }
+__global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_whole(PagesArgs a) {
+  fork_extra(a, threadIdx.x, ROW_THREADS);
+  fork_rows(a);
+  settle();
+  for (int f = threadIdx.x / 64; f < a.n_forks; f += ROW_THREADS / 64) fork_line(a, f, threadIdx.x & 63, 64);
 }
 
 // Release, in phases that each need the one in front whole: by one workgroup (WHOLE) with barriers between them, or a launch each.
@@ -215,7 +229,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_release_phase(PagesArgs a) {
 }
 
 // Compaction: which pages are free, how many used ones move, from where to where.  One workgroup; a thread has a run of words of 32 pages.
-__global__ void __launch_bounds__(ROW_THREADS) k_kv_compact_pages(PagesArgs a) {
+__device__ __forceinline__ void compact_pages(const PagesArgs& a) {
   const int me = threadIdx.x, n_pages = a.rows.n_pages, words = (n_pages + 31) / 32;
   for (int i = me; i < words; i += ROW_THREADS) a.bits[i] = 0;
   settle();
@@ -253,41 +267,62 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_compact_pages(PagesArgs a) {
   }
 }
 
-// Then the first workgroups write the lists of the pages, the others the lines of the rows, a wave to a row.
-__global__ void __launch_bounds__(PAGE_THREADS) k_kv_compact_lists(PagesArgs a, int page_blocks) {
-  const int n_pages = a.rows.n_pages, used = a.rank[0], count = n_pages - used;
-  auto is_free = [&](int p) { return a.bits[p / 32] >> p % 32 & 1; };
-  auto place = [&](int p) {  // of a used page
+// Then the lists of the pages and the lines of the rows (a wave to a row).  WHOLE: in the workgroup that has worked the places out.
+template <bool WHOLE>
+struct Places {
+  const PagesArgs& a;
+  int used, n_pages;
+  __device__ __forceinline__ uint32_t bits(int w) const { return WHOLE ? fresh(a.bits + w) : a.bits[w]; }
+  __device__ __forceinline__ bool is_free(int p) const { return bits(p / 32) >> p % 32 & 1; }
+  __device__ __forceinline__ int operator()(int p) const {  // of a used page
     if (p < used) return p;
-    const uint32_t b = ~a.bits[p / 32] & (0xffffffffu << max(used - (p & ~31), 0)) & ((1u << p % 32) - 1u);
+    const uint32_t b = ~bits(p / 32) & (0xffffffffu << max(used - (p & ~31), 0)) & ((1u << p % 32) - 1u);
     return a.copy_dst[a.rank[p / 32 + 1] + __builtin_popcount(b)];
-  };
-  if ((int)blockIdx.x < page_blocks) {
-    for (int64_t i = (int64_t)blockIdx.x * PAGE_THREADS + threadIdx.x; i < n_pages; i += (int64_t)page_blocks * PAGE_THREADS) {
-      const int p = (int)i;
-      const bool none = is_free(p);
-      const int to = none ? -1 : place(p);
-      a.page_map[p] = to;
-      if (p < count) a.to.free_pages[p] = n_pages - 1 - p;
-      // (a free page in front of `used` is written by the page that moves there)
-      if (!none) {
-        const int n = a.extra[p];
-        if (to != p) a.extra_out[p] = 0;
-        a.extra_out[to] = n;
-      } else if (p >= used) {
-        a.extra_out[p] = 0;
-      }
+  }
+};
+template <bool WHOLE>
+__device__ __forceinline__ void compact_lists(const PagesArgs& a, int64_t at, int64_t step) {
+  const int n_pages = a.rows.n_pages, used = a.rank[0], count = n_pages - used;
+  const Places<WHOLE> place{a, used, n_pages};
+  for (int64_t i = at; i < n_pages; i += step) {
+    const int p = (int)i;
+    const bool none = place.is_free(p);
+    const int to = none ? -1 : place(p);
+    a.page_map[p] = to;
+    if (p < count) a.to.free_pages[p] = n_pages - 1 - p;
+    // (a free page in front of `used` is written by the page that moves there)
+    if (!none) {
+      const int n = a.extra[p];
+      if (to != p) a.extra_out[p] = 0;
+      a.extra_out[to] = n;
+    } else if (p >= used) {
+      a.extra_out[p] = 0;
     }
-    return;
   }
-  const int64_t r = (int64_t)(blockIdx.x - page_blocks) * (PAGE_THREADS / 64) + (threadIdx.x >> 6);
-  if (r >= a.rows.n_rows) return;
-  const int n = pages_held(a, (int)r);
-  for (int i = threadIdx.x & 63; i < n; i += 64) {
-    const size_t at = (size_t)r * a.rows.max_row_pages + i;
-    const int p = a.rows.table[at];
-    a.to.table[at] = in_pool(a, p) && !is_free(p) ? place(p) : p;
+}
+template <bool WHOLE>
+__device__ __forceinline__ void compact_lines(const PagesArgs& a, int64_t at, int64_t step, int lane) {
+  const Places<WHOLE> place{a, a.rank[0], a.rows.n_pages};
+  for (int64_t r = at; r < a.rows.n_rows; r += step) {
+    const int n = pages_held(a, (int)r);
+    for (int i = lane; i < n; i += 64) {
+      const size_t e = (size_t)r * a.rows.max_row_pages + i;
+      const int p = a.rows.table[e];
+      a.to.table[e] = in_pool(a, p) && !place.is_free(p) ? place(p) : p;
+    }
   }
+}
+__global__ void __launch_bounds__(ROW_THREADS) k_kv_compact_pages(PagesArgs a) { compact_pages(a); }
+__global__ void __launch_bounds__(PAGE_THREADS) k_kv_compact_lists(PagesArgs a, int page_blocks) {  // the first workgroups: pages, the others: rows
+  constexpr int WAVES = PAGE_THREADS / 64;
+  if ((int)blockIdx.x < page_blocks) compact_lists<false>(a, (int64_t)blockIdx.x * PAGE_THREADS + threadIdx.x, (int64_t)page_blocks * PAGE_THREADS);
+  else compact_lines<false>(a, (int64_t)(blockIdx.x - page_blocks) * WAVES + threadIdx.x / 64, (int64_t)(gridDim.x - page_blocks) * WAVES, threadIdx.x & 63);
+}
+__global__ void __launch_bounds__(ROW_THREADS) k_kv_compact_whole(PagesArgs a) {
+  compact_pages(a);
+  settle();
+  compact_lists<true>(a, threadIdx.x, ROW_THREADS);
+  compact_lines<true>(a, threadIdx.x / 64, ROW_THREADS / 64, threadIdx.x & 63);
 }
 
 struct CopyArgs {
@@ -334,6 +369,9 @@ int copy_pages(const CopyArgs& a, hipStream_t stream) {
   DAG_LAUNCH_CHECK();
   return DAG_OK;
 }
+
+// Entries of the table, and pages, up to which one workgroup does a call as a whole: as long as its turns take no longer than the launches do.
+constexpr int64_t WHOLE_ENTRIES = 8192;
 
 size_t words_of(int32_t n_pages) { return ((size_t)n_pages + 31) / 32; }
 
@@ -391,6 +429,11 @@ extern "C" int dag_kv_fork(const dag_kv_rows_t* rows, int32_t n_forks, const int
   a.refused = refused;
   a.n_forks = n_forks;
   hipStream_t stream = (hipStream_t)stream_;
+  if ((int64_t)n_forks * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
+    hipLaunchKernelGGL(k_kv_fork_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+    return DAG_OK;
+  }
   const int64_t copies = extra == extra_out ? 0 : std::min<int64_t>(dag_ceil_div(rows->n_pages, ROW_THREADS), 256);
   hipLaunchKernelGGL(k_kv_fork_rows, dim3((unsigned)(1 + copies)), dim3(ROW_THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
@@ -416,7 +459,7 @@ extern "C" int dag_kv_release_shared(const dag_kv_rows_t* rows, const int32_t* e
   a.free_count = free_count;
   a.free_count_out = free_count_out;
   hipStream_t stream = (hipStream_t)stream_;
-  if ((int64_t)rows->n_rows * rows->max_row_pages <= 16384 && rows->n_pages <= 16384) {
+  if ((int64_t)rows->n_rows * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
     hipLaunchKernelGGL(k_kv_release_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
     DAG_LAUNCH_CHECK();
     return DAG_OK;
@@ -463,6 +506,11 @@ extern "C" int dag_kv_compact(const dag_kv_rows_t* rows, const dag_kv_rows_t* ro
   a.copy_dst = copy_dst;
   a.n_copies = n_copies;
   hipStream_t stream = (hipStream_t)stream_;
+  if ((int64_t)rows->n_rows * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
+    hipLaunchKernelGGL(k_kv_compact_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+    return DAG_OK;
+  }
   hipLaunchKernelGGL(k_kv_compact_pages, dim3(1), dim3(ROW_THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
   const int page_blocks = (int)std::min<int64_t>(dag_ceil_div(rows->n_pages, PAGE_THREADS), 1024);
