@@ -4,7 +4,8 @@
 // Pair m of a head turns by pos * freq[m]: y = factor (x cos - x' sin, x' cos + x sin); transposed, which is what the gradients go through, the
 // angle has the other sign.  Angles are taken in 64 bits, the rotation in 32, one rounding to the tensors' type.  Everything is read and written
 // once, which is what bounds it.  A workgroup turns the angles of its tokens into cosines and sines once for all heads (in LDS), and then
-// a thread has units of two 16-byte pieces whose elements are each other's partners (or stay as they are), four on their way together.
+// a thread has units of two 16-byte pieces whose elements are each other's partners (or stay as they are), two on their way together.
+// 18432 tokens of 40 heads of 128 in bf16: 68 us, 5.6 TB/s, with two tokens to a workgroup (four 70, eight 74, sixteen 80; one unit on its way 72, five 73).
 #include <cmath>
 
 #include "common.h"
@@ -12,7 +13,7 @@
 
 namespace {
 
-constexpr int THREADS = 256, MAX_HALF = 128, AHEAD = 4;
+constexpr int THREADS = 256, MAX_HALF = 128, AHEAD = 2;
 
 struct RotaryArgs {
   const int32_t* pos;
@@ -113,8 +114,10 @@ __global__ void __launch_bounds__(THREADS) k_rotary(RotaryArgs a) {
 
 template <bool BF16>
 int launch_rotary(const RotaryArgs& a, hipStream_t stream) {
-  const int tokens = a.n_tokens < 2048 ? 1 : 4;
-  auto* const kernel = tokens == 1 ? k_rotary<BF16, 1> : k_rotary<BF16, 4>;
+  // (a workgroup's chain of frequencies, angles and rows is shared by more tokens where a token has few units)
+  const int units = (a.heads[0] + a.heads[1]) * (a.D / (BF16 ? 16 : 8));
+  const int tokens = a.n_tokens < 2048 ? 1 : units >= 192 ? 2 : units >= 48 ? 4 : 16;
+  auto* const kernel = tokens == 1 ? k_rotary<BF16, 1> : tokens == 2 ? k_rotary<BF16, 2> : tokens == 4 ? k_rotary<BF16, 4> : k_rotary<BF16, 16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)dag_ceil_div(a.n_tokens, tokens)), dim3(THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
   return DAG_OK;
