@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_whole(PagesArgs a) {
   for (int f = threadIdx.x / 64; f < a.n_forks; f += ROW_THREADS / 64) fork_line(a, f, threadIdx.x & 63, 64);
 }
 
-// Release, in phases that each need the one in front whole: by one workgroup (WHOLE) with barriers between them, or a launch each.
+// Release, in phases that each need the one in front whole: by one workgroup with barriers between them, or a launch each.
 // What one thread of `step` does, from `at` on.
 __device__ __forceinline__ void release_clear(const PagesArgs& a, int64_t at, int64_t step) {
   for (int64_t p = at; p < a.rows.n_pages; p += step) {
@@ -157,106 +157,146 @@ __device__ __forceinline__ void release_count(const PagesArgs& a, int64_t at, in
     }
   }
 }
-__device__ __forceinline__ void release_pages(const PagesArgs& a, int64_t at, int64_t step) {
-  for (int64_t p = at; p < a.rows.n_pages; p += step) {
-    const int times = fresh(a.times + p), extra = max(a.extra[p], 0);
-    if (times <= extra) a.last[p] = 0;  // somebody holds it still
-    a.extra_out[p] = max(extra - times, 0);
-  }
-}
+// Pages that row r frees, the entries that give a page back last and leave it without a holder: how many, or (WRITE) into the free list from `to` on.
 template <bool WRITE>
+__device__ __forceinline__ int release_row(const PagesArgs& a, int64_t r, int to, int lane) {
+  const int n = a.ended[r] == 0 ? 0 : pages_held(a, (int)r);
+  for (int base = 0; base < n; base += 64) {
+    const int i = base + lane;
+    const int64_t place = r * a.rows.max_row_pages + i;
+    const int p = i < n ? a.rows.table[place] : -1;
+    const bool mine = in_pool(a, p) && fresh(a.last + p) == (uint64_t)place + 1 && fresh(a.times + p) > max(a.extra[p], 0);
+    const uint64_t all = __builtin_amdgcn_ballot_w64(mine);
+    const int at = to + __builtin_popcountll(all & ((1ull << lane) - 1));
+    if (WRITE && mine && at < a.rows.n_pages) a.rows.free_pages[at] = p;
+    to += __builtin_popcountll(all);
+  }
+  return to;
+}
 __device__ __forceinline__ void release_rows(const PagesArgs& a, int64_t at, int64_t step, int lane) {
   for (int64_t r = at; r < a.rows.n_rows; r += step) {
-    const int n = a.ended[r] == 0 ? 0 : pages_held(a, (int)r);
-    int freed = WRITE ? fresh(a.claim + r) : 0;
-    for (int base = 0; base < n; base += 64) {
-      const int i = base + lane;
-      const int64_t place = r * a.rows.max_row_pages + i;
-      const int p = i < n ? a.rows.table[place] : -1;
-      const bool mine = in_pool(a, p) && fresh(a.last + p) == (uint64_t)place + 1;
-      const uint64_t all = __builtin_amdgcn_ballot_w64(mine);
-      const int to = freed + __builtin_popcountll(all & ((1ull << lane) - 1));
-      if (WRITE && mine && to < a.rows.n_pages) a.rows.free_pages[to] = p;
-      freed += __builtin_popcountll(all);
-    }
-    if (!WRITE && lane == 0) a.claim[r] = freed;
+    const int n = release_row<false>(a, r, 0, lane);
+    if (lane == 0) a.claim[r] = n;
   }
 }
-__device__ __forceinline__ void release_scan(const PagesArgs& a) {  // by one workgroup
+// The free list of the rows [r0, r0 + ROW_WAVES), a wave each, behind the sums of all rows in front.
+constexpr int ROW_WAVES = ROW_THREADS / 64;
+__device__ __forceinline__ void release_write(const PagesArgs& a, int64_t r0) {
+  __shared__ int s_to[ROW_WAVES];
+  int64_t front = free_pages(a);
+  for (int64_t base = 0; base < r0 + ROW_WAVES; base += ROW_THREADS) {
+    const int64_t r = base + threadIdx.x;
+    int64_t x[1] = {r < a.rows.n_rows ? fresh(a.claim + r) : 0}, all[1];
+    block_scan(x, all);
+    if (r >= r0 && r < r0 + ROW_WAVES) s_to[r - r0] = (int)(front + x[0]);
+    front += all[0];
+  }
+  __syncthreads();
+  const int64_t r = r0 + threadIdx.x / 64;
+  if (r < a.rows.n_rows) release_row<true>(a, r, s_to[threadIdx.x / 64], threadIdx.x & 63);
+  __syncthreads();
+}
+// When nobody reads them any more: holders, lengths and the number of free pages.
+__device__ __forceinline__ void release_end(const PagesArgs& a, int64_t at, int64_t step) {
+  for (int64_t p = at; p < a.rows.n_pages; p += step) a.extra_out[p] = max(max(a.extra[p], 0) - fresh(a.times + p), 0);
+  for (int64_t r = at; r < a.rows.n_rows; r += step) a.row_len_out[r] = a.ended[r] != 0 ? 0 : max(a.row_len[r], 0);
+}
+// By one workgroup: the sums of the pages that rows free, the number of free pages.  PLACES: the sums in front of every row in its place.
+template <bool PLACES>
+__device__ __forceinline__ void release_scan(const PagesArgs& a) {
   int64_t front = free_pages(a);
   for (int64_t base = 0; base < a.rows.n_rows; base += ROW_THREADS) {
     const int64_t r = base + threadIdx.x;
     int64_t x[1] = {r < a.rows.n_rows ? fresh(a.claim + r) : 0}, all[1];
     block_scan(x, all);
-    if (r < a.rows.n_rows) a.claim[r] = (int32_t)(front + x[0]);
+    if (PLACES && r < a.rows.n_rows) a.claim[r] = (int32_t)(front + x[0]);
     front += all[0];
   }
   if (threadIdx.x == 0) a.free_count_out[0] = (int32_t)min(front, (int64_t)a.rows.n_pages);
 }
-__device__ __forceinline__ void release_lengths(const PagesArgs& a, int64_t at, int64_t step) {  // when nobody reads them any more
-  for (int64_t r = at; r < a.rows.n_rows; r += step) a.row_len_out[r] = a.ended[r] != 0 ? 0 : max(a.row_len[r], 0);
+__device__ __forceinline__ void release_lists(const PagesArgs& a, int64_t at, int64_t step, int lane) {
+  for (int64_t r = at; r < a.rows.n_rows; r += step) release_row<true>(a, r, fresh(a.claim + r), lane);
 }
 
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_release_whole(PagesArgs a) {
-  const int me = threadIdx.x, lane = me & 63, w = me >> 6, waves = ROW_THREADS / 64;
+  const int me = threadIdx.x, lane = me & 63, w = me >> 6;
   release_clear(a, me, ROW_THREADS);
   settle();
-  release_count(a, w, waves, lane);
+  release_count(a, w, ROW_WAVES, lane);
   settle();
-  release_pages(a, me, ROW_THREADS);
+  release_rows(a, w, ROW_WAVES, lane);
   settle();
-  release_rows<false>(a, w, waves, lane);
+  release_scan<true>(a);
   settle();
-  release_scan(a);
+  release_lists(a, w, ROW_WAVES, lane);
   settle();
-  release_rows<true>(a, w, waves, lane);
-  settle();
-  release_lengths(a, me, ROW_THREADS);
+  release_end(a, me, ROW_THREADS);
 }
 
-enum { CLEAR, COUNT, PAGES, ROWS, SCAN, WRITE, LENGTHS };
+enum { CLEAR, COUNT, ROWS, WRITE, END, SCAN, LISTS, LAST };
 template <int PHASE>
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_release_phase(PagesArgs a) {
   const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
   const int lane = threadIdx.x & 63;
   if constexpr (PHASE == CLEAR) release_clear(a, at, step);
   if constexpr (PHASE == COUNT) release_count(a, at / 64, step / 64, lane);
-  if constexpr (PHASE == PAGES) release_pages(a, at, step);
-  if constexpr (PHASE == ROWS) release_rows<false>(a, at / 64, step / 64, lane);
-  if constexpr (PHASE == SCAN) release_scan(a);
-  if constexpr (PHASE == WRITE) release_rows<true>(a, at / 64, step / 64, lane);
-  if constexpr (PHASE == LENGTHS) release_lengths(a, at, step);
+  if constexpr (PHASE == ROWS) release_rows(a, at / 64, step / 64, lane);
+  if constexpr (PHASE == WRITE) release_write(a, (int64_t)blockIdx.x * ROW_WAVES);
+  if constexpr (PHASE == END) {  // (workgroup 0 adds the pages up; their number may be written where it was read, so not before)
+    if (blockIdx.x == 0) release_scan<false>(a);
+    else release_end(a, at - blockDim.x, step - blockDim.x);
+  }
+  // (many rows: every workgroup of WRITE would go through all of them)
+  if constexpr (PHASE == SCAN) release_scan<true>(a);
+  if constexpr (PHASE == LISTS) release_lists(a, at / 64, step / 64, lane);
+  if constexpr (PHASE == LAST) release_end(a, at, step);
 }
 
 // Compaction: which pages are free, how many used ones move, from where to where.  One workgroup; a thread has a run of words of 32 pages.
+constexpr int LDS_WORDS = 8192;  // 262144 pages
 __device__ __forceinline__ void compact_pages(const PagesArgs& a) {
+  __shared__ uint32_t s_bits[LDS_WORDS];
   const int me = threadIdx.x, n_pages = a.rows.n_pages, words = (n_pages + 31) / 32;
-  for (int i = me; i < words; i += ROW_THREADS) a.bits[i] = 0;
-  settle();
-  const int count = free_pages(a);
-  for (int i = me; i < count; i += ROW_THREADS) {
-    const int p = a.rows.free_pages[i];
-    if (in_pool(a, p)) atomicOr(a.bits + p / 32, 1u << p % 32);
+  const bool lds = words <= LDS_WORDS;
+  for (int i = me; i < words; i += ROW_THREADS) {
+    if (lds) s_bits[i] = 0;
+    else a.bits[i] = 0;
   }
   settle();
+  const int count = free_pages(a);
+  constexpr int AHEAD = 4;
+  for (int base = me; base < count; base += AHEAD * ROW_THREADS) {
+    int p[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) p[i] = a.rows.free_pages[min(base + i * ROW_THREADS, count - 1)];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (!in_pool(a, p[i])) continue;
+      if (lds) atomicOr(s_bits + p[i] / 32, 1u << p[i] % 32);
+      else atomicOr(a.bits + p[i] / 32, 1u << p[i] % 32);
+    }
+  }
+  settle();
+  auto bits = [&](int i) { return lds ? s_bits[i] : fresh(a.bits + i); };
   const int each = (words + ROW_THREADS - 1) / ROW_THREADS, w0 = min(me * each, words), w1 = min(w0 + each, words);
   int64_t f[1] = {0}, n_free[1];
-  for (int i = w0; i < w1; ++i) f[0] += __builtin_popcount(fresh(a.bits + i));
+  for (int i = w0; i < w1; ++i) f[0] += __builtin_popcount(bits(i));
   block_scan(f, n_free);
   const int used = n_pages - (int)n_free[0];
-  // pages of word i in front of `used`, and those of the pool from it on
+  // pages of word i in front of `used`, and those of the pool
   auto front = [=](int i) { return i * 32 >= used ? 0u : i * 32 + 32 <= used ? 0xffffffffu : (1u << (used - i * 32)) - 1u; };
   auto there = [=](int i) { return i * 32 + 32 <= n_pages ? 0xffffffffu : (1u << (n_pages - i * 32)) - 1u; };
   int64_t x[2] = {0, 0}, all[2];
   for (int i = w0; i < w1; ++i) {
-    const uint32_t b = fresh(a.bits + i);
+    const uint32_t b = bits(i);
     x[0] += __builtin_popcount(b & front(i));
     x[1] += __builtin_popcount(~b & there(i) & ~front(i));
   }
   block_scan(x, all);
   int to = (int)x[0], from = (int)x[1];
   for (int i = w0; i < w1; ++i) {
-    const uint32_t b = fresh(a.bits + i);
+    const uint32_t b = bits(i);
+    if (lds) a.bits[i] = b;
     a.rank[i + 1] = from;
     for (uint32_t m = b & front(i); m; m &= m - 1) a.copy_dst[to++] = 32 * i + __builtin_ctz(m);
     for (uint32_t m = ~b & there(i) & ~front(i); m; m &= m - 1) a.copy_src[from++] = 32 * i + __builtin_ctz(m);
@@ -470,16 +510,23 @@ extern "C" int dag_kv_release_shared(const dag_kv_rows_t* rows, const int32_t* e
   DAG_LAUNCH_CHECK();
   hipLaunchKernelGGL(k_kv_release_phase<COUNT>, dim3(by_row), dim3(256), 0, stream, a);
   DAG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(k_kv_release_phase<PAGES>, dim3(by_page), dim3(256), 0, stream, a);
-  DAG_LAUNCH_CHECK();
   hipLaunchKernelGGL(k_kv_release_phase<ROWS>, dim3(by_row), dim3(256), 0, stream, a);
   DAG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(k_kv_release_phase<SCAN>, dim3(1), dim3(ROW_THREADS), 0, stream, a);
-  DAG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(k_kv_release_phase<WRITE>, dim3(by_row), dim3(256), 0, stream, a);
-  DAG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(k_kv_release_phase<LENGTHS>, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(dag_ceil_div(rows->n_rows, 256), 256))), dim3(256), 0,
-                     stream, a);
+  if (rows->n_rows > 4 * ROW_THREADS) {
+    hipLaunchKernelGGL(k_kv_release_phase<SCAN>, dim3(1), dim3(ROW_THREADS), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+    hipLaunchKernelGGL(k_kv_release_phase<LISTS>, dim3(by_row), dim3(256), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+    hipLaunchKernelGGL(k_kv_release_phase<LAST>, dim3(by_page), dim3(256), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+    return DAG_OK;
+  }
+  if (rows->n_rows > 0) {
+    hipLaunchKernelGGL(k_kv_release_phase<WRITE>, dim3((unsigned)dag_ceil_div(rows->n_rows, ROW_WAVES)), dim3(ROW_THREADS), 0, stream, a);
+    DAG_LAUNCH_CHECK();
+  }
+  hipLaunchKernelGGL(k_kv_release_phase<END>, dim3((unsigned)std::min<int64_t>(1 + dag_ceil_div(std::max(rows->n_pages, rows->n_rows), ROW_THREADS), 1025)),
+                     dim3(ROW_THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
   return DAG_OK;
 }

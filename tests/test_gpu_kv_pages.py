@@ -106,7 +106,7 @@ def test_no_forks_and_no_rows():
     empty.compact()
 
 
-@pytest.mark.parametrize("rows,width,in_place", [(40, 9, True), (40, 9, False), (1500, 13, True), (3000, 40, False), (2, 300, True)])
+@pytest.mark.parametrize("rows,width,in_place", [(40, 9, True), (40, 9, False), (1500, 13, True), (3000, 40, False), (2, 300, True), (5000, 3, True), (4500, 2, False), (600, 5, True)])
 def test_families(rows, width, in_place):
     """Forks of forks, releases and compactions behind one another, small tables (one workgroup) and large ones."""
     rng = np.random.default_rng(rows)
