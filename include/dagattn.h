@@ -149,7 +149,7 @@ int dag_rope_qk(const int32_t* pos_ids, int64_t n_tokens, void* q, void* k, int3
 typedef enum { DAG_ROPE_HALVES = 0, DAG_ROPE_PAIRS = 1 } dag_rope_layout_t;
 typedef struct {
   const double* freq; /* DEVICE [rotary_dim / 2]                                                 */
-  float factor;
+  double factor;
   int32_t rotary_dim;
   int32_t layout;     /* dag_rope_layout_t                                                       */
 } dag_rope_t;
@@ -164,7 +164,7 @@ int dag_rope_frequencies(double* freq, int32_t rotary_dim, double theta, double 
  * lie next to each other, tokens `stride` elements apart (the parts of a fused projection, say).  q_out may be q and k_out k, with the same
  * stride; no other output may overlap an input.  transposed != 0: the transposed rotation, with which gradients of the outputs become those of
  * the inputs (the inverse where factor is 1).  All DEVICE, 16-byte aligned, strides a multiple of 16 bytes.  head_dim and rotary_dim multiples of
- * 16, head_dim <= 256; DAG_F32 or DAG_BF16; angles in 64 bits, the rotation in 32.
+ * 16, head_dim <= 256; DAG_F32 (angles and rotation in 64 bits) or DAG_BF16 (the rotation in 32).
  * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_HIP. */
 int dag_rope_apply(const dag_rope_t* rope, const int32_t* pos, int64_t n_tokens, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                    const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t hq, int32_t hkv, int32_t head_dim, int32_t transposed,

@@ -98,7 +98,7 @@ class dag_kv_q8_t(C.Structure):
 
 
 class dag_rope_t(C.Structure):
-    _fields_ = [("freq", C.c_void_p), ("factor", C.c_float), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
+    _fields_ = [("freq", C.c_void_p), ("factor", C.c_double), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
 
 
 class dag_kv_rows_t(C.Structure):

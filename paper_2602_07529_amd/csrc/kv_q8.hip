@@ -35,7 +35,7 @@ struct AppendArgs {
   RopeTheta theta;
   // rotary positions as a description has them
   const double* freq;
-  float factor;
+  double factor;
   int rotary;
   bool pairs;
   int64_t k_stride, v_stride;  // elements from a token to the next

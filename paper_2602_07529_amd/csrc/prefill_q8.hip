@@ -40,6 +40,7 @@ struct ChunkArgs {
   int few_rows;       // pairs that a block of them may have
   int few_most;       // pairs of a node up to which they are
   float sc;           // softmax_scale * log2(e)
+  float back;         // what takes a logarithm to base 2 of a sum of exponentials back: the inverse of the factor that is in sc, as it was rounded
 };
 
 // New tokens of a node times query heads of a KV head, up to which they are k_q8_chunk_few's.
@@ -268,7 +269,7 @@ __device__ __forceinline__ void store_out(const ChunkArgs& a, size_t at, const f
       y[1] = dag_pack_bf2(O[db][4 * r + 2] * inv, O[db][4 * r + 3] * inv);
       *(u32x2*)(a.out + at * D + 32 * db + 8 * r + 4 * H) = y;
     }
-  if (a.lse && H == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  if (a.lse && H == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * a.back;
 }
 
 constexpr float TOP_SUM = 1073741824.f;  // of a block's probabilities relative to the reference: 2^30
@@ -748,7 +749,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
   for (int e = 0; e < EACH / 2; ++e) y[e] = dag_pack_bf2(o[2 * e] * inv, o[2 * e + 1] * inv);
 #pragma unroll
   for (int e = 0; e < EACH / 2; e += 2) *(u32x2*)(a.out + at * D + d0 + 2 * e) = u32x2{y[e], y[e + 1]};
-  if (a.lse && d0 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+  if (a.lse && d0 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * a.back;
 }
 
 // Puts the stretches of a context together, in their order: a wave to a pair, a lane to a stretch and then to D / 64 dims.
@@ -792,7 +793,7 @@ __global__ void __launch_bounds__(256) k_q8_chunk_merge(ChunkArgs a) {
   const float inv = total == 0.f ? 0.f : 1.f / total;
   if constexpr (EACH == 2) *(uint32_t*)(a.out + to * D + 2 * lane) = dag_pack_bf2(o[0] * inv, o[EACH - 1] * inv);
   else a.out[to * D + lane] = (uint16_t)dag_pack_bf2(o[0] * inv, 0.f);
-  if (a.lse && lane == 0) a.lse[to] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+  if (a.lse && lane == 0) a.lse[to] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * a.back;
 }
 
 // How the contexts are cut: `splits` stretches of `slice` tiles, for `slots` blocks of `pairs` pairs.
@@ -961,5 +962,6 @@ extern "C" int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* d, cons
   a.hq = hq;
   a.G = hq / kv->hkv;
   a.sc = std::isfinite(softmax_scale) ? softmax_scale * 1.4426950408889634f : NAN;
+  a.back = (float)(a.sc != 0.f && std::isfinite(a.sc) ? (double)softmax_scale / (double)a.sc : 0.69314718055994530942);
   return kv->head_dim == 128 ? launch<128>(a, p, (hipStream_t)stream_) : launch<64>(a, p, (hipStream_t)stream_);
 }

@@ -2,11 +2,12 @@
 // head, forward or transposed.
 //
 // Pair m of a head turns by pos * freq[m]: y = factor (x cos - x' sin, x' cos + x sin); transposed, which is what the gradients go through, the
-// angle has the other sign.  Angles are taken in 64 bits, the rotation in 32, one rounding to the tensors' type.  Everything is read and written
+// angle has the other sign.  Angles are taken in 64 bits, the rotation in 32 for bf16 and in 64 for 32-bit tensors, with one rounding to their type.  Everything is read and written
 // once, which is what bounds it.  A workgroup turns the angles of its tokens into cosines and sines once for all heads (in LDS), and then
 // a thread has units of two 16-byte pieces whose elements are each other's partners (or stay as they are), two on their way together.
 // 18432 tokens of 40 heads of 128 in bf16: 68 us, 5.6 TB/s, with two tokens to a workgroup (four 70, eight 74, sixteen 80; one unit on its way 72, five 73).
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "turns.h"
@@ -24,23 +25,24 @@ struct RotaryArgs {
   int64_t n_tokens;
   int heads[2];
   int D, rotary;
-  float factor, sign;
+  double factor, sign;
   bool pairs;
 };
 
 template <bool BF16, int TOKENS>
 __global__ void __launch_bounds__(THREADS) k_rotary(RotaryArgs a) {
-  __shared__ float s_cos[TOKENS][MAX_HALF], s_sin[TOKENS][MAX_HALF];
+  using T = std::conditional_t<BF16, float, double>;
+  __shared__ T s_cos[TOKENS][MAX_HALF], s_sin[TOKENS][MAX_HALF];
   constexpr int EPV = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;
   const int half = a.rotary / 2;
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
   const int n = (int)min((int64_t)TOKENS, a.n_tokens - t0);
   for (int i = threadIdx.x; i < n * half; i += THREADS) {
     const int t = i / half, m = i % half;
-    float c, s;
+    double c, s;
     cos_sin_of_turns((double)a.pos[t0 + t] * (a.freq[m] * 0.15915494309189533577), &c, &s);
-    s_cos[t][m] = c * a.factor;
-    s_sin[t][m] = s * a.factor * a.sign;
+    s_cos[t][m] = (T)(c * a.factor);
+    s_sin[t][m] = (T)(s * a.factor * a.sign);
   }
   __syncthreads();
   const int upr = a.D / (2 * EPV), rows = a.heads[0] + a.heads[1], total = n * rows * upr, turned = half / EPV;
@@ -79,20 +81,20 @@ __global__ void __launch_bounds__(THREADS) k_rotary(RotaryArgs a) {
         }
       }
       if (unit[i] < turned) {
-        const float* const cs = &s_cos[token[i]][unit[i] * EPV];
-        const float* const sn = &s_sin[token[i]][unit[i] * EPV];
+        const T* const cs = &s_cos[token[i]][unit[i] * EPV];
+        const T* const sn = &s_sin[token[i]][unit[i] * EPV];
         float y[2 * EPV];
         if (a.pairs) {  // elements 2 e, 2 e + 1 of the two pieces behind one another
 #pragma unroll
           for (int e = 0; e < EPV; ++e) {
-            y[2 * e] = x[2 * e] * cs[e] - x[2 * e + 1] * sn[e];
-            y[2 * e + 1] = x[2 * e + 1] * cs[e] + x[2 * e] * sn[e];
+            y[2 * e] = (float)(x[2 * e] * cs[e] - x[2 * e + 1] * sn[e]);
+            y[2 * e + 1] = (float)(x[2 * e + 1] * cs[e] + x[2 * e] * sn[e]);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < EPV; ++e) {
-            y[e] = x[e] * cs[e] - x[EPV + e] * sn[e];
-            y[EPV + e] = x[EPV + e] * cs[e] + x[e] * sn[e];
+            y[e] = (float)(x[e] * cs[e] - x[EPV + e] * sn[e]);
+            y[EPV + e] = (float)(x[EPV + e] * cs[e] + x[e] * sn[e]);
           }
         }
 #pragma unroll

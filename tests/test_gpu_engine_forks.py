@@ -31,7 +31,7 @@ def test_branches(capture, rotary):
 
     def turned(k, first):
         k, pos = k.double().cpu().numpy(), first + np.arange(len(k))
-        return q8.rotary(k, pos, freq, True, float(np.float32(1.1))) if rotary else orc.rope(k, pos, 10000.0)
+        return q8.rotary(k, pos, freq, True, 1.1) if rotary else orc.rope(k, pos, 10000.0)
 
     history = [[turned(k0, 0), v0.double().cpu().numpy()] for _ in range(n)]  # what every branch has seen
 

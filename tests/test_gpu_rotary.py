@@ -20,7 +20,7 @@ SCALED = [dict(theta=10000.0), dict(theta=500000.0, stretch=8.0, original=8192.0
 def oracle_of(x, pos, rotary, pairs, kind, transposed=False):
     kind = dict(kind)
     factor = kind.pop("factor", 1.0)
-    return q8.rotary(x.double().cpu().numpy(), pos.cpu().numpy(), q8.frequencies(rotary, **kind), pairs, float(np.float32(factor)), transposed)
+    return q8.rotary(x.double().cpu().numpy(), pos.cpu().numpy(), q8.frequencies(rotary, **kind), pairs, factor, transposed)
 
 
 def near(got, x, want, factor):
@@ -131,7 +131,7 @@ def test_append(layout, d, rotary, dtype, n):
         B.dag_kv_append_rotary_q8(cache, ints(slots[a:b]), ints(pos[a:b]), k[a:b], v[a:b], rope)
     codes = {m: np.zeros((n_pages, hkv, 16, d)) for m in "kv"}
     scales = {m: np.ones((n_pages, hkv)) for m in "kv"}
-    kr = q8.rotary(k.double().cpu().numpy(), pos, q8.frequencies(rotary, 10000.0, 4.0, 2048.0), layout == B.ROPE_PAIRS, float(np.float32(1.1)))
+    kr = q8.rotary(k.double().cpu().numpy(), pos, q8.frequencies(rotary, 10000.0, 4.0, 2048.0), layout == B.ROPE_PAIRS, 1.1)
     vr = v.double().cpu().numpy()
     for a, b in ((0, 7), (11, 27), (27, 28), (28, n)):
         q8.append(codes["k"], scales["k"], kr[a:b], slots[a:b])
