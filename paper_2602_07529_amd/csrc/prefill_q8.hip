@@ -5,9 +5,25 @@
 // t_j = (scale log2(e) s) q . c_j, and so does the value scale z, p'_j = 2^(t_j - m + log2 z), which the sum of the probabilities
 // takes out again.
 //
-// A work item is 32 NW (row, query head) pairs of a node and KV head, row after row, against a stretch of its pages, 32 pairs to a wave.  A tile is
-// four pages: the threads fetch the codes of the tile after next into registers, put those of the next one into LDS (keys as they are,
-// values as bf16) and work on the present one.
+// Many pairs (k_q8_chunk).  A work item is 32 NW (row, query head) pairs of a node and KV head, row after row, against a stretch of its pages, 32
+// pairs to a wave.  A tile is four pages.  The threads fetch codes into registers a tile ahead of their use and put them into LDS as bf16, which
+// holds every e4m3 value: once for eight waves, not once a wave.  A wave works in steps of 32 keys, and a step is a straight run of three things that
+// do not wait for each other: the scores of the next 32 keys, the exponentials of these, the product of the ones before with their values; slot by
+// slot, a matrix product (transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane has one pair and its probabilities are operands as they lie),
+// the read of an operand four products ahead, an element of the exponentials.  The reference in the exponent is looked after behind the fact: only
+// where a block's probabilities sum to 2^30 is the maximum taken and the block done again (their size does not matter to bf16 and fp32).
+// Masks only where a tile has a page that is not full or reaches behind a wave's first row.  A value that is no number is not looked for in the
+// tiles: where the sums of a wave turn out to hold none, it goes over its pages once more (sums_again).
+// What bounds it: the matrix pipes and the power limit, as the bf16 form (1.8 GHz).  16 nodes of 2048 new tokens behind 8192, 32 / 8 heads of 128:
+// 4.2 to 4.5 ms, 1.1 to 1.2 PFLOP/s (a library product of 8192^3 in bf16 1.39); the first form, a barrier and whole blocks a tile, codes to
+// bf16 by every wave, took 6.8.  Scores as 8-bit products, q in two e4m3 parts, are 9 % faster (4.1), but that pipe's sums are off by 2^-19 of the
+// sum of their terms' magnitudes, the bf16 one's by 2^-24: not kept.  NW 8 against 4: 4.1 / 4.5 ms.
+//
+// Few pairs (k_q8_chunk_few, nodes of up to 64): a workgroup's four or eight waves share a stretch of the pages for 32 pairs, each a run of its own,
+// straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 34 us (130 MB); three nodes of nine behind 1500: 16.5,
+// of which what a step of a wave takes, a microsecond, is the most.
+//
+// Contexts are cut among workgroups by what that costs (cut); a second launch puts the stretches together.
 #include <algorithm>
 #include <cmath>
 
@@ -16,7 +32,6 @@
 
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
 constexpr int PAGE = DAG_PAGE_SIZE;
 constexpr int TILE = 4;          // pages
 constexpr int MAX_SPLITS = 64;   // (the lanes of the wave that puts them together)
@@ -104,58 +119,11 @@ __device__ __forceinline__ float2 page_scales(const ChunkArgs& a, float ks, floa
 
 template <int D, int NW>
 struct Lds {
-  static constexpr int KPAGE = D * PAGE;
-  uint8_t k[2][TILE * KPAGE];
+  uint8_t k[3][TILE * D * PAGE * 2];  // [page][half of a piece][piece of 16 dims][slot][8 dims]
   uint8_t v[3][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
   float2 page[4][TILE];               // key scale with the softmax's, log2 of the value scale
   int len[4][TILE];                   // tokens
 };
-
-// Query operands in 8 bits: q = 2^e (a + 2^-5 b) with a and b in e4m3, e the row's: a has the first four significant bits of an element, b the
-// other four.  Exact for elements down to 2^-14 of the row's largest, below that off by at most 2^-22 of it.
-template <int D>
-struct QueryCodes {
-  i32x8 a[D / 64], b[D / 64];
-  int ea, eb;  // scale bytes
-};
-template <int D>
-__device__ __forceinline__ void split_q(QueryCodes<D>& y, const bf16x8 (&q)[D / 16]) {
-  float most = 0.f;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const u32x4 x = __builtin_bit_cast(u32x4, q[s]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float lo = fabsf(dag_bf_lo(x[i])), hi = fabsf(dag_bf_hi(x[i]));
-      most = fmaxf(most, fmaxf(lo < INFINITY ? lo : 0.f, hi < INFINITY ? hi : 0.f));
-    }
-  }
-  most = fmaxf(most, other_half(most));
-  const int e = max((int)(__float_as_uint(most) >> 23) - 127 - 7, -121);  // largest element in [128, 256) (2^-114 and more)
-  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const u32x4 x = __builtin_bit_cast(u32x4, q[s]);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float f[4];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        f[2 * j] = dag_bf_lo(x[2 * i + j]) * inv;
-        f[2 * j + 1] = dag_bf_hi(x[2 * i + j]) * inv;
-      }
-      int wa = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-      wa = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], wa, true);
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(wa, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(wa, true);
-      int wb = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - lo[0]) * 32.f, (f[1] - lo[1]) * 32.f, 0, false);
-      wb = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - hi[0]) * 32.f, (f[3] - hi[1]) * 32.f, wb, true);
-      y.a[s / 4][2 * (s % 4) + i] = wa;
-      y.b[s / 4][2 * (s % 4) + i] = wb;
-    }
-  }
-  y.ea = 127 + e;
-  y.eb = 127 + e - 5;
-}
 
 // A wave's pairs once more, page by page from memory, where a value that is no number was among those that it multiplied: it may not reach
 // the rows that do not see it, and a probability of zero does not keep it from them.  Such values are cleared here, and the sums of the rows
@@ -302,13 +270,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
   float m = -1e30f, l = 0.f;
 
   if (t0 < t1) {
-    QueryCodes<D> q;
-    {
-      bf16x8 x[D / 16];
-      fetch_q<D>(x, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
-      sign_q<D>(x, a.sc);
-      split_q<D>(q, x);
-    }
+    bf16x8 q[D / 16];
+    fetch_q<D>(q, a.q + ((size_t)(pl.row0 + row) * a.hq + head) * D, lane);
+    sign_q<D>(q, a.sc);
     // ids and tokens of 64 pages, a lane each, and of the 64 behind them
     int win_pg, win_len, next_pg, next_len;
     auto ask = [&](int rel) __attribute__((always_inline)) {
@@ -347,11 +311,14 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       for (int i = 0; i < PIECES; ++i)
         if (my_v) fetch(a.kv.v_pool, t, i, vpiece[i], &held[i]);
     };
-    auto store_k = [&](int t) __attribute__((always_inline)) {
+    auto store_k = [&](int t, int buf) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const int x = wv * 64 + i * THREADS;
-        if (my_k) *(u32x4*)(lds.k[t & 1] + x / D * lds.KPAGE + (x % D + lane) * 16) = kpiece[i];
+        if (!my_k) break;
+        uint8_t* const to = lds.k[buf] + x / D * (D * 32) + (x % D + lane) * 16;
+        *(bf16x8*)to = codes_to_bf16(kpiece[i][0], kpiece[i][1]);
+        *(bf16x8*)(to + D * 16) = codes_to_bf16(kpiece[i][2], kpiece[i][3]);
       }
       if (w < TILE && lane == 0) {
         lds.page[t & 3][w] = page_scales(a, ks, vs, len);
@@ -373,23 +340,23 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
       }
     };
-    const int koff = (L >> 2 & 1) * lds.KPAGE + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = H * (D * 32) + L * 16;
-    constexpr int NK = D / 32, NV = D / 16, SLOTS = 3 * D / 32;  // operands of a block's keys and values, matrix products of a step
-    int v_old = 0, v_now = 0, v_next = 1;  // buffers of the values of tiles t - 1, t, t + 1
-    constexpr int AHEAD = 4;  // operands of values on their way
-    u32x4 kop[NK], vop[AHEAD];
-    auto read_k = [&](int i, int t, int b) __attribute__((always_inline)) { kop[i] = *(const u32x4*)(lds.k[t & 1] + 2 * b * lds.KPAGE + koff + i * 512); };
+    const int koff = (L >> 2 & 1) * (D * 32) + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = H * (D * 32) + L * 16;
+    constexpr int NK = D / 16, NV = D / 16, SLOTS = D / 8;  // operands of a block's keys and values, matrix products of a step
+    int v_old = 0, v_now = 0, v_next = 1;  // buffers of tiles t - 1 (values), t and t + 1
+    constexpr int AHEAD = 4;  // operands of either on their way
+    u32x4 kop[AHEAD], vop[AHEAD];
+    auto read_k = [&](int i, int buf, int b) __attribute__((always_inline)) {
+      kop[i % AHEAD] = *(const u32x4*)(lds.k[buf] + 2 * b * (D * 32) + koff + (i & 1) * (D * 16) + (i >> 1) * 512);
+    };
     auto read_v = [&](int i, int buf, int b) __attribute__((always_inline)) {
       vop[i % AHEAD] = *(const u32x4*)(lds.v[buf] + 2 * b * (D * 32) + voff + i / (D / 32) * (D * 16) + i % (D / 32) * 512);
     };
     auto score = [&](f32x16& S, int j) __attribute__((always_inline)) {  // product j of a block's scores
-      const u32x4 x = kop[j & ~1], y = kop[j | 1];
-      const i32x8 k = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
       if (j == 0) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[r] = 0.f;
       }
-      S = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, j & 1 ? q.b[j >> 1] : q.a[j >> 1], S, 0, 0, 0, 127, 0, j & 1 ? q.eb : q.ea);
+      S = mfma32(__builtin_bit_cast(bf16x8, kop[j % AHEAD]), q[j], S);
     };
     auto product = [&](int i, const u32x4(&p)[2]) __attribute__((always_inline)) {
       O[i % (D / 32)] = mfma32(__builtin_bit_cast(bf16x8, vop[i % AHEAD]), __builtin_bit_cast(bf16x8, p[i / (D / 32)]), O[i % (D / 32)]);
@@ -434,15 +401,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < SLOTS; ++i) {
-        if (i % 3 == 0) {
-          const int j = i / 3;
+        const int j = i >> 1;
+        if ((i & 1) == 0) {
           score(S_next, j);
-          if (j & 1) {
-            read_k(j - 1, t + 1, b);
-            read_k(j, t + 1, b);
-          }
+          if (j + AHEAD < NK) read_k(j + AHEAD, b ? v_next : v_now, 1 - b);  // of this block g + 1, then of the next one
+          else read_k(j + AHEAD - NK, v_next, b);
         } else {
-          const int j = i / 3 * 2 + i % 3 - 1;
           product(j, p_before);
           if (j + AHEAD < NV) read_v(j + AHEAD, b ? v_now : v_old, 1 - b);  // of this block g - 1, then of the next one
           else read_v(j + AHEAD - NV, v_now, b);
@@ -507,24 +471,27 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
     load_k(t0);
     load_v(t0);
     f0 = is_full(t0);
-    store_k(t0);
+    store_k(t0, 0);
     store_v(0);
     window(t0 + 1);
     load_k(t0 + 1);
     load_v(t0 + 1);
     f1 = is_full(t0 + 1);
-    store_k(t0 + 1);
+    store_k(t0 + 1, 1);
     window(t0 + 2);
     load_k(t0 + 2);
     f2 = is_full(t0 + 2);
     lds_barrier();
     f32x16 S0, S1;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) read_k(i, t0, 0);
+    for (int i = 0; i < AHEAD; ++i) read_k(i, 0, 0);
 #pragma unroll
-    for (int j = 0; j < NK; ++j) score(S0, j);
+    for (int j = 0; j < NK; ++j) {
+      score(S0, j);
+      if (j + AHEAD < NK) read_k(j + AHEAD, 0, 0);
+    }
 #pragma unroll
-    for (int i = 0; i < NK; ++i) read_k(i, t0, 1);
+    for (int i = 0; i < AHEAD; ++i) read_k(i, 0, 1);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read_v(i, 0, 1);  // (the first product is of zeros)
     float2 page0 = lds.page[t0 & 3][H], page1 = lds.page[t0 & 3][2 + H];
@@ -533,7 +500,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       if (idle) {  // no row is this wave's: it fetches its share and leaves the matrix pipe to the others
         store_v(v_next);
         load_v(t + 2);
-        store_k(t + 2);
+        store_k(t + 2, 3 - v_now - v_next);
         window(t + 3);
         load_k(t + 3);
       } else {
@@ -543,7 +510,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         page0 = lds.page[(t + 1) & 3][H];
       });
       step(S1, S0, P[1], P[0], page1, t, 1, !f0, [&]() __attribute__((always_inline)) {
-        store_k(t + 2);
+        store_k(t + 2, 3 - v_now - v_next);
         window(t + 3);
         load_k(t + 3);
         f3 = is_full(t + 3);
@@ -852,7 +819,7 @@ bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, in
       p->few_waves = 8;
     }
   }
-  p->waves = most <= 128 ? 4 : 8;
+  p->waves = most <= 128 && D == 64 ? 4 : 8;  // (at dimension 128 two workgroups' tiles do not fit a compute unit)
   if (!none && most > FEW_PAIRS) {
     p->many.pairs = 32 * p->waves;
     p->many.slots = n_rows * G / p->many.pairs + d->n_nodes;  // (the last node's last one is below: find_place)
@@ -904,7 +871,9 @@ int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   float* const ws = a.part_o;
   if (p.many.slots > 0) {
     use(p.many, ws);
-    const int rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
+    int rc;
+    if constexpr (D == 64) rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
+    else rc = launch_many<D, 8>(a, p.many, stream);
     if (rc != DAG_OK) return rc;
   }
   if (p.few.slots == 0) return DAG_OK;
