@@ -378,11 +378,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
       const float inv = __builtin_amdgcn_exp2f(-plv);
       float ref = plv - m, sum[2] = {0.f, 0.f};
       float x[16];
-      // (elements of slot i)
+      // (elements of slot i; the last two slots have none left, so that their sum is there when it is asked for: 853 -> 832 us for 64 joins of 131)
       auto of_slot = [&](int i, auto&& f) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (r >= i * 16 / SLOTS && r < (i + 1) * 16 / SLOTS) f(r);
+          if (i < SLOTS - 2 && r >= i * 16 / (SLOTS - 2) && r < (i + 1) * 16 / (SLOTS - 2)) f(r);
       };
       auto soft_a = [&](int i) __attribute__((always_inline)) { of_slot(i, [&](int r) __attribute__((always_inline)) { x[r] = fmaf(S[r], pks, ref); }); };
       auto soft_b = [&](int i) __attribute__((always_inline)) { of_slot(i, [&](int r) __attribute__((always_inline)) { x[r] = __builtin_amdgcn_exp2f(x[r]); }); };
