@@ -164,7 +164,7 @@ int dag_rope_frequencies(double* freq, int32_t rotary_dim, double theta, double 
  * lie next to each other, tokens `stride` elements apart (the parts of a fused projection, say).  q_out may be q and k_out k, with the same
  * stride; no other output may overlap an input.  transposed != 0: the transposed rotation, with which gradients of the outputs become those of
  * the inputs (the inverse where factor is 1).  All DEVICE, 16-byte aligned, strides a multiple of 16 bytes.  head_dim and rotary_dim multiples of
- * 16, head_dim <= 256; DAG_F32 (angles and rotation in 64 bits) or DAG_BF16 (the rotation in 32).
+ * 16, head_dim <= 256, at most 4096 heads; DAG_F32 (angles and rotation in 64 bits) or DAG_BF16 (the rotation in 32).
  * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_HIP. */
 int dag_rope_apply(const dag_rope_t* rope, const int32_t* pos, int64_t n_tokens, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                    const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t hq, int32_t hkv, int32_t head_dim, int32_t transposed,
@@ -463,8 +463,8 @@ int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* desc, const dag_kv_
  * slots behind its last token may hold any codes, and what a row does not see does not reach it, whatever it holds; page ids outside the
  * pool are clamped, never followed; a row that sees no token gets zeros and an lse of minus infinity.  softmax_scale may be of either sign, or zero;
  * if it is not finite the rows that see a token get NaN.  Sums, maxima and partial results are fp32; probabilities are rounded to bf16 for the
- * second product.  Enqueued on `stream` (one launch, two where contexts are cut among workgroups); the call allocates nothing and does
- * not synchronise; calls that overlap need a workspace each (16-byte aligned; may be NULL where no bytes are needed).
+ * second product.  Enqueued on `stream` (one launch, another where contexts are cut among workgroups, and the same for the nodes of few new tokens
+ * beside those of many); the call allocates nothing and does not synchronise; calls that overlap need a workspace each (16-byte aligned; may be NULL where no bytes are needed).
  * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE, DAG_ERR_HIP. */
 size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* desc, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim);
 int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* desc, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
