@@ -19,9 +19,9 @@
 // bf16 by every wave, took 6.8.  Scores as 8-bit products, q in two e4m3 parts, are 9 % faster (4.1), but that pipe's sums are off by 2^-19 of the
 // sum of their terms' magnitudes, the bf16 one's by 2^-24: not kept.  NW 8 against 4: 4.1 / 4.5 ms.
 //
-// Few pairs (k_q8_chunk_few, nodes of up to 64): a workgroup's four or eight waves share a stretch of the pages for 32 pairs, each a run of its own,
-// straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 34 us (130 MB); three nodes of nine behind 1500: 16.5,
-// of which what a step of a wave takes, a microsecond, is the most.
+// Few pairs (k_q8_chunk_few, nodes of up to 64): a workgroup's four waves share a stretch of the pages for 32 pairs, each a run of its own,
+// straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 35 us (130 MB); three nodes of nine behind 1500: 14,
+// of which what a step of a wave takes, half a microsecond to one, is the most.
 //
 // Contexts are cut among workgroups by what that costs (cut); a second launch puts the stretches together.
 #include <algorithm>
@@ -504,18 +504,18 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         window(t + 3);
         load_k(t + 3);
       } else {
-      step(S0, S1, P[0], P[1], page0, t, 0, !f0, [&]() __attribute__((always_inline)) {
-        store_v(v_next);
-        load_v(t + 2);
-        page0 = lds.page[(t + 1) & 3][H];
-      });
-      step(S1, S0, P[1], P[0], page1, t, 1, !f0, [&]() __attribute__((always_inline)) {
-        store_k(t + 2, 3 - v_now - v_next);
-        window(t + 3);
-        load_k(t + 3);
-        f3 = is_full(t + 3);
-        page1 = lds.page[(t + 1) & 3][2 + H];
-      });
+        step(S0, S1, P[0], P[1], page0, t, 0, !f0, [&]() __attribute__((always_inline)) {
+          store_v(v_next);
+          load_v(t + 2);
+          page0 = lds.page[(t + 1) & 3][H];
+        });
+        step(S1, S0, P[1], P[0], page1, t, 1, !f0, [&]() __attribute__((always_inline)) {
+          store_k(t + 2, 3 - v_now - v_next);
+          window(t + 3);
+          load_k(t + 3);
+          f3 = is_full(t + 3);
+          page1 = lds.page[(t + 1) & 3][2 + H];
+        });
       }
       v_old = v_now;
       v_now = v_next;
@@ -542,7 +542,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
 
 // Few pairs: 32 of them to a workgroup, whose waves share a stretch of the pages, each a run of its own, straight from memory, and put their sums
 // together in LDS.  What bounds it is how the pages come: two blocks of two pages of a wave are on their way.
-template <int D, int FEW_WAVES>
+constexpr int FEW_WAVES = 4;
+template <int D>
 __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_o[];  // [wave][pair][D + 4], of as many pairs as a block may have
   __shared__ float2 s_ml[FEW_WAVES][32];
@@ -771,7 +772,7 @@ struct Cut {
 };
 struct Plan {
   Cut few, many;  // slots 0: not launched
-  int blocks, few_rows, few_waves, waves;
+  int blocks, few_rows, waves;
   size_t floats(int hkv, int D) const { return (few.parts(hkv) + many.parts(hkv)) * (D + 2); }
 };
 // As many stretches as take the least time: rounds of the workgroups that the device holds at once, each as long as its steps through a stretch
@@ -802,22 +803,14 @@ bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, in
   const int64_t G = hq / hkv, tiles = dag_ceil_div(d->max_ctx_pages, TILE), most = d->max_new * G;
   const bool none = d->max_new == 0 || d->n_nodes == 0 || n_rows == 0;
   p->few = p->many = Cut{0, 1, 1, 32};
-  p->few_waves = 4;
   p->blocks = (int)std::max<int64_t>(1, dag_ceil_div(std::min<int64_t>(most, FEW_PAIRS), 32));
   p->few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, 32));
   // (few new tokens in all: a node with more is a tile kernel's, which has a slot for it wherever there is one)
   // (a single node whose bound is past them is one of many pairs, whatever it has: a launch less)
   if (!none && (most <= FEW_PAIRS || d->n_nodes > 1)) {
     p->few.slots = (int64_t)d->n_nodes * p->blocks;
-    // four waves to a workgroup, or eight where that leaves compute units free
-    const double items = (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv;
-    Cut wide = p->few;
-    const double time = cut(&p->few, items, tiles, D, Cost{0.4, 5., 4., 512});
-    p->few_waves = 4;
-    if (cut(&wide, items, tiles, D, Cost{0.28, 5., 4., 256}) < time) {
-      p->few = wide;
-      p->few_waves = 8;
-    }
+    // (eight waves to a workgroup in place of a cut: three nodes of nine behind 1500 16.7 us, cut 14.2; one token behind 2000 11.2, 9.4)
+    cut(&p->few, (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv, tiles, D, Cost{0.4, 5., 4., 512});
   }
   p->waves = most <= 128 && D == 64 ? 4 : 8;  // (at dimension 128 two workgroups' tiles do not fit a compute unit)
   if (!none && most > FEW_PAIRS) {
@@ -848,15 +841,6 @@ int launch_many(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
   }
   return DAG_OK;
 }
-template <int D, int FEW_WAVES>
-int launch_few(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
-  const size_t lds = (size_t)FEW_WAVES * a.few_rows * (D + 4) * sizeof(float);
-  auto* const kernel = k_q8_chunk_few<D, FEW_WAVES>;
-  if (lds > 65536 && hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return DAG_ERR_HIP;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(c.slots * a.kv.hkv * c.splits)), dim3(64 * FEW_WAVES), lds, stream, a);
-  DAG_LAUNCH_CHECK();
-  return DAG_OK;
-}
 template <int D>
 int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   a.blocks = p.blocks;
@@ -878,8 +862,11 @@ int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   }
   if (p.few.slots == 0) return DAG_OK;
   use(p.few, ws + p.many.parts(a.kv.hkv) * (D + 2));
-  const int rc = p.few_waves == 4 ? launch_few<D, 4>(a, p.few, stream) : launch_few<D, 8>(a, p.few, stream);
-  if (rc != DAG_OK) return rc;
+  const size_t lds = (size_t)FEW_WAVES * a.few_rows * (D + 4) * sizeof(float);
+  static_assert((size_t)FEW_WAVES * 32 * (D + 4) * sizeof(float) <= 68 << 10, "");
+  if (lds > 65536 && hipFuncSetAttribute((const void*)k_q8_chunk_few<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return DAG_ERR_HIP;
+  hipLaunchKernelGGL(k_q8_chunk_few<D>, dim3((unsigned)(p.few.slots * a.kv.hkv * p.few.splits)), dim3(64 * FEW_WAVES), lds, stream, a);
+  DAG_LAUNCH_CHECK();
   if (p.few.splits > 1) {
     hipLaunchKernelGGL((k_q8_chunk_merge<D, 32, true>), dim3((unsigned)(p.few.slots * a.kv.hkv * 8)), dim3(256), 0, stream, a);
     DAG_LAUNCH_CHECK();
