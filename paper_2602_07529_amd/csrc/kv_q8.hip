@@ -33,7 +33,9 @@ struct AppendArgs {
   int64_t n_slots;
   int hkv;
   RopeTheta theta;
-  // rotary positions as a description has them
+};
+// With rotary positions as a description has them.
+struct RotaryAppendArgs : AppendArgs {
   const double* freq;
   double factor;
   int rotary;
@@ -47,7 +49,10 @@ struct Partners {
   int lo, hi;
   bool turned, apart;
 };
-__device__ __forceinline__ Partners partners(const AppendArgs& a, int m, int each) {
+template <int D>
+__device__ __forceinline__ Partners partners(const AppendArgs&, int m, int each) { return Partners{m, m + D / (2 * each), true, true}; }
+template <int D>
+__device__ __forceinline__ Partners partners(const RotaryAppendArgs& a, int m, int each) {
   const int half = a.rotary / (2 * each);
   Partners p;
   p.turned = m < half;
@@ -56,6 +61,19 @@ __device__ __forceinline__ Partners partners(const AppendArgs& a, int m, int eac
   p.hi = p.apart ? m + half : 2 * m + 1;
   return p;
 }
+// Where head h of token t begins among the new keys, the new values; what pair m turns by for a position (0 for one that does not).
+template <int D>
+__device__ __forceinline__ size_t key_at(const AppendArgs& a, int64_t t, int h) { return ((size_t)t * a.hkv + h) * D; }
+template <int D>
+__device__ __forceinline__ size_t key_at(const RotaryAppendArgs& a, int64_t t, int h) { return (size_t)t * a.k_stride + h * D; }
+template <int D>
+__device__ __forceinline__ size_t value_at(const AppendArgs& a, int64_t t, int h) { return ((size_t)t * a.hkv + h) * D; }
+template <int D>
+__device__ __forceinline__ size_t value_at(const RotaryAppendArgs& a, int64_t t, int h) { return (size_t)t * a.v_stride + h * D; }
+template <int D>
+__device__ __forceinline__ double frequency(const AppendArgs& a, int m) { return dag_rope_freq(a.theta, m, D); }
+template <int D>
+__device__ __forceinline__ double frequency(const RotaryAppendArgs& a, int m) { return m < a.rotary / 2 ? a.freq[m] : 0.; }
 
 // 2^k with the smallest k of at least -100 that brings `most` (finite, not negative) within 448 = 0.875 * 2^9.
 __device__ __forceinline__ float q8_scale(float most) {
@@ -116,6 +134,8 @@ struct Raw2 {
 
 constexpr int SPAN = 16, THREADS = 256;
 template <bool ROTARY>
+using ArgsOf = std::conditional_t<ROTARY, RotaryAppendArgs, AppendArgs>;
+template <bool ROTARY>
 using Angle = std::conditional_t<ROTARY, double, float>;
 // x cos - y sin and x sin + y cos (as dag_kv_append_rope rotates, in 32 bits).
 __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
@@ -136,7 +156,7 @@ struct Angles {  // of the tokens from a workgroup's first one on; lines four lo
 
 // A run of n tokens from token t0 on, which go to the slots i0 .. of a page; ang: row of the first one's angles.
 template <int D, bool BF16, bool ROTARY>
-__device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D, Angle<ROTARY>>& angles, int ang, int64_t t0, int n, int64_t page, int i0, int h,
+__device__ __forceinline__ void append_run(const ArgsOf<ROTARY>& a, const Angles<D, Angle<ROTARY>>& angles, int ang, int64_t t0, int n, int64_t page, int i0, int h,
                                            int lane) {
   const bool begins = i0 == 0;
   const size_t ph = (size_t)page * a.hkv + h;
@@ -144,10 +164,10 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D, 
   // keys
   const int slot = lane & 15, g = lane >> 4, j = slot - i0;
   const bool active = g < HALF / 16, mine = active && j >= 0 && j < n;
-  const Partners pt = ROTARY ? partners(a, g, 16) : Partners{g, g + HALF / 16, true, true};
+  const Partners pt = partners<D>(a, g, 16);
   Raw16<BF16> k_lo, k_hi;
   if (mine) {
-    const size_t at = ROTARY ? (size_t)(t0 + j) * a.k_stride + h * D : ((size_t)(t0 + j) * a.hkv + h) * D;
+    const size_t at = key_at<D>(a, t0 + j, h);
     k_lo.load(a.k_new, at + 16 * pt.lo);
     k_hi.load(a.k_new, at + 16 * pt.hi);
   }
@@ -156,7 +176,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D, 
   Raw2<BF16> v[PAGE] = {};
 #pragma unroll
   for (int i = 0; i < PAGE; ++i)
-    if (active_v && i >= i0 && i < i0 + n) v[i].load(a.v_new, (ROTARY ? (size_t)(t0 + i - i0) * a.v_stride + h * D : ((size_t)(t0 + i - i0) * a.hkv + h) * D) + 2 * lane);
+    if (active_v && i >= i0 && i < i0 + n) v[i].load(a.v_new, value_at<D>(a, t0 + i - i0, h) + 2 * lane);
   const float before = begins ? 0.f : a.k_scale[ph], before_v = begins ? 0.f : a.v_scale[ph];
   float lo[16], hi[16], most = 0.f;
   if (mine) {
@@ -240,14 +260,13 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, const Angles<D, 
 
 // A single token.  Where its page begins or its scale grows the whole page is written, else the token's bytes.
 template <int D, bool BF16, bool ROTARY>
-__device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D, Angle<ROTARY>>& angles, int ang, uint8_t* lds, int64_t t, int64_t page, int i0, int h,
+__device__ __forceinline__ void append_one(const ArgsOf<ROTARY>& a, const Angles<D, Angle<ROTARY>>& angles, int ang, uint8_t* lds, int64_t t, int64_t page, int i0, int h,
                                            int lane) {
   constexpr int HALF = D / 2;
   const bool begins = i0 == 0, active = lane < HALF;
   const int m = active ? lane : 0;
-  const size_t ph = (size_t)page * a.hkv + h, at = ROTARY ? (size_t)t * a.k_stride + h * D : ((size_t)t * a.hkv + h) * D;
-  const size_t at_v = ROTARY ? (size_t)t * a.v_stride + h * D : at;
-  const Partners pt = ROTARY ? partners(a, m, 1) : Partners{m, m + HALF, true, true};
+  const size_t ph = (size_t)page * a.hkv + h, at = key_at<D>(a, t, h), at_v = value_at<D>(a, t, h);
+  const Partners pt = partners<D>(a, m, 1);
   float x, y;
   if constexpr (BF16) {
     x = __uint_as_float((uint32_t)((const uint16_t*)a.k_new)[at + pt.lo] << 16);
@@ -312,7 +331,7 @@ __device__ __forceinline__ void append_one(const AppendArgs& a, const Angles<D, 
 }
 
 template <int D, bool BF16, bool ROTARY>
-__global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendArgs a, int span) {
+__global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(ArgsOf<ROTARY> a, int span) {
   __shared__ Angles<D, Angle<ROTARY>> angles;
   __shared__ __attribute__((aligned(16))) uint8_t one[THREADS / 64][D];
   constexpr int HALF = D / 2;
@@ -331,9 +350,8 @@ __global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendAr
   const int begin = __builtin_ctzll(lead), last = 63 - __builtin_clzll(lead), n_ang = last + length(last) - begin;
   {
     const int m = tid % HALF;
-    const bool turned = !ROTARY || m < a.rotary / 2;
-    const double f = (ROTARY ? (turned ? a.freq[m] : 0.) : dag_rope_freq(a.theta, m, D)) * 0.15915494309189533577;  // turns
-    for (int i = tid / HALF; turned && i < n_ang; i += THREADS / HALF) {
+    const double f = frequency<D>(a, m) * 0.15915494309189533577;  // turns
+    for (int i = tid / HALF; i < n_ang; i += THREADS / HALF) {
       cos_sin_of_turns((double)a.pos[first - 1 + begin + i] * f, &angles.cs[i][m], &angles.sn[i][m]);
       if constexpr (ROTARY) {
         angles.cs[i][m] *= a.factor;
@@ -354,7 +372,7 @@ __global__ void __launch_bounds__(THREADS, BF16 ? 3 : 2) k_kv_append_q8(AppendAr
 }
 
 template <bool ROTARY>
-int launch_append(const AppendArgs& a, int D, dag_dtype_t dtype, hipStream_t stream) {
+int launch_append(const ArgsOf<ROTARY>& a, int D, dag_dtype_t dtype, hipStream_t stream) {
   auto* const kernel = dtype == DAG_BF16 ? (D == 128 ? k_kv_append_q8<128, true, ROTARY> : k_kv_append_q8<64, true, ROTARY>)
                                          : (D == 128 ? k_kv_append_q8<128, false, ROTARY> : k_kv_append_q8<64, false, ROTARY>);
   const int span = a.n_tokens >= 512 * SPAN ? SPAN : a.n_tokens >= 2048 ? 4 : 1;
@@ -376,8 +394,9 @@ int check_append(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos
   return DAG_OK;
 }
 
-AppendArgs append_args(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new, const void* v_new) {
-  AppendArgs a = {};
+template <typename A>
+A append_args(const dag_kv_q8_t* kv, const int32_t* slots, const int32_t* pos, int64_t n_tokens, const void* k_new, const void* v_new) {
+  A a = {};
   a.slots = slots;
   a.pos = pos;
   a.k_new = k_new;
@@ -401,7 +420,7 @@ extern "C" int dag_kv_append_rope_q8(const dag_kv_q8_t* kv, const int32_t* slots
   if (!(theta > 0.f)) return DAG_ERR_UNSUPPORTED;
   const int rc = check_append(kv, slots, pos, n_tokens, k_new, v_new, dtype);
   if (rc != DAG_OK || n_tokens == 0) return rc;
-  AppendArgs a = append_args(kv, slots, pos, n_tokens, k_new, v_new);
+  AppendArgs a = append_args<AppendArgs>(kv, slots, pos, n_tokens, k_new, v_new);
   a.theta = dag_rope_theta(theta);
   return launch_append<false>(a, kv->head_dim, dtype, (hipStream_t)stream_);
 }
@@ -420,7 +439,7 @@ extern "C" int dag_kv_append_rotary_q8(const dag_kv_q8_t* kv, const int32_t* slo
   if (k_stride < row || v_stride < row) return DAG_ERR_BAD_LEN;
   if (!rope->freq) return DAG_ERR_NULL;
   if (k_stride % each != 0 || v_stride % each != 0 || ((uintptr_t)rope->freq & 7)) return DAG_ERR_ALIGN;
-  AppendArgs a = append_args(kv, slots, pos, n_tokens, k_new, v_new);
+  RotaryAppendArgs a = append_args<RotaryAppendArgs>(kv, slots, pos, n_tokens, k_new, v_new);
   a.freq = rope->freq;
   a.factor = rope->factor;
   a.rotary = rope->rotary_dim;
