@@ -464,7 +464,8 @@ int dag_attn_decode_segments_q8(const dag_decode_seg_desc_t* desc, const dag_kv_
  * pool are clamped, never followed; a row that sees no token gets zeros and an lse of minus infinity.  softmax_scale may be of either sign, or zero;
  * if it is not finite the rows that see a token get NaN.  Sums, maxima and partial results are fp32; probabilities are rounded to bf16 for the
  * second product.  Enqueued on `stream` (one launch, another where contexts are cut among workgroups, and the same for the nodes of few new tokens
- * beside those of many); the call allocates nothing and does not synchronise; calls that overlap need a workspace each (16-byte aligned; may be NULL where no bytes are needed).
+ * beside those of many); the call allocates nothing and does not synchronise; calls that overlap need a workspace each (16-byte aligned, of the
+ * bytes that the same description, n_rows and heads ask for; may be NULL where no bytes are needed).
  * Errors: DAG_ERR_NULL, DAG_ERR_BAD_LEN, DAG_ERR_UNSUPPORTED, DAG_ERR_ALIGN, DAG_ERR_WORKSPACE, DAG_ERR_HIP. */
 size_t dag_prefill_paged_q8_workspace_bytes(const dag_paged_prefill_desc_t* desc, int64_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim);
 int dag_attn_prefill_paged_q8(const dag_paged_prefill_desc_t* desc, const dag_kv_q8_t* kv, const void* q, int64_t n_rows, void* out, float* lse,
