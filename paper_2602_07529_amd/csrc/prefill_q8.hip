@@ -3,7 +3,7 @@
 // out_i = sum_j p_ij v_j / sum_j p_ij with p_ij = exp(scale q_i . k_j), over the slots j of the node's list of pages that hold a token and do
 // not lie behind new token i.  A code c of a page stands for its scale times c; the key scale goes into the exponent,
 // t_j = (scale log2(e) s) q . c_j, and so does the value scale z, p'_j = 2^(t_j - m + log2 z), which the sum of the probabilities
-// takes out again.
+// takes out again (value_exponent: all of it but what is left over of a tiny one, which the values get).
 //
 // Many pairs (k_q8_chunk).  A work item is 32 NW (row, query head) pairs of a node and KV head, row after row, against a stretch of its pages, 32
 // pairs to a wave.  A tile is four pages.  The threads fetch codes into registers a tile ahead of their use and put them into LDS as bf16, which
@@ -114,14 +114,15 @@ __device__ __forceinline__ uint32_t slots_mask(int n) { return n >= 4 ? 0xffffff
 __device__ __forceinline__ float2 page_scales(const ChunkArgs& a, float ks, float vs, int len) {
   ks *= fabsf(a.sc);
   ks = ks < 1.2e-38f ? 1.2e-38f : ks;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
-  return len == 0 ? make_float2(1.f, 0.f) : make_float2(ks, __builtin_amdgcn_logf(vs));  // (nobody looks at the scales of a page without tokens)
+  return len == 0 ? make_float2(1.f, 0.f) : make_float2(ks, value_log2(vs));  // (nobody looks at the scales of a page without tokens)
 }
 
 template <int D, int NW>
 struct Lds {
   uint8_t k[3][TILE * D * PAGE * 2];  // [page][half of a piece][piece of 16 dims][slot][8 dims]
   uint8_t v[3][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
-  float2 page[4][TILE];               // key scale with the softmax's, log2 of the value scale
+  float2 page[4][TILE];               // key scale with the softmax's, what the exponent gets of the value scale
+  float left[4][TILE];                // what the values get of it
   int len[4][TILE];                   // tokens
 };
 
@@ -162,6 +163,8 @@ __device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, 
     const int plen = H ? len[1] : len[0], n = min(plen, lim - (pg0 + H) * PAGE + 1);
     float2 page = page_scales(a, a.kv.k_scale[mine], a.kv.v_scale[mine], plen);
     if (n <= 0) page = make_float2(1.f, 0.f);
+    float left;
+    page.y = value_exponent(page.y, &left);
     f32x16 S;
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[r] = 0.f;
@@ -207,7 +210,7 @@ __device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, 
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         none = mfma32(codes_to_bf16(one[2 * e], one[2 * e + 1]), __builtin_convertvector(seen[e], bf16x8), none);
-        O[db] = mfma32(codes_to_bf16(c[2 * e], c[2 * e + 1]), __builtin_convertvector(x[e], bf16x8), O[db]);
+        O[db] = mfma32(codes_to_bf16(c[2 * e], c[2 * e + 1], left), __builtin_convertvector(x[e], bf16x8), O[db]);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) O[db][r] = none[r] > 0.f ? NAN : O[db][r];
@@ -321,9 +324,17 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
         *(bf16x8*)(to + D * 16) = codes_to_bf16(kpiece[i][2], kpiece[i][3]);
       }
       if (w < TILE && lane == 0) {
-        lds.page[t & 3][w] = page_scales(a, ks, vs, len);
+        float2 page = page_scales(a, ks, vs, len);
+        page.y = value_exponent(page.y, &lds.left[t & 3][w]);
+        lds.page[t & 3][w] = page;
         lds.len[t & 3][w] = len;
       }
+    };
+    float left[PIECES];
+    auto ask_left = [&](int t) __attribute__((always_inline)) {  // (a barrier behind store_k of the tile, and some time in front of store_v)
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        if (my_v) left[i] = lds.left[t & 3][(wv * 64 + i * THREADS) / D];
     };
     auto store_v = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
@@ -336,8 +347,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
           for (int e = 0; e < 4; ++e) c[e] &= slots_mask(held[i] - 4 * e);
         }
         uint8_t* const to = lds.v[buf] + x / D * (D * 32) + (x % D + lane) * 16;
-        *(bf16x8*)to = codes_to_bf16(c[0], c[1]);
-        *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3]);
+        *(bf16x8*)to = codes_to_bf16(c[0], c[1], left[i]);
+        *(bf16x8*)(to + D * 16) = codes_to_bf16(c[2], c[3], left[i]);
       }
     };
     const int koff = (L >> 2 & 1) * (D * 32) + H * 256 + ((L & 3) + 4 * (L >> 3)) * 16, voff = H * (D * 32) + L * 16;
@@ -472,6 +483,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
     load_v(t0);
     f0 = is_full(t0);
     store_k(t0, 0);
+    lds_barrier();
+    ask_left(t0);
     store_v(0);
     window(t0 + 1);
     load_k(t0 + 1);
@@ -497,6 +510,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
     float2 page0 = lds.page[t0 & 3][H], page1 = lds.page[t0 & 3][2 + H];
     for (int t = t0; t < t1; ++t) {
       lds_barrier();
+      ask_left(t + 1);
       if (idle) {  // no row is this wave's: it fetches its share and leaves the matrix pipe to the others
         store_v(v_next);
         load_v(t + 2);
@@ -614,7 +628,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
       for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) S = mfma32(codes_to_bf16(y.k[s >> 1][2 * (s & 1)], y.k[s >> 1][2 * (s & 1) + 1]), q[s], S);
-      float pks = y.ks, plv = y.lv;
+      float pks = y.ks, left, plv = value_exponent(y.lv, &left);
       const int pos = (p0 + rel) * PAGE;
       if (y.len[0] < PAGE || y.len[1] < PAGE || pos + 2 * PAGE - 1 > lim_first) {
         asm volatile("");  // (a branch: the compiler would compare and select in every block)
@@ -655,7 +669,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
         }
         const bf16x8 p = __builtin_convertvector(e, bf16x8);  // (rounded to bf16, as the probabilities over a bf16 cache are)
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(y.v[db][2 * h], y.v[db][2 * h + 1]), p, O[db]);
+        for (int db = 0; db < D / 32; ++db) O[db] = mfma32(codes_to_bf16(y.v[db][2 * h], y.v[db][2 * h + 1], left), p, O[db]);
         __builtin_amdgcn_sched_barrier(0);
       }
       l = fmaf(sum, __builtin_amdgcn_exp2f(-plv), l);

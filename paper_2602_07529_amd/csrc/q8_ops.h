@@ -16,14 +16,30 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return 
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
-// Eight codes as bf16 (exact: e4m3 has four significant bits).
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi) {
+// Eight codes, times a power of two, as bf16 (exact: e4m3 has four significant bits).
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi, float power = 1.f) {
   u32x4 x;
-  x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
-  x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
-  x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
-  x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+  x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false));
+  x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true));
+  x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false));
+  x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true));
   return __builtin_bit_cast(bf16x8, x);
+}
+
+// Value scales z go into the exponent, and the sum of the probabilities takes them out again.  The exponential's results end at 2^-126, so under
+// z = 2^-100, the scale of a page of zeros, a key 2^-27 of the largest would be missing from the sum (2^20 of them: 1 % of it).  So the exponent
+// gets no less than 2^LEAST_VALUE, and a key is missing from 2^-66 of the largest on; the power of two that is left over goes into the values as
+// they become bf16.
+constexpr float LEAST_VALUE = -60.f;
+__device__ __forceinline__ float value_log2(float z) {
+  const float lv = __builtin_amdgcn_logf(z);
+  return lv < -149.f ? -149.f : lv;  // (not minus infinity; no number stays none)
+}
+// What the exponent gets of value_log2's result; *left: the power of two for the values.
+__device__ __forceinline__ float value_exponent(float lv, float* left) {
+  const float t = fminf(floorf(lv) - LEAST_VALUE, 0.f);
+  *left = __builtin_amdgcn_exp2f(t);
+  return lv - t;
 }
 
 __device__ __forceinline__ float other_half(float x) { return __uint_as_float(dag_other_group<32>(__float_as_uint(x))); }  // of lane ^ 32
