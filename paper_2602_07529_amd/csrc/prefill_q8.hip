@@ -162,9 +162,9 @@ __device__ __forceinline__ void sums_again(const ChunkArgs& a, const Place& pl, 
     const size_t mine = H ? at[1] : at[0], key = L >> 2 & 1 ? at[1] : at[0];
     const int plen = H ? len[1] : len[0], n = min(plen, lim - (pg0 + H) * PAGE + 1);
     float2 page = page_scales(a, a.kv.k_scale[mine], a.kv.v_scale[mine], plen);
-    if (n <= 0) page = make_float2(1.f, 0.f);
-    float left;
+    float left;  // (of the page, not of the row: the lane has values for all rows)
     page.y = value_exponent(page.y, &left);
+    if (n <= 0) page = make_float2(1.f, 0.f);
     f32x16 S;
 #pragma unroll
     for (int r = 0; r < 16; ++r) S[r] = 0.f;
@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, 2) k_q8_chunk_few(ChunkArgs a)
       for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) S = mfma32(codes_to_bf16(y.k[s >> 1][2 * (s & 1)], y.k[s >> 1][2 * (s & 1) + 1]), q[s], S);
-      float pks = y.ks, left, plv = value_exponent(y.lv, &left);
+      float pks = y.ks, left, plv = value_exponent(y.lv, &left);  // (left: of the page, not of the row)
       const int pos = (p0 + rel) * PAGE;
       if (y.len[0] < PAGE || y.len[1] < PAGE || pos + 2 * PAGE - 1 > lim_first) {
         asm volatile("");  // (a branch: the compiler would compare and select in every block)
