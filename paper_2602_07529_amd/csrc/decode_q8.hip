@@ -132,8 +132,7 @@ constexpr float Q8_TH = 3.f;
 
 // A block: scores, probabilities, their product with the values.  ks: key scale of the lane's page times |softmax scale| log2(e),
 // lv: log2 of its value scale.  A lane's 16 scores are of one page, so their largest is found among the plain products, one
-// multiply-add gives the exponent with the value scale in it, and the sum of a lane loses that factor again once.  (The exponential's results
-// reach down to 2^-149: on a page of zeros, scale 2^-100, a key loses at most 2^-50 of the largest in the sum, 2^31 of them 2^-19.)
+// multiply-add gives the exponent with the value scale in it (value_exponent), and the sum of a lane loses that factor again once.
 // key0: first key of the block; keys from `lim` on are hidden from the lane's row; len: the smallest lim of the wave; slots from vlen on hold
 // no token.  A wave by itself takes 1,005 cycles for a block at head dimension 128, two waves of a SIMD 512 each, as long as the 16 MFMAs.
 template <int D, bool LIMITS>
@@ -144,6 +143,8 @@ __device__ __forceinline__ void compute_block(Block<D>& b, const bf16x8 (&q)[D /
   for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) S = mfma32(codes_to_bf16(b.k[s >> 1][2 * (s & 1)], b.k[s >> 1][2 * (s & 1) + 1]), q[s], S);
+  float left;  // (of the page, not of the row: the lane has values for all rows)
+  lv = value_exponent(lv, &left);
   if (key0 + 32 > len) {
     asm volatile("");  // (a branch: the compiler would compare and select in every block)
 #pragma unroll
@@ -185,7 +186,7 @@ __device__ __forceinline__ void compute_block(Block<D>& b, const bf16x8 (&q)[D /
 #pragma unroll
   for (int e = 0; e < 2; ++e)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) sums.O[db] = mfma32(codes_to_bf16(b.v[db][2 * e], b.v[db][2 * e + 1]), p[e], sums.O[db]);
+    for (int db = 0; db < D / 32; ++db) sums.O[db] = mfma32(codes_to_bf16(b.v[db][2 * e], b.v[db][2 * e + 1], left), p[e], sums.O[db]);
 }
 
 // Page ids (clamped to the pool) and scales of 64 pages of a slice, a lane each.
@@ -200,7 +201,7 @@ struct Window {
   __device__ __forceinline__ void have(float sc) {
     ks *= fabsf(sc);
     ks = ks < 1.2e-38f ? 1.2e-38f : ks;  // (not zero: hidden keys have scores of minus infinity; no number stays none)
-    lv = __builtin_amdgcn_logf(lv);
+    lv = value_log2(lv);
     asm volatile("" ::"v"(ks), "v"(lv));  // (arrived: a wait for them later would also wait for the blocks in flight)
   }
   static __device__ __forceinline__ float of(float x, int rel, int np, int H) {  // of page rel + H
