@@ -706,15 +706,16 @@ class KvRows:
         n_rows, width = table.shape
         self.c = dag_kv_rows_t(n_rows, PAGE, width, free_pages.numel(), table.data_ptr(), free_pages.data_ptr())
         self.workspace = torch.zeros(int(lib().dag_kv_tables_workspace_bytes(n_rows)), dtype=torch.uint8, device=table.device)
-        self.shared_workspace = None  # of the calls on shared pages
+        self.shared_workspaces, self.shared_forks = [], 0  # of the calls on shared pages, the last one in use; forks that it has room for
 
     def for_shared(self, n_forks=0):
-        """The workspace of dag_kv_fork, dag_kv_release_shared and dag_kv_compact, made at the first of them (outside a capture)."""
-        if self.shared_workspace is None or n_forks > self.shared_forks:
-            self.shared_forks = max(n_forks, self.c.n_rows)
+        """The workspace of dag_kv_fork, dag_kv_release_shared and dag_kv_compact, made at the first of them (outside a capture).  A call with
+        more forks than it has room for gets a larger one, and the old one is kept: graphs that were captured before go on writing to it."""
+        if not self.shared_workspaces or n_forks > self.shared_forks:
+            self.shared_forks = max(n_forks, self.c.n_rows, 2 * self.shared_forks)
             need = int(lib().dag_kv_pages_workspace_bytes(self.c.n_rows, self.c.n_pages, self.shared_forks))
-            self.shared_workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
-        return self.shared_workspace
+            self.shared_workspaces.append(torch.empty(need, dtype=torch.uint8, device=self.table.device))
+        return self.shared_workspaces[-1]
 
 
 def _at(x):
