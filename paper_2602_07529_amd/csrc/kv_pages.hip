@@ -127,7 +127,9 @@ __global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_rows(PagesArgs a) {
   if (blockIdx.x == 0) fork_rows(a);
   else fork_extra(a, (int64_t)(blockIdx.x - 1) * ROW_THREADS + threadIdx.x, (int64_t)(gridDim.x - 1) * ROW_THREADS);
 }
-__global__ void __launch_bounds__(LIST_THREADS) k_kv_fork_lines(PagesArgs a) { fork_line(a, blockIdx.x, threadIdx.x, LIST_THREADS); }
+__global__ void __launch_bounds__(LIST_THREADS) k_kv_fork_lines(PagesArgs a) {
+  for (int f = blockIdx.x; f < a.n_forks; f += gridDim.x) fork_line(a, f, threadIdx.x, LIST_THREADS);
+}
 __global__ void __launch_bounds__(ROW_THREADS) k_kv_fork_whole(PagesArgs a) {
   fork_extra(a, threadIdx.x, ROW_THREADS);
   fork_rows(a);
@@ -412,13 +414,16 @@ int copy_pages(const CopyArgs& a, hipStream_t stream) {
 
 // Entries of the table, and pages, up to which one workgroup does a call as a whole: as long as its turns take no longer than the launches do.
 constexpr int64_t WHOLE_ENTRIES = 8192;
+// Workgroups of a launch at most (its threads are counted in 32 bits); they go on with the rows or forks that are left.
+constexpr int64_t MOST_BLOCKS = 1 << 20;
 
 size_t words_of(int32_t n_pages) { return ((size_t)n_pages + 31) / 32; }
 
 int check_pages(const dag_kv_rows_t* rows, const void* ws, size_t ws_bytes, int64_t n_forks) {
   if (!rows) return DAG_ERR_NULL;
+  // (rows and forks are counted in 32 bits, a workgroup's threads past the last one too)
   if (rows->n_rows < 0 || rows->max_row_pages < 0 || rows->n_pages < 0 || rows->n_pages > INT32_MAX / PAGE || rows->max_row_pages > INT32_MAX / PAGE ||
-      n_forks < 0 || n_forks > INT32_MAX)
+      rows->n_rows > INT32_MAX / PAGE || n_forks < 0 || n_forks > INT32_MAX / PAGE)
     return DAG_ERR_BAD_LEN;
   if (rows->page_size != PAGE) return DAG_ERR_UNSUPPORTED;
   if ((rows->n_rows > 0 && rows->max_row_pages > 0 && !rows->table) || (rows->n_pages > 0 && !rows->free_pages)) return DAG_ERR_NULL;
@@ -478,7 +483,7 @@ extern "C" int dag_kv_fork(const dag_kv_rows_t* rows, int32_t n_forks, const int
   hipLaunchKernelGGL(k_kv_fork_rows, dim3((unsigned)(1 + copies)), dim3(ROW_THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
   if (n_forks > 0) {
-    hipLaunchKernelGGL(k_kv_fork_lines, dim3((unsigned)n_forks), dim3(LIST_THREADS), 0, stream, a);
+    hipLaunchKernelGGL(k_kv_fork_lines, dim3((unsigned)std::min<int64_t>(n_forks, MOST_BLOCKS)), dim3(LIST_THREADS), 0, stream, a);
     DAG_LAUNCH_CHECK();
   }
   return DAG_OK;
@@ -561,7 +566,7 @@ extern "C" int dag_kv_compact(const dag_kv_rows_t* rows, const dag_kv_rows_t* ro
   hipLaunchKernelGGL(k_kv_compact_pages, dim3(1), dim3(ROW_THREADS), 0, stream, a);
   DAG_LAUNCH_CHECK();
   const int page_blocks = (int)std::min<int64_t>(dag_ceil_div(rows->n_pages, PAGE_THREADS), 1024);
-  const int64_t blocks = page_blocks + dag_ceil_div(rows->n_rows, PAGE_THREADS / 64);
+  const int64_t blocks = page_blocks + std::min<int64_t>(dag_ceil_div(rows->n_rows, PAGE_THREADS / 64), MOST_BLOCKS);
   if (blocks > 0) {
     hipLaunchKernelGGL(k_kv_compact_lists, dim3((unsigned)blocks), dim3(PAGE_THREADS), 0, stream, a, page_blocks);
     DAG_LAUNCH_CHECK();
