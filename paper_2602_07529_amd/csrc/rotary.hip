@@ -6,6 +6,7 @@
 // once, which is what bounds it.  A workgroup turns the angles of its tokens into cosines and sines once for all heads (in LDS), and then
 // a thread has units of two 16-byte pieces whose elements are each other's partners (or stay as they are), two on their way together.
 // 18432 tokens of 40 heads of 128 in bf16: 68 us, 5.6 TB/s, with two tokens to a workgroup (four 70, eight 74, sixteen 80; one unit on its way 72, five 73).
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -133,6 +134,7 @@ extern "C" int dag_rope_frequencies(double* freq, int32_t rotary_dim, double the
       (original > 0. && !(high > low)))
     return DAG_ERR_UNSUPPORTED;
   if (!freq) return DAG_ERR_NULL;
+  double table[MAX_HALF];
   for (int m = 0; m < rotary_dim / 2; ++m) {
     const double f = std::pow(theta, -2. * m / rotary_dim);
     double keep = 0.;
@@ -140,8 +142,10 @@ extern "C" int dag_rope_frequencies(double* freq, int32_t rotary_dim, double the
       keep = (original * f / 6.283185307179586477 - low) / (high - low);
       keep = keep < 0. ? 0. : keep > 1. ? 1. : keep;
     }
-    freq[m] = keep * f + (1. - keep) * f / stretch;
+    table[m] = keep * f + (1. - keep) * f / stretch;
+    if (!std::isfinite(table[m])) return DAG_ERR_UNSUPPORTED;  // (a bound of the parts, or a theta or stretch, past what numbers hold)
   }
+  std::copy(table, table + rotary_dim / 2, freq);
   return DAG_OK;
 }
 
