@@ -412,8 +412,13 @@ int copy_pages(const CopyArgs& a, hipStream_t stream) {
   return DAG_OK;
 }
 
-// Entries of the table, and pages, up to which one workgroup does a call as a whole: as long as its turns take no longer than the launches do.
-constexpr int64_t WHOLE_ENTRIES = 8192;
+// One workgroup does a call as a whole as long as its turns take no longer than the launches do: with two lines of the table (rows, or the children of
+// forks) to a wave, up to 4096 pages (2048 to compact) and 4096 entries (2048 of forks).  Whole / in launches, replayed: 24 rows of 64 and 833 pages, 6 forks 5.3 / 7.0 us, release
+// 8.0 / 11.1, compaction 9.0 / 9.4; 32 rows of 128 and 2003 pages 7.0 / 7.4, 12.3 / 13.6, 11.9 / 11.2; 64 rows of 48 (16 forks) 5.9 / 7.1, 12.6 / 11.8,
+// 11.5 / 10.3; 128 rows of 64 and 3589 pages 10.6 / 7.0, 25.3 / 12.4, 15.4 / 10.6; 150 rows of 12 (30 forks) 7.3 / 7.4, 25.1 / 11.9, 14.5 / 10.2.
+inline bool by_one(int64_t lines, const dag_kv_rows_t* rows, int64_t most_entries, int64_t most_pages) {
+  return lines <= 2 * ROW_WAVES && lines * rows->max_row_pages <= most_entries && rows->n_pages <= most_pages;
+}
 // Workgroups of a launch at most (its threads are counted in 32 bits); they go on with the rows or forks that are left.
 constexpr int64_t MOST_BLOCKS = 1 << 20;
 
@@ -474,7 +479,7 @@ extern "C" int dag_kv_fork(const dag_kv_rows_t* rows, int32_t n_forks, const int
   a.refused = refused;
   a.n_forks = n_forks;
   hipStream_t stream = (hipStream_t)stream_;
-  if ((int64_t)n_forks * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
+  if (by_one(n_forks, rows, 2048, 4096)) {
     hipLaunchKernelGGL(k_kv_fork_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
     DAG_LAUNCH_CHECK();
     return DAG_OK;
@@ -504,7 +509,7 @@ extern "C" int dag_kv_release_shared(const dag_kv_rows_t* rows, const int32_t* e
   a.free_count = free_count;
   a.free_count_out = free_count_out;
   hipStream_t stream = (hipStream_t)stream_;
-  if ((int64_t)rows->n_rows * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
+  if (by_one(rows->n_rows, rows, 4096, 4096)) {
     hipLaunchKernelGGL(k_kv_release_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
     DAG_LAUNCH_CHECK();
     return DAG_OK;
@@ -558,7 +563,7 @@ extern "C" int dag_kv_compact(const dag_kv_rows_t* rows, const dag_kv_rows_t* ro
   a.copy_dst = copy_dst;
   a.n_copies = n_copies;
   hipStream_t stream = (hipStream_t)stream_;
-  if ((int64_t)rows->n_rows * rows->max_row_pages <= WHOLE_ENTRIES && rows->n_pages <= WHOLE_ENTRIES) {
+  if (by_one(rows->n_rows, rows, 4096, 2048)) {
     hipLaunchKernelGGL(k_kv_compact_whole, dim3(1), dim3(ROW_THREADS), 0, stream, a);
     DAG_LAUNCH_CHECK();
     return DAG_OK;
