@@ -15,12 +15,14 @@
 // Masks only where a tile has a page that is not full or reaches behind a wave's first row.  A value that is no number is not looked for in the
 // tiles: where the sums of a wave turn out to hold none, it goes over its pages once more (sums_again).
 // What bounds it: the matrix pipes and the power limit, as the bf16 form (1.8 GHz).  16 nodes of 2048 new tokens behind 8192, 32 / 8 heads of 128:
-// 4.2 to 4.5 ms, 1.1 to 1.2 PFLOP/s (a library product of 8192^3 in bf16 1.39); the first form, a barrier and whole blocks a tile, codes to
+// 4.5 to 4.65 ms, 1.1 PFLOP/s (a library product of 8192^3 in bf16 1.39); the first form, a barrier and whole blocks a tile, codes to
 // bf16 by every wave, took 6.8.  Scores as 8-bit products, q in two e4m3 parts, are 9 % faster (4.1), but that pipe's sums are off by 2^-19 of the
-// sum of their terms' magnitudes, the bf16 one's by 2^-24: not kept.  NW 8 against 4: 4.1 / 4.5 ms.
+// sum of their terms' magnitudes, the bf16 one's by 2^-24: not kept.  Eight waves to a workgroup or four, of which a compute unit holds one at dimension 128 as well: 4.6
+// / 7.9 ms.  Probabilities are rounded to bf16 for the second product: a product of 32-bit operands takes sixteen times as long, and two parts of bf16 would double
+// it.  Outputs are off by 0.0023 of their size (2-norm), of which their own rounding is 0.0016.
 //
-// Few pairs (k_q8_chunk_few, nodes of up to 64): a workgroup's four waves share a stretch of the pages for 32 pairs, each a run of its own,
-// straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 35 us (130 MB); three nodes of nine behind 1500: 14,
+// Few pairs (k_q8_chunk_few, nodes of up to 128): a workgroup's four waves share a stretch of the pages for 32 pairs, each a run of its own,
+// straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 36 us (130 MB); three nodes of nine behind 1500: 14.5,
 // of which what a step of a wave takes, half a microsecond to one, is the most.
 //
 // Contexts are cut among workgroups by what that costs (cut); a second launch puts the stretches together.
@@ -58,8 +60,10 @@ struct ChunkArgs {
   float back;         // what takes a logarithm to base 2 of a sum of exponentials back: the inverse of the factor that is in sc, as it was rounded
 };
 
-// New tokens of a node times query heads of a KV head, up to which they are k_q8_chunk_few's.
-constexpr int FEW_PAIRS = 64;
+// New tokens of a node times query heads of a KV head, up to which they are k_q8_chunk_few's.  It reads a context for every 32 of them, k_q8_chunk for every 256.  Few /
+// many, 32 / 8 heads of 128, us: 64 pairs, 2 nodes behind 300 9.5 / 14.5, 48 behind 4000 102 / 182, 120 behind 1500 111 / 155; 96 pairs 9.4 / 16.7, 137 / 175, 145 / 193;
+// 128 pairs 9.5 / 17.3, 171 / 185, 173 / 175.  16 / 4 heads of 64, 128 pairs: 7.4 / 14.6, 56 / 104, 56 / 86; as many KV heads as heads, or one, alike: 0.45 to 1.01.
+constexpr int FEW_PAIRS = 128;
 
 // The pairs pair0 .. of a node, n new tokens from row0 on; pages / np: its list, nstart: place of its first new token in it.
 struct Place {
@@ -117,7 +121,8 @@ __device__ __forceinline__ float2 page_scales(const ChunkArgs& a, float ks, floa
   return len == 0 ? make_float2(1.f, 0.f) : make_float2(ks, value_log2(vs));  // (nobody looks at the scales of a page without tokens)
 }
 
-template <int D, int NW>
+constexpr int NW = 8;  // waves of a workgroup of many pairs
+template <int D>
 struct Lds {
   uint8_t k[3][TILE * D * PAGE * 2];  // [page][half of a piece][piece of 16 dims][slot][8 dims]
   uint8_t v[3][TILE * D * PAGE * 2];  // [page][half of the slots][dim][8 slots]
@@ -245,12 +250,12 @@ __device__ __forceinline__ void store_out(const ChunkArgs& a, size_t at, const f
 
 constexpr float TOP_SUM = 1073741824.f;  // of a block's probabilities relative to the reference: 2^30
 
-template <int D, int NW>
+template <int D>
 __global__ void __launch_bounds__(64 * NW, 2) k_q8_chunk(ChunkArgs a) {
   constexpr int PAIRS = 32 * NW, THREADS = 64 * NW, PIECES = (TILE * D + THREADS - 1) / THREADS;  // 16-byte pieces of the keys of a tile to a thread
   constexpr bool HALF = TILE * D < THREADS;  // the upper half of the waves fetches the values, the lower one the keys
   static_assert(!HALF || 2 * TILE * D == THREADS, "");
-  __shared__ __attribute__((aligned(16))) Lds<D, NW> lds;
+  __shared__ __attribute__((aligned(16))) Lds<D> lds;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, L = lane & 31, H = lane >> 5;
   const int hkv = a.kv.hkv, hk = blockIdx.x % hkv, split = blockIdx.x / hkv % a.splits;
   const int64_t slot = blockIdx.x / hkv / a.splits;
@@ -786,11 +791,14 @@ struct Cut {
 };
 struct Plan {
   Cut few, many;  // slots 0: not launched
-  int blocks, few_rows, waves;
+  int blocks, few_rows;
   size_t floats(int hkv, int D) const { return (few.parts(hkv) + many.parts(hkv)) * (D + 2); }
 };
 // As many stretches as take the least time: rounds of the workgroups that the device holds at once, each as long as its steps through a stretch
 // and what a workgroup costs apart from them, then the second launch and the partial results, which are written and read.  In microseconds.
+// Against calls cut in 1 to 64, what it takes / the fastest, 32 / 8 heads of 128: one token behind 2000 9.8 / 9.8, behind 64000 36 / 32 (in 24); eight nodes of 8 behind 8000
+// 34.6 / 31.6; 128 tokens behind 30000 81 / 80 (uncut 701), 1024 behind 31000 481 / 480 (uncut 748); four nodes of 500 behind 10000, where the host's bound
+// on the items is one over a round, 360 / 305; 64 of 121 behind 6000 uncut, as fastest.
 struct Cost {
   double tile, each, merge;
   int at_once;
@@ -826,12 +834,11 @@ bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, in
     // (eight waves to a workgroup in place of a cut: three nodes of nine behind 1500 16.7 us, cut 14.2; one token behind 2000 11.2, 9.4)
     cut(&p->few, (double)std::min<int64_t>(p->few.slots, n_rows * G / 32 + d->n_nodes) * hkv, tiles, D, Cost{0.4, 5., 4., 512});
   }
-  p->waves = most <= 128 && D == 64 ? 4 : 8;  // (at dimension 128 two workgroups' tiles do not fit a compute unit)
   if (!none && most > FEW_PAIRS) {
-    p->many.pairs = 32 * p->waves;
+    p->many.pairs = 32 * NW;
     p->many.slots = n_rows * G / p->many.pairs + d->n_nodes;  // (the last node's last one is below: find_place)
     const double items = d->n_nodes == 1 ? (double)dag_ceil_div(n_rows * G, p->many.pairs) : (double)n_rows * G / p->many.pairs + 0.5 * d->n_nodes;
-    cut(&p->many, items * hkv, tiles, D, p->waves == 4 ? Cost{D / 64., 6., 5., 512} : Cost{D / 64., 6., 5., 256});
+    cut(&p->many, items * hkv, tiles, D, Cost{D / 64., 6., 5., 256});
   }
   for (const Cut* c : {&p->few, &p->many}) {  // (threads of a launch are counted in 32 bits)
     const int64_t most = (int64_t)1 << 22;
@@ -845,9 +852,9 @@ bool bounds_ok(const dag_paged_prefill_desc_t* d, int64_t n_rows, int32_t hq, in
          hq >= 1 && hq % hkv == 0 && hq / hkv <= 256 && (int64_t)d->max_new * (hq / hkv) <= INT32_MAX && (head_dim == 64 || head_dim == 128);
 }
 
-template <int D, int NW>
+template <int D>
 int launch_many(const ChunkArgs& a, const Cut& c, hipStream_t stream) {
-  hipLaunchKernelGGL((k_q8_chunk<D, NW>), dim3((unsigned)(c.slots * a.kv.hkv * c.splits)), dim3(64 * NW), 0, stream, a);
+  hipLaunchKernelGGL(k_q8_chunk<D>, dim3((unsigned)(c.slots * a.kv.hkv * c.splits)), dim3(64 * NW), 0, stream, a);
   DAG_LAUNCH_CHECK();
   if (c.splits > 1) {
     hipLaunchKernelGGL((k_q8_chunk_merge<D, 32 * NW, false>), dim3((unsigned)(c.slots * a.kv.hkv * (32 * NW / 4))), dim3(256), 0, stream, a);
@@ -869,9 +876,7 @@ int launch(ChunkArgs a, const Plan& p, hipStream_t stream) {
   float* const ws = a.part_o;
   if (p.many.slots > 0) {
     use(p.many, ws);
-    int rc;
-    if constexpr (D == 64) rc = p.waves == 4 ? launch_many<D, 4>(a, p.many, stream) : launch_many<D, 8>(a, p.many, stream);
-    else rc = launch_many<D, 8>(a, p.many, stream);
+    const int rc = launch_many<D>(a, p.many, stream);
     if (rc != DAG_OK) return rc;
   }
   if (p.few.slots == 0) return DAG_OK;

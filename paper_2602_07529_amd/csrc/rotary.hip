@@ -2,10 +2,10 @@
 // head, forward or transposed.
 //
 // Pair m of a head turns by pos * freq[m]: y = factor (x cos - x' sin, x' cos + x sin); transposed, which is what the gradients go through, the
-// angle has the other sign.  Angles are taken in 64 bits, the rotation in 32 for bf16 and in 64 for 32-bit tensors, with one rounding to their type.  Everything is read and written
-// once, which is what bounds it.  A workgroup turns the angles of its tokens into cosines and sines once for all heads (in LDS), and then
+// angle has the other sign.  Angles are taken in 64 bits, the rotation in 32 for
+// bf16 and in 64 for 32-bit tensors, with one rounding to their type.  Everything is read and written once, which is what bounds it.  A workgroup turns the angles of its tokens into cosines and sines once for all heads (in LDS), and then
 // a thread has units of two 16-byte pieces whose elements are each other's partners (or stay as they are), two on their way together.
-// 18432 tokens of 40 heads of 128 in bf16: 68 us, 5.6 TB/s, with two tokens to a workgroup (four 70, eight 74, sixteen 80; one unit on its way 72, five 73).
+// 18432 tokens of 40 heads of 128 in bf16: 67 us, 5.6 TB/s, with two units on their way (one 72, five 73).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -117,7 +117,9 @@ __global__ void __launch_bounds__(THREADS) k_rotary(RotaryArgs a) {
 
 template <bool BF16>
 int launch_rotary(const RotaryArgs& a, hipStream_t stream) {
-  // (a workgroup's chain of frequencies, angles and rows is shared by more tokens where a token has few units)
+  // (a workgroup's chain of frequencies, angles and rows is shared by more tokens where a token has few units: with 1 / 2 / 4 / 8 / 16 tokens, 20000 of 320
+  // units in bf16 take 72 / 73 / 76 / 80 / 84 us, of 80 29 / 21 / 17.5 / 17.5 / 18, of 20 19 / 11 / 10 / 8 / 6.7, of 640 in 32 bits 140 / 147 / 155 / 162 / 164; 1024 of 320
+  // 5.2 / 5.2 / 5.4 / 7.3 / 11.7, of 20 2.8 whichever; 2048 of 320 8.4 / 7.4 / 7.9 / 9.0 / 13.0, of 80 5.0 / 4.1 / 3.9 / 4.4 / 5.8)
   const int units = (a.heads[0] + a.heads[1]) * (a.D / (BF16 ? 16 : 8));
   const int tokens = a.n_tokens < 2048 ? 1 : units >= 192 ? 2 : units >= 48 ? 4 : 16;
   auto* const kernel = tokens == 1 ? k_rotary<BF16, 1> : tokens == 2 ? k_rotary<BF16, 2> : tokens == 4 ? k_rotary<BF16, 4> : k_rotary<BF16, 16>;
