@@ -157,7 +157,8 @@ typedef struct {
 /* A table of frequencies: f = theta^(-2 m / rotary_dim), for contexts `stretch` times as long as those of the training.  original = 0: all are
  * divided by it (positions are interpolated).  original > 0, a length in tokens: by parts, a pair that turns `high` times or more over it keeps
  * f, one that turns `low` times or less has f / stretch, in between the two are mixed in proportion.  `freq` HOST [rotary_dim / 2];
- * rotary_dim even and <= 256.  Errors: DAG_ERR_NULL, DAG_ERR_UNSUPPORTED. */
+ * rotary_dim even and <= 256.  A table that would hold what is no number, or infinite, is refused, and `freq` left as it is.
+ * Errors: DAG_ERR_NULL, DAG_ERR_UNSUPPORTED. */
 int dag_rope_frequencies(double* freq, int32_t rotary_dim, double theta, double stretch, double original, double low, double high);
 
 /* Rotates q [n_tokens][hq][head_dim] and k [n_tokens][hkv][head_dim] (either may be NULL) at pos [n_tokens] into q_out and k_out; a token's heads
@@ -513,7 +514,7 @@ int dag_kv_tables(const dag_kv_rows_t* rows, const int32_t* new_len, const int32
                   const int32_t* pos0, int32_t* pos, int32_t* page_off, int32_t* pages, int64_t max_pages, int32_t* refused,
                   void* ws, size_t ws_bytes, void* stream);
 
-/* Rows that share pages.  extra [n_pages] DEVICE int32 says how many rows hold a page besides its first holder (0 for a page of one row and for a
+/* Rows that share pages (at most 2^27 - 1 rows and forks).  extra [n_pages] DEVICE int32 says how many rows hold a page besides its first holder (0 for a page of one row and for a
  * free one).  dag_kv_tables goes on as before (a row's new tokens only go into a last page of its own: dag_kv_fork sees to that); rows give
  * their pages back through dag_kv_release_shared in the place of dag_kv_release.  Bytes of the DEVICE workspace (8-byte aligned, any contents) of the
  * three calls below, n_forks for dag_kv_fork; calls that overlap need one each. */
@@ -538,9 +539,9 @@ int dag_kv_release_shared(const dag_kv_rows_t* rows, const int32_t* ended, const
 
 /* Moves the pages in use to the front of the pool: with U = n_pages - *free_count the k-th used page (ascending) from U on goes to the k-th free page in
  * front of U.  copy_src / copy_dst [n_pages / 2] get the *n_copies pairs, for dag_kv_copy_pages(_q8) (entries behind them are left as they were);
- * page_map [n_pages] every page's new id, -1 for free ones, for lists other than the table's; extra_out the holders by new id; rows_out (of the
+ * page_map [n_pages] every page's new id, -1 for free ones, for lists other than the table's; extra_out (may be extra) the holders by new id; rows_out (of the
  * same sizes; its arrays may be those of rows) the table's lines with new ids as far as they are held, and the free pages so that the lowest is taken first
- * (entries behind *free_count are left).  The free list has to name every free page once. */
+ * (entries behind *free_count are left).  No other output may overlap an input.  The free list has to name every free page once. */
 int dag_kv_compact(const dag_kv_rows_t* rows, const dag_kv_rows_t* rows_out, const int32_t* row_len, const int32_t* extra, int32_t* extra_out,
                    const int32_t* free_count, int32_t* page_map, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies, void* ws, size_t ws_bytes,
                    void* stream);
