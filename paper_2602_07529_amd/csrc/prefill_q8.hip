@@ -840,9 +840,9 @@ bool plan(const dag_paged_prefill_desc_t* d, int64_t n_rows, int hq, int hkv, in
     const double items = d->n_nodes == 1 ? (double)dag_ceil_div(n_rows * G, p->many.pairs) : (double)n_rows * G / p->many.pairs + 0.5 * d->n_nodes;
     cut(&p->many, items * hkv, tiles, D, Cost{D / 64., 6., 5., 256});
   }
-  for (const Cut* c : {&p->few, &p->many}) {  // (threads of a launch are counted in 32 bits)
-    const int64_t most = (int64_t)1 << 22;
-    if (c->slots > most || hkv > most || c->slots * hkv * c->splits > most || (c->splits > 1 && c->slots * hkv * (c->pairs / 4) > 2 * most)) return false;
+  for (const Cut* c : {&p->few, &p->many}) {  // (threads of a launch, 256 or 512 a workgroup, are counted in 32 bits)
+    const int64_t most = (int64_t)1 << (c == &p->few ? 23 : 22), merge = (int64_t)1 << 23;
+    if (c->slots > most || hkv > most || c->slots * hkv * c->splits > most || (c->splits > 1 && c->slots * hkv * (c->pairs / 4) > merge)) return false;
   }
   return true;
 }
