@@ -116,3 +116,22 @@ def test_chunk_over_tiny_values(new, d, none):
         out = np.delete(out, 7, axis=2)
     want = np.array([of_small(*counts(pages, SMALL, n)) for n in seen])[:, None, None]
     close(out, want, want * SMALL_ROOM)
+
+
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -149, 2.0 ** -127, 2.0 ** -126, 2.0 ** -61, 2.0 ** -60])
+@pytest.mark.parametrize("new", [1, 40])
+def test_chunk_over_value_scales_down_to_zero(new, scale):
+    """Scores of zero: a page of 1.5, one of 256 times the scale, three full ones of the node's own of zeros.  The results are their mean."""
+    cache = cache_of(64)
+    cache.v_pool[TOP] = torch.full((1, 64, 16), 1.5, device=DEV).to(torch.float8_e4m3fn)
+    cache.v_scale[SMALL] = scale
+    q = torch.zeros((new, 4, 64), dtype=torch.bfloat16, device=DEV)
+    pages = [TOP, SMALL, ZEROS, ZEROS, ZEROS]
+    desc = B.PagedPrefillDesc.on_device(1, new, 5, ints([0, new]), ints([0, 5]), ints(pages), ints([16] * 5), ints([2]), ints([48]))
+    out, lse = torch.full_like(q, 7.0), torch.full((new, 4), 7.0, device=DEV)
+    ws = torch.full((max(256, B.dag_prefill_paged_q8_workspace_bytes(desc, cache, new, 4)),), 0xff, dtype=torch.uint8, device=DEV)
+    B.dag_attn_prefill_paged_q8(desc, q, cache, out, ws, lse=lse)
+    seen = (80 - new + 1 + np.arange(new))[:, None, None].astype(np.float64)
+    want = (16 * 1.5 + 16 * 256 * scale) / seen
+    close(out.double().cpu().numpy(), want, want * (2.0 ** -8 + 2.0 ** -20))
+    close(lse.double().cpu().numpy(), np.log(seen[..., 0]), 2.0 ** -20)
