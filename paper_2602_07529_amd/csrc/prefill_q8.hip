@@ -18,8 +18,9 @@
 // 4.5 to 4.65 ms, 1.1 PFLOP/s (a library product of 8192^3 in bf16 1.39); the first form, a barrier and whole blocks a tile, codes to
 // bf16 by every wave, took 6.8.  Scores as 8-bit products, q in two e4m3 parts, are 9 % faster (4.1), but that pipe's sums are off by 2^-19 of the
 // sum of their terms' magnitudes, the bf16 one's by 2^-24: not kept.  Eight waves to a workgroup or four, of which a compute unit holds one at dimension 128 as well: 4.6
-// / 7.9 ms.  Probabilities are rounded to bf16 for the second product: a product of 32-bit operands takes sixteen times as long, and two parts of bf16 would double
-// it.  Outputs are off by 0.0023 of their size (2-norm), of which their own rounding is 0.0016.
+// / 7.9 ms.  Probabilities are rounded to bf16 for the second product: in 32 bits it takes sixteen times as long, in two parts
+// of bf16 twice, and fp16, of three bits more, has them down to 2^-14 of the largest only (many keys behind a large one of small values).  Outputs are off by
+// 0.0023 of their size (2-norm), of which their own rounding is 0.0016.
 //
 // Few pairs (k_q8_chunk_few, nodes of up to 128): a workgroup's four waves share a stretch of the pages for 32 pairs, each a run of its own,
 // straight from memory into registers, and add their sums up in LDS.  One token behind 64,000, 32 / 8 heads: 36 us (130 MB); three nodes of nine behind 1500: 14.5,
